@@ -25,6 +25,14 @@
  *                      (the space-filling-curve reordering of Sec. 4)
  *   avq_gilbert_order  host helper: that order for a 2-D grid of tokens
  *
+ * Beside it stand exact attention and the cache that a server keeps (their
+ * conventions are given with them):
+ *
+ *   avq_prompt_attention_fwd  exact attention of packed prompts
+ *   avq_cache_append   keys and values into a paged cache, with the rotation
+ *   avq_cache_gather   cached positions read back
+ *   avq_cache_attention_fwd  exact attention of the newest tokens over the cache
+ *
  * Conventions shared by every call:
  *   - Every array argument is a DEVICE pointer owned by the caller, contiguous,
  *     row-major and 16-byte aligned. Inputs are never written. Outputs are
@@ -363,6 +371,162 @@ avq_status_t avq_codebook_update(avq_dtype_t dtype, int32_t B, int32_t H, int32_
                                  int32_t M0, int32_t Ch, float lambda, const float* sums,
                                  const int32_t* counts, float* S, float* Nema, void* Cp_out,
                                  void* Cc_out, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Exact attention of packed prompts, and the paged cache (serving).
+ *
+ * These calls take tokens of several sequences packed one after the other:
+ * rows of tokens, each row its heads [H][d] contiguous, q_stride / k_stride /
+ * v_stride elements from one token's row to the next (at least H*d, a multiple
+ * of 16 bytes, at most 2^22: slices of a fused projection need no copy).
+ * cu [S + 1] (int32, device): sequence s owns rows cu[s] .. cu[s + 1] - 1; cu
+ * must not decrease and may leave rows behind cu[S], whose outputs are left as
+ * they were. Values outside [0, T] are taken as the nearest of 0 and T.
+ * Hq query heads share Hkv key-value heads: head h reads h / (Hq / Hkv).
+ * Sizes: d in {64, 128}; Hq <= 1024, a multiple of Hkv; S <= 2^20; T <= 2^24
+ * packed tokens, 0 included (nothing is then written). Element counts may pass
+ * 2^31. An infinity or NaN in a sequence's inputs leaves the outputs of other
+ * sequences as they are; the sequence's own are unspecified.
+ */
+
+/*
+ * avq_prompt_attention_fwd - exact softmax attention (Eq. (standardattention))
+ * of packed sequences.
+ *
+ * With Lq queries and Lk keys in sequence s, S_ij = scale q_i . k_j:
+ *   lse_i = ln sum_j exp(S_ij),  Y_i = sum_j exp(S_ij - lse_i) v_j
+ * over j < Lk, and with causal = 1 only j <= i + Lk - Lq: the queries are the
+ * last Lq of the Lk positions (a whole prompt when Lq = Lk, a chunk behind
+ * earlier keys when Lq < Lk). A query that sees no key (Lk = 0, or causal with
+ * Lq > Lk + i) gets Y_i = 0 and lse_i = -inf.
+ *
+ *   scale  > 0, finite;  causal  0 or 1
+ *   Q      [Tq] rows of [Hq][d], K, V [Tk] rows of [Hkv][d], dtype
+ *   cu_q, cu_k  [S + 1] int32 (they may be one array)
+ *   Y      [Tq][Hq][d] dtype, contiguous, out
+ *   lse    [Tq][Hq] fp32, out, nullable
+ * Arithmetic as avq_attention_fwd: bf16 products with fp32 accumulation and
+ * fp32 softmax state, weights rounded to bf16 for the value product; fp32
+ * throughout for fp32.
+ */
+avq_status_t avq_prompt_attention_fwd(avq_dtype_t dtype, int32_t S, int32_t Tq, int32_t Tk,
+                                      int32_t Hq, int32_t Hkv, int32_t d, float scale,
+                                      int32_t causal, const void* Q, int64_t q_stride,
+                                      const void* K, int64_t k_stride, const void* V,
+                                      int64_t v_stride, const int32_t* cu_q, const int32_t* cu_k,
+                                      void* Y, float* lse, void* stream);
+
+/* Element format of a paged cache: the calls' dtype, or 4 bits. */
+typedef int32_t avq_cache_t;
+enum { AVQ_CACHE_NATIVE = 0, AVQ_CACHE_FP4 = 1 };
+
+/*
+ * Bytes E of one (page, key-value head). The cache is one array
+ * [n_pages][Hkv][E]; a page holds page_size (16, 32, 64, 128 or 256)
+ * consecutive positions of a sequence:
+ *   native  K [page_size][d], V [page_size/8][d][8], dtype
+ *   fp4     K codes [page_size][d/2], V codes [page_size/8][d/2][8],
+ *           K scales [page_size][d/32], V scales [page_size/8][d/32][8]: bytes.
+ *           A code byte holds dimensions 2i (low 4 bits) and 2i+1 of one
+ *           position as e2m1: sign, then 0, 0.5, 1, 1.5, 2, 3, 4, 6 for codes
+ *           0 .. 7. A scale byte e in 1 .. 254 is 2^(e - 127), shared by 32
+ *           dimensions of one position: 4.25 bits per element.
+ * block_table [S][max_pages] (int32, device) names the page of positions
+ * i*page_size .. (i+1)*page_size - 1 of each sequence in column i; columns past
+ * a sequence's length are not read. A position without a page (past max_pages,
+ * or an entry outside [0, n_pages)) is not written by avq_cache_append, reads
+ * as 0 in avq_cache_gather and takes no part in avq_cache_attention_fwd.
+ * max_pages * page_size <= 2^30. Returns -1 for unsupported arguments.
+ */
+int64_t avq_cache_page_bytes(avq_dtype_t dtype, avq_cache_t format, int32_t page_size, int32_t d);
+
+/*
+ * avq_cache_append - appends new keys and values to the cache, with the keys
+ * (and the queries of the same tokens) rotated to their positions.
+ *
+ * Token i of sequence s (packed row cu[s] + i) has position start[s] + i. The
+ * first rot dimensions are rotated in pairs (a, b) = dimensions (i, i + rot/2),
+ * or with interleaved = 1 (2i, 2i + 1), i < rot/2, by the angle whose cosine
+ * and sine the caller gives for (position, i):
+ *   a' = a cos - b sin,  b' = b cos + a sin      (fp32)
+ * Rotated queries and keys are rounded once to dtype. In the 4-bit cache each
+ * 32 dimensions of a rotated key (before that rounding) and of a value take
+ * the smallest power-of-two scale that leaves no magnitude above 6, and every
+ * element the nearest code (ties to the even code).
+ *
+ *   rot          0 (no rotation; cos, sin and n_pos are then not used) or a
+ *                multiple of 16 up to d
+ *   cos, sin     [n_pos][rot/2] fp32; nothing is written for a token whose
+ *                position lies outside [0, n_pos)
+ *   Q            [T] rows of [Hq][d], nullable with Q_out (Hq and q_stride are
+ *                then not used)
+ *   K, V         [T] rows of [Hkv][d], dtype
+ *   cu           [S + 1]; NULL: one token per sequence, T = S
+ *   start        [S] int32, tokens already cached; a negative one makes the
+ *                sequence take no part
+ *   block_table  [S][max_pages] int32; the pages of the call's positions must
+ *                be pairwise different (shared pages are read only)
+ *   cache        [n_pages][Hkv][E], in/out: only the new positions are written
+ *   Q_out        [T][Hq][d] dtype, out (may be Q itself if Q is contiguous)
+ *   K_out        [T][Hkv][d] dtype, out, nullable: the rotated keys (may be K
+ *                itself if K is contiguous)
+ * One launch. Otherwise outputs overlap no input.
+ */
+avq_status_t avq_cache_append(avq_dtype_t dtype, avq_cache_t format, int32_t S, int32_t T,
+                              int32_t Hq, int32_t Hkv, int32_t d, int32_t n_pages,
+                              int32_t page_size, int32_t max_pages, int32_t rot, int32_t n_pos,
+                              int32_t interleaved, const void* Q, int64_t q_stride, const void* K,
+                              int64_t k_stride, const void* V, int64_t v_stride,
+                              const int32_t* cu, const int32_t* start, const int32_t* block_table,
+                              const float* cos, const float* sin, void* cache, void* Q_out,
+                              void* K_out, void* stream);
+
+/*
+ * avq_cache_gather - cached positions read back as packed rows: row cu[s] + i
+ * is position start[s] + i of sequence s, in dtype (4-bit values are exact in
+ * either type). With start = 0 and cu the cached lengths these are the K and V
+ * that avq_prompt_attention_fwd takes for a chunk behind a cached prefix.
+ *
+ *   cu           [S + 1], start [S], block_table [S][max_pages]: int32
+ *   K, V         [T][Hkv][d] dtype, contiguous, out
+ */
+avq_status_t avq_cache_gather(avq_dtype_t dtype, avq_cache_t format, int32_t S, int32_t T,
+                              int32_t Hkv, int32_t d, int32_t n_pages, int32_t page_size,
+                              int32_t max_pages, const void* cache, const int32_t* cu,
+                              const int32_t* start, const int32_t* block_table, void* K, void* V,
+                              void* stream);
+
+/* Bytes of the workspace of avq_cache_attention_fwd (-1 for unsupported
+ * sizes). Its contents need not be set and mean nothing afterwards; calls that
+ * may run at the same time need one each. */
+int64_t avq_cache_attention_workspace(int32_t S, int32_t n_q, int32_t Hq, int32_t Hkv, int32_t d);
+
+/*
+ * avq_cache_attention_fwd - exact softmax attention of the n_q newest tokens of
+ * every sequence over its cache (single tokens: n_q = 1).
+ *
+ * lens[s] positions of sequence s are cached, the n_q tokens' own keys and
+ * values among them (appended before). Token i < n_q sees the positions
+ * j < lens[s] - (n_q - 1 - i). Y and lse as in avq_prompt_attention_fwd; a
+ * token that sees no position (lens[s] = 0: an idle entry of a padded batch)
+ * gets 0 and -inf. lens is taken as at least 0 and at most
+ * max_pages * page_size.
+ *
+ *   n_q          1 .. 16
+ *   Q            [S * n_q] rows of [Hq][d], dtype, q_stride as above
+ *   cache, block_table  as above; lens [S] int32
+ *   Y            [S][n_q][Hq][d] dtype, out;  lse [S][n_q][Hq] fp32, nullable
+ *   workspace    avq_cache_attention_workspace() bytes
+ * Two launches (one where no sequence can hold more than 128 positions). What
+ * lies in cache slots behind a sequence's length has no effect, whatever it is.
+ */
+avq_status_t avq_cache_attention_fwd(avq_dtype_t dtype, avq_cache_t format, int32_t S, int32_t n_q,
+                                     int32_t Hq, int32_t Hkv, int32_t d, int32_t n_pages,
+                                     int32_t page_size, int32_t max_pages, float scale,
+                                     const void* Q, int64_t q_stride, const void* cache,
+                                     const int32_t* lens, const int32_t* block_table, void* Y,
+                                     float* lse, void* workspace, int64_t workspace_bytes,
+                                     void* stream);
 
 #ifdef __cplusplus
 }

@@ -27,7 +27,9 @@ _DTYPES = {torch.float32: AVQ_F32, torch.bfloat16: AVQ_BF16}
 SYMBOLS = ("avq_version", "avq_last_error", "avq_packed_bytes", "avq_assign",
            "avq_aggregate", "avq_attention_fwd", "avq_attention_fwd_tiled",
            "avq_codebook_update", "avq_attention_fwd_ordered", "avq_gilbert_order",
-           "avq_pack_aggregates", "avq_assign_aggregate")
+           "avq_pack_aggregates", "avq_assign_aggregate", "avq_prompt_attention_fwd",
+           "avq_cache_page_bytes", "avq_cache_append", "avq_cache_gather",
+           "avq_cache_attention_workspace", "avq_cache_attention_fwd")
 IMPORTANCE_TILE = 64  # parents per codeword tile of attention_fwd(tiled_importance=True)
 
 
@@ -68,6 +70,20 @@ def lib():
         L.avq_pack_aggregates.argtypes = [ctypes.c_int, i32, i32, i32, i32, i32, vp, vp, vp, vp]
         L.avq_assign_aggregate.argtypes = [ctypes.c_int, i32, i32, i32, i32, i32, i32,
                                            vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+        i64, ci, cf = ctypes.c_int64, ctypes.c_int, ctypes.c_float
+        L.avq_prompt_attention_fwd.argtypes = [ci, i32, i32, i32, i32, i32, i32, cf, i32, vp, i64,
+                                               vp, i64, vp, i64, vp, vp, vp, vp, vp]
+        L.avq_cache_page_bytes.argtypes = [ci, ci, i32, i32]
+        L.avq_cache_page_bytes.restype = i64
+        L.avq_cache_append.argtypes = [ci, ci] + [i32] * 11 + [vp, i64, vp, i64, vp, i64] + [vp] * 9
+        L.avq_cache_gather.argtypes = [ci, ci] + [i32] * 7 + [vp] * 7
+        L.avq_cache_attention_workspace.argtypes = [i32] * 5
+        L.avq_cache_attention_workspace.restype = i64
+        L.avq_cache_attention_fwd.argtypes = [ci, ci] + [i32] * 8 + [cf, vp, i64, vp, vp, vp, vp,
+                                                                     vp, vp, i64, vp]
+        for name in ("avq_prompt_attention_fwd", "avq_cache_append", "avq_cache_gather",
+                     "avq_cache_attention_fwd"):
+            getattr(L, name).restype = ci
         for name in ("avq_assign", "avq_aggregate", "avq_attention_fwd", "avq_pack_aggregates",
                      "avq_assign_aggregate",
                      "avq_attention_fwd_tiled", "avq_codebook_update",
@@ -320,3 +336,252 @@ def gilbert_order(width: int, height: int):
     _check(lib().avq_gilbert_order(int(width), int(height), _ptr(order), _ptr(rank)))
     return order, rank
 
+
+
+# ---- exact attention of packed prompts, and the paged cache ------------------
+
+
+def _launch_stream(stream, device: torch.device):
+    """The stream a call runs on, which must be one of the tensors' device: the
+    library launches on the current device."""
+    s = torch.cuda.current_stream() if stream is None else stream
+    if s.device != device or torch.cuda.current_device() != device.index:
+        raise ValueError(f"tensors on {device}: the current device is "
+                         f"cuda:{torch.cuda.current_device()}, the stream's {s.device}")
+    return s
+
+
+def _same_device(ref: torch.Tensor, **tensors) -> None:
+    for name, t in tensors.items():
+        if t is not None and t.device != ref.device:
+            raise ValueError(f"{name} is on {t.device}, expected {ref.device}")
+
+
+def _empty(stream, shape, dtype, device):
+    """An output, allocated on the stream the call runs on: the allocator then
+    reuses its memory only behind the call."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _rows(t: torch.Tensor, name: str, H=None, d=None, dtype=None) -> int:
+    """Checks packed token rows [T, H, d] with contiguous heads; returns the
+    elements from one token to the next."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError(f"{name} must be a tensor on the GPU")
+    if dtype is not None and t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.dim() != 3 or (H is not None and t.shape[1] != H) or (d is not None and t.shape[2] != d):
+        raise ValueError(f"{name} must be [tokens, {'heads' if H is None else H}, "
+                         f"{'d' if d is None else d}], got {tuple(t.shape)}")
+    T, h, w = t.shape
+    if (w > 1 and t.stride(2) != 1) or (h > 1 and t.stride(1) != w):
+        raise ValueError(f"{name}: the heads of a token must be contiguous")
+    return t.stride(0) if T > 1 else h * w
+
+
+def prompt_attention_fwd(Q, K, V, cu_q, cu_k, scale: float, causal: bool = True, Y=None,
+                         with_lse: bool = False, lse=None, stream=None):
+    """Exact attention of packed sequences (``avq_prompt_attention_fwd``).
+
+    Q [Tq, Hq, d], K and V [Tk, Hkv, d]: packed token rows (a token's heads
+    contiguous; slices of a fused projection are taken as they are). cu_q,
+    cu_k: int32 [S + 1] on the GPU. With ``causal`` the queries are the last
+    ones of their sequence's keys. Rows behind the last sequence are left as
+    they were. Returns Y [Tq, Hq, d], or (Y, lse) with ``with_lse`` (lse: fp32
+    [Tq, Hq]).
+    """
+    q_stride = _rows(Q, "Q")
+    Tq, Hq, d = Q.shape
+    k_stride = _rows(K, "K", d=d, dtype=Q.dtype)
+    Tk, Hkv = K.shape[0], K.shape[1]
+    v_stride = _rows(V, "V", Hkv, d, Q.dtype)
+    if V.shape[0] != Tk:
+        raise ValueError(f"V must have {Tk} tokens, got {V.shape[0]}")
+    _dev(cu_q, "cu_q", torch.int32)
+    _dev(cu_k, "cu_k", torch.int32, cu_q.shape)
+    if cu_q.dim() != 1 or cu_q.shape[0] < 2:
+        raise ValueError(f"cu_q must be [sequences + 1], got {tuple(cu_q.shape)}")
+    s = _launch_stream(stream, Q.device)
+    if Y is None:
+        Y = _empty(stream, (Tq, Hq, d), Q.dtype, Q.device)
+    _dev(Y, "Y", Q.dtype, (Tq, Hq, d))
+    if with_lse and lse is None:
+        lse = _empty(stream, (Tq, Hq), torch.float32, Q.device)
+    if lse is not None:
+        _dev(lse, "lse", torch.float32, (Tq, Hq))
+    _same_device(Q, K=K, V=V, cu_q=cu_q, cu_k=cu_k, Y=Y, lse=lse)
+    _check(lib().avq_prompt_attention_fwd(
+        _dtype_code(Q), cu_q.shape[0] - 1, Tq, Tk, Hq, Hkv, d, float(scale), int(bool(causal)),
+        _ptr(Q), q_stride, _ptr(K), k_stride, _ptr(V), v_stride, _ptr(cu_q), _ptr(cu_k), _ptr(Y),
+        _ptr(lse), s.cuda_stream))
+    return (Y, lse) if with_lse else Y
+
+
+def cache_page_bytes(dtype: torch.dtype, page_size: int, d: int, fp4: bool = False) -> int:
+    """Bytes of one (page, key-value head) of a paged cache: the cache is a
+    uint8 tensor [n_pages, Hkv, cache_page_bytes(...)]."""
+    if dtype not in _DTYPES:
+        raise ValueError(f"unsupported dtype {dtype}: use float32 or bfloat16")
+    n = lib().avq_cache_page_bytes(_DTYPES[dtype], int(bool(fp4)), page_size, d)
+    if n < 0:
+        raise ValueError(f"unsupported page_size={page_size} d={d}")
+    return n
+
+
+_cache_page_bytes_of = functools.lru_cache(maxsize=256)(cache_page_bytes)
+
+
+def _cache(cache, block_table, dtype, page_size, d, fp4, S=None):
+    """Checks a cache and its block table; returns (n_pages, Hkv, S, max_pages)."""
+    _dev(cache, "cache", torch.uint8)
+    if cache.dim() != 3:
+        raise ValueError(f"cache must be [pages, heads, page bytes], got {tuple(cache.shape)}")
+    n_pages, Hkv, E = cache.shape
+    need = _cache_page_bytes_of(dtype, page_size, d, bool(fp4))
+    if E != need:
+        raise ValueError(f"cache holds {E} bytes per page and head, expected {need}")
+    _dev(block_table, "block_table", torch.int32)
+    if block_table.dim() != 2 or (S is not None and block_table.shape[0] != S):
+        raise ValueError(f"block_table must be [{'sequences' if S is None else S}, pages], "
+                         f"got {tuple(block_table.shape)}")
+    return n_pages, Hkv, block_table.shape[0], block_table.shape[1]
+
+
+def cache_append(K, V, cache, block_table, start, page_size: int, cu=None, Q=None, cos=None,
+                 sin=None, interleaved: bool = False, fp4: bool = False, Q_out=None,
+                 with_K: bool = False, K_out=None, stream=None):
+    """Appends keys (rotated to their positions) and values to a paged cache
+    (``avq_cache_append``), and rotates the same tokens' queries.
+
+    K, V [T, Hkv, d] and Q [T, Hq, d]: packed token rows as for
+    ``prompt_attention_fwd``; cu int32 [S + 1], or None for one token per
+    sequence (T = S); start int32 [S]: tokens cached before; cos, sin fp32
+    [n_pos, rot / 2] (None: no rotation). The cache is written in place.
+    Returns (Q_out, K_out): the rotated queries (None without Q) and, with
+    ``with_K`` or a buffer, the rotated keys (otherwise None).
+    """
+    k_stride = _rows(K, "K")
+    T, Hkv, d = K.shape
+    v_stride = _rows(V, "V", Hkv, d, K.dtype)
+    if V.shape[0] != T:
+        raise ValueError(f"V must have {T} tokens, got {V.shape[0]}")
+    _dev(start, "start", torch.int32)
+    if start.dim() != 1:
+        raise ValueError(f"start must be [sequences], got {tuple(start.shape)}")
+    S = start.shape[0]
+    n_pages, heads, _, max_pages = _cache(cache, block_table, K.dtype, page_size, d, fp4, S)
+    if heads != Hkv:
+        raise ValueError(f"cache holds {heads} heads, expected {Hkv}")
+    if cu is not None:
+        _dev(cu, "cu", torch.int32, (S + 1,))
+    rot = n_pos = 0
+    if (cos is None) != (sin is None):
+        raise ValueError("cos and sin come together")
+    if cos is not None:
+        _dev(cos, "cos", torch.float32)
+        _dev(sin, "sin", torch.float32, cos.shape)
+        if cos.dim() != 2:
+            raise ValueError(f"cos must be [positions, rot / 2], got {tuple(cos.shape)}")
+        n_pos, rot = cos.shape[0], 2 * cos.shape[1]
+        if rot == 0:
+            raise ValueError("cos holds no angles: pass None for no rotation")
+    s = _launch_stream(stream, K.device)
+    Hq, q_stride = Hkv, 0
+    if Q is not None:
+        q_stride = _rows(Q, "Q", d=d, dtype=K.dtype)
+        Hq = Q.shape[1]
+        if Q.shape[0] != T:
+            raise ValueError(f"Q must have {T} tokens, got {Q.shape[0]}")
+        if Q_out is None:
+            Q_out = _empty(stream, (T, Hq, d), Q.dtype, Q.device)
+        _dev(Q_out, "Q_out", Q.dtype, (T, Hq, d))
+    elif Q_out is not None:
+        raise ValueError("Q_out without Q")
+    if K_out is None and with_K:
+        K_out = _empty(stream, (T, Hkv, d), K.dtype, K.device)
+    if K_out is not None:
+        _dev(K_out, "K_out", K.dtype, (T, Hkv, d))
+    _same_device(K, V=V, cache=cache, block_table=block_table, start=start, cu=cu, Q=Q, cos=cos,
+                 sin=sin, Q_out=Q_out, K_out=K_out)
+    _check(lib().avq_cache_append(
+        _dtype_code(K), int(bool(fp4)), S, T, Hq, Hkv, d, n_pages, page_size, max_pages, rot, n_pos,
+        int(bool(interleaved)), _ptr(Q), q_stride, _ptr(K), k_stride, _ptr(V), v_stride, _ptr(cu),
+        _ptr(start), _ptr(block_table), _ptr(cos), _ptr(sin), _ptr(cache), _ptr(Q_out),
+        _ptr(K_out), s.cuda_stream))
+    return Q_out, K_out
+
+
+def cache_gather(cache, block_table, start, cu, T: int, page_size: int, dtype, d: int,
+                 fp4: bool = False, K=None, V=None, stream=None):
+    """Cached positions start[s] + i as packed rows cu[s] + i
+    (``avq_cache_gather``). Returns (K, V), [T, Hkv, d] in ``dtype``."""
+    n_pages, Hkv, S, max_pages = _cache(cache, block_table, dtype, page_size, d, fp4)
+    _dev(start, "start", torch.int32, (S,))
+    _dev(cu, "cu", torch.int32, (S + 1,))
+    s = _launch_stream(stream, cache.device)
+    if K is None:
+        K = _empty(stream, (T, Hkv, d), dtype, cache.device)
+    if V is None:
+        V = _empty(stream, (T, Hkv, d), dtype, cache.device)
+    _dev(K, "K", dtype, (T, Hkv, d))
+    _dev(V, "V", dtype, (T, Hkv, d))
+    _same_device(cache, block_table=block_table, start=start, cu=cu, K=K, V=V)
+    _check(lib().avq_cache_gather(
+        _DTYPES[dtype], int(bool(fp4)), S, T, Hkv, d, n_pages, page_size, max_pages, _ptr(cache),
+        _ptr(cu), _ptr(start), _ptr(block_table), _ptr(K), _ptr(V), s.cuda_stream))
+    return K, V
+
+
+def cache_attention_workspace(S: int, n_q: int, Hq: int, Hkv: int, d: int) -> int:
+    """Bytes of the workspace of ``cache_attention_fwd``."""
+    n = lib().avq_cache_attention_workspace(S, n_q, Hq, Hkv, d)
+    if n < 0:
+        raise ValueError(f"unsupported sizes S={S} n_q={n_q} Hq={Hq} Hkv={Hkv} d={d}")
+    return n
+
+
+_cache_workspace_of = functools.lru_cache(maxsize=256)(cache_attention_workspace)
+
+
+def cache_attention_fwd(Q, cache, block_table, lens, page_size: int, scale: float,
+                        fp4: bool = False, Y=None, with_lse: bool = False, lse=None,
+                        workspace=None, stream=None):
+    """Exact attention of each sequence's newest tokens over its paged cache
+    (``avq_cache_attention_fwd``).
+
+    Q [S, n_q, Hq, d]; lens int32 [S]: cached positions, the n_q tokens' own
+    among them. workspace: a uint8 tensor of ``cache_attention_workspace(...)``
+    bytes (allocated if not given). Returns Y [S, n_q, Hq, d], or (Y, lse) with
+    ``with_lse`` (lse: fp32 [S, n_q, Hq]).
+    """
+    if not isinstance(Q, torch.Tensor) or not Q.is_cuda:
+        raise ValueError("Q must be a tensor on the GPU")
+    if Q.dim() != 4:
+        raise ValueError(f"Q must be [sequences, tokens, heads, d], got {tuple(Q.shape)}")
+    S, n_q, Hq, d = Q.shape
+    if S > 1 and n_q > 1 and Q.stride(0) != n_q * Q.stride(1):
+        raise ValueError("Q: the tokens must be evenly spaced")
+    q_stride = _rows(Q.flatten(0, 1) if n_q == 1 or S == 1 else Q.view(S * n_q, Hq, d), "Q")
+    n_pages, Hkv, _, max_pages = _cache(cache, block_table, Q.dtype, page_size, d, fp4, S)
+    _dev(lens, "lens", torch.int32, (S,))
+    s = _launch_stream(stream, Q.device)
+    if Y is None:
+        Y = _empty(stream, (S, n_q, Hq, d), Q.dtype, Q.device)
+    _dev(Y, "Y", Q.dtype, (S, n_q, Hq, d))
+    if with_lse and lse is None:
+        lse = _empty(stream, (S, n_q, Hq), torch.float32, Q.device)
+    if lse is not None:
+        _dev(lse, "lse", torch.float32, (S, n_q, Hq))
+    if workspace is None:
+        workspace = _empty(stream, (_cache_workspace_of(S, n_q, Hq, Hkv, d),), torch.uint8, Q.device)
+    _dev(workspace, "workspace", torch.uint8)
+    _same_device(Q, cache=cache, block_table=block_table, lens=lens, Y=Y, lse=lse,
+                 workspace=workspace)
+    _check(lib().avq_cache_attention_fwd(
+        _dtype_code(Q), int(bool(fp4)), S, n_q, Hq, Hkv, d, n_pages, page_size, max_pages,
+        float(scale), _ptr(Q), q_stride, _ptr(cache), _ptr(lens), _ptr(block_table), _ptr(Y),
+        _ptr(lse), _ptr(workspace), workspace.numel(), s.cuda_stream))
+    return (Y, lse) if with_lse else Y

@@ -24,7 +24,8 @@ ROOT = PKG.parent
 CSRC = PKG / "csrc"
 LIB = PKG / "libavq.so"
 SOURCES = ["avq_api.hip", "avq_assign.hip", "avq_aggregate.hip", "avq_attention.hip",
-           "avq_codebook.hip", "avq_order.hip", "avq_pack.hip"]
+           "avq_codebook.hip", "avq_order.hip", "avq_pack.hip", "avq_prompt.hip", "avq_cache.hip",
+           "avq_cache_attention.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 COMPILE_FLAGS = [

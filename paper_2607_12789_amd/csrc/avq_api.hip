@@ -7,6 +7,7 @@
 #include <atomic>
 
 #include "../../include/avq.h"
+#include "avq_cache.hpp"
 #include "avq_common.hpp"
 #include "avq_packed.hpp"
 
@@ -309,6 +310,221 @@ avq_status_t avq_gilbert_order(int32_t width, int32_t height, int32_t* order, in
   if (rank)
     for (long long k = 0; k < n; ++k) rank[order[k]] = (int32_t)k;
   return ok();
+}
+
+}  // extern "C"
+
+// ---- exact attention of packed prompts and the paged cache -------------------------------
+
+namespace {
+
+constexpr int64_t kMaxStride = 1 << 22;  // elements between tokens: 64 rows stay below 2^31 bytes
+constexpr int kMaxHeads = 1024;
+constexpr int kMaxDrafts = 16;
+
+avq_status_t check_heads(const char* name, avq_dtype_t dtype, int32_t S, int32_t Hq, int32_t Hkv,
+                         int32_t d) {
+  if (dtype != AVQ_F32 && dtype != AVQ_BF16)
+    return fail(AVQ_ERR_INVALID_ARG, "%s: unknown dtype %d", name, (int)dtype);
+  if (S < 1 || Hq < 1 || Hkv < 1 || d < 1)
+    return fail(AVQ_ERR_INVALID_ARG, "%s: sizes must be positive (S=%d Hq=%d Hkv=%d d=%d)", name, S,
+                Hq, Hkv, d);
+  if (Hq % Hkv != 0)
+    return fail(AVQ_ERR_INVALID_ARG, "%s: Hq=%d must be a multiple of Hkv=%d", name, Hq, Hkv);
+  if (d != 64 && d != 128) return fail(AVQ_ERR_UNSUPPORTED, "%s: d=%d: only 64 and 128", name, d);
+  if (Hq > kMaxHeads) return fail(AVQ_ERR_UNSUPPORTED, "%s: Hq=%d: at most %d", name, Hq, kMaxHeads);
+  if (S > (1 << 20)) return fail(AVQ_ERR_UNSUPPORTED, "%s: S=%d: at most 2^20 sequences", name, S);
+  return AVQ_OK;
+}
+
+avq_status_t check_stride(const char* name, const char* what, avq_dtype_t dtype, int64_t stride,
+                          int32_t H, int32_t d) {
+  const int unit = dtype == AVQ_BF16 ? 8 : 4;
+  if (stride < (int64_t)H * d || stride % unit != 0)
+    return fail(AVQ_ERR_INVALID_ARG,
+                "%s: %s=%lld must be at least heads * d = %lld and a multiple of 16 bytes", name,
+                what, (long long)stride, (long long)H * d);
+  if (stride > kMaxStride)
+    return fail(AVQ_ERR_UNSUPPORTED, "%s: %s=%lld: at most 2^22", name, what, (long long)stride);
+  return AVQ_OK;
+}
+
+avq_status_t check_scale(const char* name, float scale) {
+  if (!(scale > 0.f && scale <= 3.0e38f))
+    return fail(AVQ_ERR_INVALID_ARG, "%s: scale=%g must be positive and finite", name, (double)scale);
+  return AVQ_OK;
+}
+
+avq_status_t check_cache(const char* name, avq_cache_t format, int32_t n_pages, int32_t page_size,
+                         int32_t max_pages) {
+  if (format != AVQ_CACHE_NATIVE && format != AVQ_CACHE_FP4)
+    return fail(AVQ_ERR_INVALID_ARG, "%s: unknown cache format %d", name, (int)format);
+  if (n_pages < 1 || max_pages < 1)
+    return fail(AVQ_ERR_INVALID_ARG, "%s: n_pages=%d and max_pages=%d must be positive", name,
+                n_pages, max_pages);
+  if (page_size < 16 || page_size > 256 || (page_size & (page_size - 1)) != 0)
+    return fail(AVQ_ERR_UNSUPPORTED, "%s: page_size=%d: only 16, 32, 64, 128, 256", name, page_size);
+  if ((int64_t)max_pages * page_size > (1LL << 30))
+    return fail(AVQ_ERR_UNSUPPORTED, "%s: max_pages * page_size = %lld: at most 2^30 positions", name,
+                (long long)max_pages * page_size);
+  return AVQ_OK;
+}
+
+avq_status_t misaligned(const char* name) {
+  return fail(AVQ_ERR_INVALID_ARG, "%s: arrays must be 16-byte aligned", name);
+}
+avq_status_t null_pointer(const char* name) {
+  return fail(AVQ_ERR_INVALID_ARG, "%s: null pointer argument", name);
+}
+
+// calls launch<T, D> for the dtype and head width
+#define AVQ_BY_TYPE(launch, ...)                                                        \
+  (dtype == AVQ_BF16 ? (d == 64 ? avq::launch<avq::bf16, 64>(__VA_ARGS__)               \
+                                : avq::launch<avq::bf16, 128>(__VA_ARGS__))             \
+                     : (d == 64 ? avq::launch<float, 64>(__VA_ARGS__)                   \
+                                : avq::launch<float, 128>(__VA_ARGS__)))
+
+}  // namespace
+
+extern "C" {
+
+avq_status_t avq_prompt_attention_fwd(avq_dtype_t dtype, int32_t S, int32_t Tq, int32_t Tk,
+                                      int32_t Hq, int32_t Hkv, int32_t d, float scale,
+                                      int32_t causal, const void* Q, int64_t q_stride,
+                                      const void* K, int64_t k_stride, const void* V,
+                                      int64_t v_stride, const int32_t* cu_q, const int32_t* cu_k,
+                                      void* Y, float* lse, void* stream) {
+  const char* name = "avq_prompt_attention_fwd";
+  avq_status_t st = check_heads(name, dtype, S, Hq, Hkv, d);
+  if (st == AVQ_OK) st = check_stride(name, "q_stride", dtype, q_stride, Hq, d);
+  if (st == AVQ_OK) st = check_stride(name, "k_stride", dtype, k_stride, Hkv, d);
+  if (st == AVQ_OK) st = check_stride(name, "v_stride", dtype, v_stride, Hkv, d);
+  if (st == AVQ_OK) st = check_scale(name, scale);
+  if (st != AVQ_OK) return st;
+  if (Tq < 0 || Tk < 0)
+    return fail(AVQ_ERR_INVALID_ARG, "%s: Tq=%d and Tk=%d must not be negative", name, Tq, Tk);
+  if (Tq > (1 << 24) || Tk > (1 << 24))
+    return fail(AVQ_ERR_UNSUPPORTED, "%s: Tq=%d, Tk=%d: at most 2^24 tokens", name, Tq, Tk);
+  if (causal != 0 && causal != 1)
+    return fail(AVQ_ERR_INVALID_ARG, "%s: causal=%d: must be 0 or 1", name, causal);
+  if (!cu_q || !cu_k || (Tq > 0 && (!Q || !Y)) || (Tk > 0 && (!K || !V))) return null_pointer(name);
+  if (!aligned16(Q) || !aligned16(K) || !aligned16(V) || !aligned16(cu_q) || !aligned16(cu_k) ||
+      !aligned16(Y) || !aligned16(lse))
+    return misaligned(name);
+  if (Tq == 0) return ok();
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  return from_hip(AVQ_BY_TYPE(launch_prompt_attention, S, Tq, Tk, Hq, Hkv, scale, causal, Q,
+                              q_stride, K, k_stride, V, v_stride, cu_q, cu_k, Y, lse, s),
+                  "avq_prompt_attention_fwd launch");
+}
+
+int64_t avq_cache_page_bytes(avq_dtype_t dtype, avq_cache_t format, int32_t page_size, int32_t d) {
+  if ((dtype != AVQ_F32 && dtype != AVQ_BF16) || (d != 64 && d != 128)) return -1;
+  if (format != AVQ_CACHE_NATIVE && format != AVQ_CACHE_FP4) return -1;
+  if (page_size < 16 || page_size > 256 || (page_size & (page_size - 1)) != 0) return -1;
+  return (int64_t)avq::page_layout(format == AVQ_CACHE_FP4, dtype == AVQ_BF16 ? 2 : 4, page_size, d)
+      .bytes;
+}
+
+avq_status_t avq_cache_append(avq_dtype_t dtype, avq_cache_t format, int32_t S, int32_t T,
+                              int32_t Hq, int32_t Hkv, int32_t d, int32_t n_pages,
+                              int32_t page_size, int32_t max_pages, int32_t rot, int32_t n_pos,
+                              int32_t interleaved, const void* Q, int64_t q_stride, const void* K,
+                              int64_t k_stride, const void* V, int64_t v_stride,
+                              const int32_t* cu, const int32_t* start, const int32_t* block_table,
+                              const float* cos, const float* sin, void* cache, void* Q_out,
+                              void* K_out, void* stream) {
+  const char* name = "avq_cache_append";
+  avq_status_t st = check_heads(name, dtype, S, Q ? Hq : Hkv, Hkv, d);
+  if (st == AVQ_OK) st = check_cache(name, format, n_pages, page_size, max_pages);
+  if (st == AVQ_OK && Q) st = check_stride(name, "q_stride", dtype, q_stride, Hq, d);
+  if (st == AVQ_OK) st = check_stride(name, "k_stride", dtype, k_stride, Hkv, d);
+  if (st == AVQ_OK) st = check_stride(name, "v_stride", dtype, v_stride, Hkv, d);
+  if (st != AVQ_OK) return st;
+  if (T < 0) return fail(AVQ_ERR_INVALID_ARG, "%s: T=%d must not be negative", name, T);
+  if (T > (1 << 24)) return fail(AVQ_ERR_UNSUPPORTED, "%s: T=%d: at most 2^24 tokens", name, T);
+  if (!cu && T != S)
+    return fail(AVQ_ERR_INVALID_ARG, "%s: without cu, T=%d must be S=%d (one token each)", name, T, S);
+  if (rot < 0 || rot > d || rot % 16 != 0)
+    return fail(AVQ_ERR_INVALID_ARG, "%s: rot=%d must be a multiple of 16 in [0, d=%d]", name, rot, d);
+  if (rot > 0 && (!cos || !sin || n_pos < 1))
+    return fail(AVQ_ERR_INVALID_ARG, "%s: rot=%d needs cos, sin and n_pos >= 1", name, rot);
+  if (interleaved != 0 && interleaved != 1)
+    return fail(AVQ_ERR_INVALID_ARG, "%s: interleaved=%d: must be 0 or 1", name, interleaved);
+  if ((T > 0 && (!K || !V)) || !start || !block_table || !cache || (!Q != !Q_out))
+    return null_pointer(name);
+  if (!aligned16(Q) || !aligned16(K) || !aligned16(V) || !aligned16(cu) || !aligned16(start) ||
+      !aligned16(block_table) || !aligned16(cos) || !aligned16(sin) || !aligned16(cache) ||
+      !aligned16(Q_out) || !aligned16(K_out))
+    return misaligned(name);
+  if (T == 0) return ok();
+  const avq::CacheShape c{format == AVQ_CACHE_FP4, n_pages, page_size, max_pages, Hkv};
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  return from_hip(AVQ_BY_TYPE(launch_cache_append, c, S, T, Hq, rot, n_pos, interleaved, Q, q_stride,
+                              K, k_stride, V, v_stride, cu, start, block_table, cos, sin, cache,
+                              Q_out, K_out, s),
+                  "avq_cache_append launch");
+}
+
+avq_status_t avq_cache_gather(avq_dtype_t dtype, avq_cache_t format, int32_t S, int32_t T,
+                              int32_t Hkv, int32_t d, int32_t n_pages, int32_t page_size,
+                              int32_t max_pages, const void* cache, const int32_t* cu,
+                              const int32_t* start, const int32_t* block_table, void* K, void* V,
+                              void* stream) {
+  const char* name = "avq_cache_gather";
+  avq_status_t st = check_heads(name, dtype, S, Hkv, Hkv, d);
+  if (st == AVQ_OK) st = check_cache(name, format, n_pages, page_size, max_pages);
+  if (st != AVQ_OK) return st;
+  if (T < 0) return fail(AVQ_ERR_INVALID_ARG, "%s: T=%d must not be negative", name, T);
+  if (T > (1 << 24)) return fail(AVQ_ERR_UNSUPPORTED, "%s: T=%d: at most 2^24 tokens", name, T);
+  if (!cache || !cu || !start || !block_table || (T > 0 && (!K || !V))) return null_pointer(name);
+  if (!aligned16(cache) || !aligned16(cu) || !aligned16(start) || !aligned16(block_table) ||
+      !aligned16(K) || !aligned16(V))
+    return misaligned(name);
+  if (T == 0) return ok();
+  const avq::CacheShape c{format == AVQ_CACHE_FP4, n_pages, page_size, max_pages, Hkv};
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  return from_hip(AVQ_BY_TYPE(launch_cache_gather, c, S, T, cache, cu, start, block_table, K, V, s),
+                  "avq_cache_gather launch");
+}
+
+int64_t avq_cache_attention_workspace(int32_t S, int32_t n_q, int32_t Hq, int32_t Hkv, int32_t d) {
+  if (S < 1 || S > (1 << 20) || n_q < 1 || n_q > kMaxDrafts || Hq < 1 || Hkv < 1 ||
+      Hq > kMaxHeads || Hq % Hkv != 0 || (d != 64 && d != 128))
+    return -1;
+  return (int64_t)avq::cache_attention_workspace(S, n_q, Hq, Hkv, d);
+}
+
+avq_status_t avq_cache_attention_fwd(avq_dtype_t dtype, avq_cache_t format, int32_t S, int32_t n_q,
+                                     int32_t Hq, int32_t Hkv, int32_t d, int32_t n_pages,
+                                     int32_t page_size, int32_t max_pages, float scale,
+                                     const void* Q, int64_t q_stride, const void* cache,
+                                     const int32_t* lens, const int32_t* block_table, void* Y,
+                                     float* lse, void* workspace, int64_t workspace_bytes,
+                                     void* stream) {
+  const char* name = "avq_cache_attention_fwd";
+  avq_status_t st = check_heads(name, dtype, S, Hq, Hkv, d);
+  if (st == AVQ_OK) st = check_cache(name, format, n_pages, page_size, max_pages);
+  if (st == AVQ_OK) st = check_stride(name, "q_stride", dtype, q_stride, Hq, d);
+  if (st == AVQ_OK) st = check_scale(name, scale);
+  if (st != AVQ_OK) return st;
+  if (n_q < 1) return fail(AVQ_ERR_INVALID_ARG, "%s: n_q=%d must be positive", name, n_q);
+  if (n_q > kMaxDrafts)
+    return fail(AVQ_ERR_UNSUPPORTED, "%s: n_q=%d: at most %d tokens per sequence", name, n_q,
+                kMaxDrafts);
+  if (!Q || !cache || !lens || !block_table || !Y || !workspace) return null_pointer(name);
+  if (!aligned16(Q) || !aligned16(cache) || !aligned16(lens) || !aligned16(block_table) ||
+      !aligned16(Y) || !aligned16(lse) || !aligned16(workspace))
+    return misaligned(name);
+  const int64_t need = avq_cache_attention_workspace(S, n_q, Hq, Hkv, d);
+  if (workspace_bytes < need)
+    return fail(AVQ_ERR_INVALID_ARG, "%s: workspace of %lld bytes, %lld are needed", name,
+                (long long)workspace_bytes, (long long)need);
+  const avq::CacheShape c{format == AVQ_CACHE_FP4, n_pages, page_size, max_pages, Hkv};
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  return from_hip(AVQ_BY_TYPE(launch_cache_attention, c, S, n_q, Hq, scale, Q, q_stride, cache, lens,
+                              block_table, Y, lse, workspace, s),
+                  "avq_cache_attention_fwd launch");
 }
 
 }  // extern "C"

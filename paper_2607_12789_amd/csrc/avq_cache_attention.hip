@@ -1,0 +1,560 @@
+// Exact attention of the newest tokens over the paged cache (single tokens, or
+// a few drafted ones): softmax(scale Q K^T) V per sequence, grouped heads.
+//
+// Bound by the cache: every byte of it is read once and each key takes 4 d
+// flop per query row, so the rows of one key-value head (n_q tokens x Hq/Hkv
+// heads) are processed together, 16 to a tile. Everything is computed
+// transposed, keys x queries, with 16x16x32 bf16 (16x16x4 fp32) MFMA, from
+// registers: nothing is staged in LDS. A wave takes 32 keys per step. Row 4 g
+// + r of logit tile t is key 8 g + 4 t + r, so lane (g, c) ends up with the
+// logits of query c and the 8 keys of octet g: after exp2 they are the B
+// operand of the value product, whose A operand, the same octet at one
+// column, lies together in the page ([d][8]). The contraction over d may run
+// in any order: with a 4-bit cache lane g takes the contiguous quarter g of
+// a key's row (one 16-byte load at d = 128, and one scale), decoded by one
+// conversion per pair; a value byte (two columns of one key) is decoded with
+// its key's scale and the pairs are separated by byte permutes.
+//
+// Division of the work: lengths are known on the device only. A unit is 128
+// keys (one step of the workgroup's four waves) of one (row tile, head,
+// sequence); the units lie in one line, (row tile, head) slowest, then the
+// sequences, and each workgroup takes an equal run of it, whatever the
+// lengths. A run covers parts of one or more segments (a segment is all of
+// one (row tile, head, sequence)): a whole segment is normalised and stored,
+// a part leaves its running max, sum and numerator in the workspace, and a
+// second launch joins the parts. At most a run's first and last segment are
+// parts, so two slots per workgroup hold them.
+#include "avq_cache.hpp"
+#include "avq_launch.hpp"
+
+#include <type_traits>
+
+namespace avq {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / kWave;
+constexpr int kRows = 16;                  // query rows per tile
+constexpr int kStep = 32;                  // keys per wave and step
+constexpr int kUnit = kStep * kWaves;      // keys per unit
+constexpr int kMaxWorkgroups = 1024;       // four per CU
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kLazy = 8.f;         // log2 units the running max may lag behind
+constexpr float kMaxFloor = -1e30f;  // finite start of the running max
+
+struct CacheAttnArgs {
+  CacheArgs cache;
+  const void* Q;
+  int64_t q_stride;     // elements between tokens
+  const int32_t* lens;  // [S]
+  void* Y;
+  float* lse;           // nullable
+  float* parts;         // [workgroups][2][kRows][D + 2]: numerator, max, sum
+  int32_t* joins;       // [segments][2]: first workgroup and its slot, parts
+  int S, n_q, Hq, G, row_tiles;
+  float scale_log2;
+};
+
+// cached positions of sequence s that can be read
+__device__ __forceinline__ int length_of(const CacheAttnArgs& a, int s) {
+  const long long cap = (long long)a.cache.max_pages << a.cache.ps_log2;
+  const int n = max(a.lens[s], 0);
+  return (long long)n < cap ? n : (int)cap;
+}
+// every segment has a unit, so that empty ones are stored too
+__device__ __forceinline__ int units_of(int len) { return max(1, (len + kUnit - 1) / kUnit); }
+
+template <typename T, int D, bool FP4>
+struct Keys {
+  static constexpr bool kB = Elem<T>::kBf16;
+  static constexpr int H2 = D / 64;  // halves of 64 columns
+  // raw registers of one step: keys (two tiles), values, scales
+  static constexpr int KW = FP4 ? D / 32 : D * (int)sizeof(T) / 16;       // words per key tile
+  static constexpr int VW = FP4 ? 4 : 4 * 8 * (int)sizeof(T) / 4;         // words per 64 columns
+  uint32_t k[2][KW];
+  uint32_t v[H2][VW];
+  uint32_t ks[2];
+  uint32_t vs[H2][2];
+};
+
+template <int N>
+__device__ __forceinline__ void load_words(const unsigned char* p, uint32_t* w) {
+  if constexpr (N == 2) {
+    const uint2 v = *reinterpret_cast<const uint2*>(p);
+    w[0] = v.x, w[1] = v.y;
+  } else {
+    static_assert(N % 4 == 0, "16-byte loads");
+#pragma unroll
+    for (int i = 0; i < N; i += 4) {
+      const uint4 v = *reinterpret_cast<const uint4*>(p + 4 * i);
+      w[i] = v.x, w[i + 1] = v.y, w[i + 2] = v.z, w[i + 3] = v.w;
+    }
+  }
+}
+
+template <typename T, int D, bool FP4>
+__global__ __launch_bounds__(kThreads) void cache_attention_kernel(CacheAttnArgs a) {
+  constexpr bool kB = Elem<T>::kBf16;
+  using Raw = Keys<T, D, FP4>;
+  constexpr int H2 = D / 64;
+  constexpr int KQ = kB ? D / 32 : D / 4;  // k-steps of the logit product
+  using QFrag = typename std::conditional<kB, bf16x8, float>::type;
+
+  __shared__ int s_units[kThreads];      // units of the sequences before thread i's
+  __shared__ int s_wave[kWaves];
+  __shared__ float s_m[kWaves][kRows], s_l[kWaves][kRows];
+  __shared__ __attribute__((aligned(16))) float s_o[kWaves][kRows][D + 4];
+
+  const int tid = threadIdx.x, wave = tid / kWave, lane = tid % kWave;
+  const int g = lane / 16, c = lane % 16;
+  const int w = blockIdx.x;
+
+  // ---- units before each thread's run of sequences -------------------------
+  const int per = (a.S + kThreads - 1) / kThreads;
+  int mine = 0;
+  for (int i = 0; i < per; ++i) {
+    const int s = tid * per + i;
+    if (s < a.S) mine += units_of(length_of(a, s));
+  }
+  const int incl = wave_incl_scan(mine);
+  if (lane == kWave - 1) s_wave[wave] = incl;
+  __syncthreads();
+  int before = 0, total = 0;
+  for (int i = 0; i < kWaves; ++i) {
+    if (i < wave) before += s_wave[i];
+    total += s_wave[i];
+  }
+  s_units[tid] = before + incl - mine;
+  __syncthreads();
+
+  const int heads = a.cache.Hkv * a.row_tiles;
+  const long long U = (long long)total * heads;
+  const int W = (int)min((long long)gridDim.x, U);  // each takes a unit at least
+  if (w >= W) return;
+  long long u = U * w / W;
+  const long long u_end = U * (w + 1) / W;
+  const long long u_first = u;
+
+  // head and sequence of the run's first unit
+  int hr = (int)(u / total);
+  int x = (int)(u % total);
+  int t = 0;  // the last thread whose sequences start at or before x
+  for (int step = kThreads / 2; step > 0; step /= 2)
+    if (t + step < kThreads && s_units[t + step] <= x) t += step;
+  int s = t * per;
+  x -= s_units[t];
+  int len = length_of(a, s), n_units = units_of(len);
+  while (x >= n_units && s + 1 < a.S) {
+    x -= n_units;
+    ++s;
+    len = length_of(a, s);
+    n_units = units_of(len);
+  }
+
+  const PageLayout L = page_layout(FP4, sizeof(T), 1 << a.cache.ps_log2, D);
+  const int ps_mask = (1 << a.cache.ps_log2) - 1;
+  const int rows_all = a.n_q * a.G;
+
+  while (true) {
+    // ---- one segment: units [x, x_end) of sequence s, head hr ---------------
+    const int x_end = (int)min((long long)n_units, x + (u_end - u));
+    const int kvh = hr / a.row_tiles, row0 = hr % a.row_tiles * kRows;
+    const int row = row0 + c;                    // the lane's query
+    const bool has_row = row < rows_all;
+    const int qi = has_row ? row / a.G : 0;
+    const int hq = kvh * a.G + (has_row ? row % a.G : 0);
+    const int last = has_row ? len - a.n_q + qi + 1 : 0;  // keys the row sees
+    const int all_see = len - a.n_q + 1;                  // keys every row sees
+
+    QFrag q[KQ];
+    {
+      const T* qp = static_cast<const T*>(a.Q) + ((size_t)s * a.n_q + qi) * a.q_stride +
+                    (size_t)hq * D;
+#pragma unroll
+      for (int k = 0; k < KQ; ++k) {
+        if constexpr (kB) {
+          const int d0 = FP4 ? D / 4 * g + 8 * k : 32 * k + 8 * g;
+          q[k] = *reinterpret_cast<const bf16x8*>(qp + d0);
+        } else {
+          q[k] = qp[FP4 ? D / 4 * g + k : 16 * (k / 4) + 4 * g + k % 4];
+        }
+      }
+    }
+
+    float m = kMaxFloor, l = 0.f;
+    f32x4 o[H2][4];
+#pragma unroll
+    for (int h = 0; h < H2; ++h)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) o[h][k] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+    for (int y = x; y < x_end; ++y) {
+      const int key0 = y * kUnit + wave * kStep;
+      if (key0 >= len) break;
+      // ---- loads: the octet's page for values, the key rows' for keys -------
+      Raw raw;
+      const int vpos = key0 + 8 * g, kpos = key0 + 8 * (c / 4);
+      const unsigned char* vp = vpos < len ? page_of(a.cache, L.bytes, s, vpos, kvh) : nullptr;
+      const unsigned char* kp = kpos < len ? page_of(a.cache, L.bytes, s, kpos, kvh) : nullptr;
+      // without a page (past the end, or a bad entry) the lane reads page 0,
+      // which exists, and its keys take no part
+      const bool vok = vp != nullptr;
+      const unsigned char* none = a.cache.pool + (size_t)kvh * L.bytes;
+      if (!vp) vp = none;
+      if (!kp) kp = none;
+      const int oct = (vpos & ps_mask) / 8, slot0 = (kpos & ps_mask) + c % 4;
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt) {
+        const int slot = slot0 + 4 * tt;
+        if constexpr (FP4) {
+          load_words<Raw::KW>(kp + slot * (D / 2) + D / 8 * g, raw.k[tt]);
+          raw.ks[tt] = kp[L.ks + slot * (D / 32) + (D / 4 * g) / 32];
+        } else {
+          const unsigned char* rowp = kp + (size_t)slot * D * sizeof(T);
+#pragma unroll
+          for (int k = 0; k < Raw::KW / 4; ++k)  // 16-byte pieces g, g + 4, ...
+            load_words<4>(rowp + 64 * k + 16 * g, &raw.k[tt][4 * k]);
+        }
+      }
+#pragma unroll
+      for (int h = 0; h < H2; ++h) {
+        if constexpr (FP4) {
+          load_words<4>(vp + L.v + (oct * (D / 2) + 32 * h + 2 * c) * 8, raw.v[h]);
+          load_words<2>(vp + L.vs + (oct * (D / 32) + 2 * h + c / 8) * 8, raw.vs[h]);
+        } else {
+          load_words<Raw::VW>(vp + L.v + (size_t)(oct * D + 64 * h + 4 * c) * 8 * sizeof(T),
+                              raw.v[h]);
+        }
+      }
+
+      // ---- logits ----------------------------------------------------------
+      f32x4 sc[2];
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt) {
+        f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
+        if constexpr (FP4) {
+          const float scale = __uint_as_float(raw.ks[tt] << 23);
+#pragma unroll
+          for (int k = 0; k < D / 32; ++k) {  // a word holds 8 dimensions
+            const uint32_t wd = raw.k[tt][k];
+            if constexpr (kB) {
+              const bf16x2 p0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(wd, scale, 0);
+              const bf16x2 p1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(wd, scale, 1);
+              const bf16x2 p2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(wd, scale, 2);
+              const bf16x2 p3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(wd, scale, 3);
+              acc = mfma_bf16(bf16x8{p0[0], p0[1], p1[0], p1[1], p2[0], p2[1], p3[0], p3[1]},
+                              q[k], acc);
+            } else {
+              const auto p0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(wd, scale, 0);
+              const auto p1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(wd, scale, 1);
+              const auto p2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(wd, scale, 2);
+              const auto p3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(wd, scale, 3);
+              const float e[8] = {p0[0], p0[1], p1[0], p1[1], p2[0], p2[1], p3[0], p3[1]};
+#pragma unroll
+              for (int i = 0; i < 8; ++i) acc = mfma_f32(e[i], q[8 * k + i], acc);
+            }
+          }
+        } else {
+#pragma unroll
+          for (int k = 0; k < Raw::KW / 4; ++k) {
+            if constexpr (kB) {
+              acc = mfma_bf16(__builtin_bit_cast(bf16x8, *reinterpret_cast<uint4*>(&raw.k[tt][4 * k])),
+                              q[k], acc);
+            } else {
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                acc = mfma_f32(__uint_as_float(raw.k[tt][4 * k + i]), q[4 * k + i], acc);
+            }
+          }
+        }
+        sc[tt] = acc;
+      }
+
+      // ---- masks: only where a key of the step is not seen by every row ------
+      float p[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) p[i] = sc[i / 4][i % 4] * a.scale_log2;
+      const bool masked = key0 + kStep > all_see || __any(!vok);
+      if (masked) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (!vok || vpos + i >= last) p[i] = -INFINITY;
+      }
+
+      // ---- running max, weights ---------------------------------------------
+      float mx = fmaxf(fmaxf(fmaxf(p[0], p[1]), fmaxf(p[2], p[3])),
+                       fmaxf(fmaxf(p[4], p[5]), fmaxf(p[6], p[7])));
+      if (__any(mx > m + kLazy)) {
+        mx = max_xor<32>(max_xor<16>(mx));
+        const float mn = fmaxf(m, mx);
+        const float f = exp2_hw(m - mn);
+        m = mn;
+        l *= f;
+#pragma unroll
+        for (int h = 0; h < H2; ++h)
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) o[h][k][r] *= f;
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        p[i] = exp2_hw(p[i] - m);
+        l += p[i];
+      }
+
+      // ---- values ------------------------------------------------------------
+      // Masked keys have weight 0; what lies in their slots may be anything
+      // (never written, or not a page of this sequence), also infinities and
+      // NaN, and 0 times those is not 0: their values are cleared.
+      if (masked) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const bool ok = vok && vpos + i < len;
+          if constexpr (FP4) {
+            if (!ok)
+#pragma unroll
+              for (int h = 0; h < H2; ++h) raw.vs[h][i / 4] &= ~(0xffu << (8 * (i % 4)));
+          } else if constexpr (kB) {
+            if (!ok)
+#pragma unroll
+              for (int h = 0; h < H2; ++h)
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                  raw.v[h][4 * k + i / 2] &= i % 2 ? 0x0000ffffu : 0xffff0000u;
+          } else {
+            if (!ok)
+#pragma unroll
+              for (int h = 0; h < H2; ++h)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) raw.v[h][8 * k + i] = 0u;
+          }
+        }
+      }
+      if constexpr (kB) {
+        const bf16x8 pb = {(bf16)p[0], (bf16)p[1], (bf16)p[2], (bf16)p[3],
+                           (bf16)p[4], (bf16)p[5], (bf16)p[6], (bf16)p[7]};
+#pragma unroll
+        for (int h = 0; h < H2; ++h) {
+          if constexpr (FP4) {
+            float f[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              f[i] = __uint_as_float((raw.vs[h][i / 4] >> (8 * (i % 4)) & 0xffu) << 23);
+#pragma unroll
+            for (int pr = 0; pr < 2; ++pr) {  // pairs 2c, 2c + 1: columns 4c + 2 pr ..
+              bf16x2 e[8];
+#pragma unroll
+              for (int i = 0; i < 8; i += 4) {
+                const uint32_t wd = raw.v[h][2 * pr + i / 4];
+                e[i] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(wd, f[i], 0);
+                e[i + 1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(wd, f[i + 1], 1);
+                e[i + 2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(wd, f[i + 2], 2);
+                e[i + 3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(wd, f[i + 3], 3);
+              }
+#pragma unroll
+              for (int b = 0; b < 2; ++b)
+                o[h][2 * pr + b] =
+                    mfma_bf16(bf16x8{e[0][b], e[1][b], e[2][b], e[3][b], e[4][b], e[5][b],
+                                     e[6][b], e[7][b]},
+                              pb, o[h][2 * pr + b]);
+            }
+          } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              o[h][k] = mfma_bf16(
+                  __builtin_bit_cast(bf16x8, *reinterpret_cast<uint4*>(&raw.v[h][4 * k])), pb,
+                  o[h][k]);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int h = 0; h < H2; ++h) {
+          if constexpr (FP4) {
+            float f[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              f[i] = __uint_as_float((raw.vs[h][i / 4] >> (8 * (i % 4)) & 0xffu) << 23);
+#pragma unroll
+            for (int pr = 0; pr < 2; ++pr)
+#pragma unroll
+              for (int i = 0; i < 8; i += 4) {
+                const uint32_t wd = raw.v[h][2 * pr + i / 4];
+                const auto e0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(wd, f[i], 0);
+                const auto e1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(wd, f[i + 1], 1);
+                const auto e2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(wd, f[i + 2], 2);
+                const auto e3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(wd, f[i + 3], 3);
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                  f32x4 acc = o[h][2 * pr + b];
+                  acc = mfma_f32(e0[b], p[i], acc);
+                  acc = mfma_f32(e1[b], p[i + 1], acc);
+                  acc = mfma_f32(e2[b], p[i + 2], acc);
+                  acc = mfma_f32(e3[b], p[i + 3], acc);
+                  o[h][2 * pr + b] = acc;
+                }
+              }
+          } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+              for (int i = 0; i < 8; ++i)
+                o[h][k] = mfma_f32(__uint_as_float(raw.v[h][8 * k + i]), p[i], o[h][k]);
+          }
+        }
+      }
+    }
+
+    // ---- the four waves joined ------------------------------------------------
+    l = add_xor<32>(add_xor<16>(l));
+    if (g == 0) {
+      s_m[wave][c] = m;
+      s_l[wave][c] = l;
+    }
+    // row 4 g + r of value tile k of half h is column 64 h + 4 (4 g + r) + k
+#pragma unroll
+    for (int h = 0; h < H2; ++h)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        *reinterpret_cast<f32x4*>(&s_o[wave][c][64 * h + 16 * g + 4 * r]) =
+            f32x4{o[h][0][r], o[h][1][r], o[h][2][r], o[h][3][r]};
+    __syncthreads();
+    {
+      constexpr int C = D / 16;  // columns per thread
+      const int rr = tid / 16, d0 = tid % 16 * C;
+      float mm = s_m[0][rr];
+      for (int i = 1; i < kWaves; ++i) mm = fmaxf(mm, s_m[i][rr]);
+      float ll = 0.f, acc[C] = {};
+      for (int i = 0; i < kWaves; ++i) {
+        const float f = exp2_hw(s_m[i][rr] - mm);
+        ll = fmaf(f, s_l[i][rr], ll);
+#pragma unroll
+        for (int k = 0; k < C; ++k) acc[k] = fmaf(f, s_o[i][rr][d0 + k], acc[k]);
+      }
+      const long long seg = (long long)s * heads + hr;
+      const long long seg_u = u - x;  // unit where the segment starts
+      const int out_row = row0 + rr;
+      if (x == 0 && x_end == n_units) {
+        if (out_row < rows_all) {
+          const int oi = out_row / a.G, oh = kvh * a.G + out_row % a.G;
+          const size_t at = ((size_t)s * a.n_q + oi) * a.Hq + oh;
+          const float inv = ll > 0.f ? 1.f / ll : 0.f;
+          T* y = static_cast<T*>(a.Y) + at * D + d0;
+#pragma unroll
+          for (int k = 0; k < C; ++k) y[k] = (T)(acc[k] * inv);
+          if (a.lse && d0 == 0) a.lse[at] = ll > 0.f ? (mm + log2_hw(ll)) * kLn2 : -INFINITY;
+        }
+        if (tid == 0) a.joins[2 * seg + 1] = 1;
+      } else {
+        const int slot = u == u_first ? 0 : 1;
+        float* part = a.parts + ((size_t)(2 * w + slot) * kRows + rr) * (D + 2);
+#pragma unroll
+        for (int k = 0; k < C; ++k) part[d0 + k] = acc[k];
+        if (d0 == 0) {
+          part[D] = mm;
+          part[D + 1] = ll;
+        }
+        if (tid == 0 && x == 0) {
+          // the workgroup that holds unit v is ((v + 1) W - 1) / U
+          const long long w_last = ((seg_u + n_units) * W - 1) / U;
+          a.joins[2 * seg] = 2 * w + slot;
+          a.joins[2 * seg + 1] = (int)(w_last - w) + 1;
+        }
+      }
+    }
+    u += x_end - x;
+    if (u >= u_end) break;
+    __syncthreads();  // the exchange area is used again
+    x = 0;
+    if (++s == a.S) {
+      s = 0;
+      ++hr;
+    }
+    len = length_of(a, s);
+    n_units = units_of(len);
+  }
+}
+
+// Joins the parts of one segment: the first part is in the slot that joins
+// names, the others in slot 0 of the workgroups that follow.
+template <typename T, int D>
+__global__ __launch_bounds__(kThreads) void cache_join_kernel(CacheAttnArgs a) {
+  constexpr int C = D / 16;
+  const int seg = blockIdx.x;
+  const int n = a.joins[2 * seg + 1];
+  if (n == 1) return;
+  const int first = a.joins[2 * seg];
+  const int heads = a.cache.Hkv * a.row_tiles;
+  const int s = seg / heads, hr = seg % heads;
+  const int kvh = hr / a.row_tiles, row = hr % a.row_tiles * kRows + threadIdx.x / 16;
+  const int d0 = threadIdx.x % 16 * C;
+  if (row >= a.n_q * a.G) return;
+  float m = kMaxFloor, l = 0.f, acc[C] = {};
+  for (int i = 0; i < n; ++i) {
+    const int slot = i == 0 ? first : 2 * (first / 2 + i);
+    const float* part = a.parts + ((size_t)slot * kRows + threadIdx.x / 16) * (D + 2);
+    const float pm = part[D], mn = fmaxf(m, pm);
+    const float f = exp2_hw(m - mn), pf = exp2_hw(pm - mn);
+    m = mn;
+    l = l * f + part[D + 1] * pf;
+#pragma unroll
+    for (int k = 0; k < C; ++k) acc[k] = acc[k] * f + part[d0 + k] * pf;
+  }
+  const size_t at = ((size_t)s * a.n_q + row / a.G) * a.Hq + kvh * a.G + row % a.G;
+  const float inv = l > 0.f ? 1.f / l : 0.f;
+  T* y = static_cast<T*>(a.Y) + at * D + d0;
+#pragma unroll
+  for (int k = 0; k < C; ++k) y[k] = (T)(acc[k] * inv);
+  if (a.lse && d0 == 0) a.lse[at] = l > 0.f ? (m + log2_hw(l)) * kLn2 : -INFINITY;
+}
+
+int row_tiles_of(int n_q, int G) { return (n_q * G + kRows - 1) / kRows; }
+size_t parts_bytes(int D) { return (size_t)kMaxWorkgroups * 2 * kRows * (D + 2) * sizeof(float); }
+
+}  // namespace
+
+size_t cache_attention_workspace(int S, int n_q, int Hq, int Hkv, int d) {
+  const size_t segs = (size_t)S * Hkv * row_tiles_of(n_q, Hq / Hkv);
+  return parts_bytes(d) + segs * 2 * sizeof(int32_t);
+}
+
+template <typename T, int D>
+hipError_t launch_cache_attention(const CacheShape& c, int S, int n_q, int Hq, float scale,
+                                  const void* Q, int64_t q_stride, const void* cache,
+                                  const int32_t* lens, const int32_t* table, void* Y, float* lse,
+                                  void* workspace, hipStream_t stream) {
+  CacheAttnArgs a;
+  a.cache = {static_cast<unsigned char*>(const_cast<void*>(cache)), table, c.n_pages, c.max_pages,
+             31 - __builtin_clz((unsigned)c.page_size), c.Hkv};
+  a.Q = Q, a.q_stride = q_stride, a.lens = lens, a.Y = Y, a.lse = lse;
+  a.parts = static_cast<float*>(workspace);
+  a.joins = reinterpret_cast<int32_t*>(static_cast<unsigned char*>(workspace) + parts_bytes(D));
+  a.S = S, a.n_q = n_q, a.Hq = Hq, a.G = Hq / c.Hkv;
+  a.row_tiles = row_tiles_of(n_q, a.G);
+  a.scale_log2 = scale * kLog2e;
+  const long long segs = (long long)S * c.Hkv * a.row_tiles;
+  const long long cap = ((long long)c.max_pages * c.page_size + kUnit - 1) / kUnit;
+  const long long most = segs * (cap > 0 ? cap : 1);
+  const unsigned W = (unsigned)(most < kMaxWorkgroups ? most : kMaxWorkgroups);
+  if (c.fp4)
+    hipLaunchKernelGGL((cache_attention_kernel<T, D, true>), dim3(W), dim3(kThreads), 0, stream, a);
+  else
+    hipLaunchKernelGGL((cache_attention_kernel<T, D, false>), dim3(W), dim3(kThreads), 0, stream, a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || cap <= 1) return e;  // segments of one unit are never in parts
+  hipLaunchKernelGGL((cache_join_kernel<T, D>), dim3((unsigned)segs), dim3(kThreads), 0, stream, a);
+  return hipGetLastError();
+}
+
+#define AVQ_INSTANCE(T, D)                                                                         \
+  template hipError_t launch_cache_attention<T, D>(                                                \
+      const CacheShape&, int, int, int, float, const void*, int64_t, const void*, const int32_t*,  \
+      const int32_t*, void*, float*, void*, hipStream_t);
+AVQ_INSTANCE(bf16, 64)
+AVQ_INSTANCE(bf16, 128)
+AVQ_INSTANCE(float, 64)
+AVQ_INSTANCE(float, 128)
+#undef AVQ_INSTANCE
+
+}  // namespace avq
