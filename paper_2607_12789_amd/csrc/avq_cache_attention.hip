@@ -27,6 +27,7 @@
 #include "avq_cache.hpp"
 #include "avq_launch.hpp"
 
+#include <algorithm>
 #include <type_traits>
 
 namespace avq {
@@ -38,7 +39,8 @@ constexpr int kWaves = kThreads / kWave;
 constexpr int kRows = 16;                  // query rows per tile
 constexpr int kStep = 32;                  // keys per wave and step
 constexpr int kUnit = kStep * kWaves;      // keys per unit
-constexpr int kMaxWorkgroups = 1024;       // four per CU
+constexpr int kMaxWorkgroups = 1024;       // slots in the workspace
+constexpr int kPerCu = 4;                  // workgroups per CU, at most
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kLazy = 8.f;         // log2 units the running max may lag behind
 constexpr float kMaxFloor = -1e30f;  // finite start of the running max
@@ -50,7 +52,7 @@ struct CacheAttnArgs {
   const int32_t* lens;  // [S]
   void* Y;
   float* lse;           // nullable
-  float* parts;         // [workgroups][2][kRows][D + 2]: numerator, max, sum
+  float* parts;         // [workgroups][2] of part_floats(D): see there
   int32_t* joins;       // [segments][2]: first workgroup and its slot, parts
   int S, n_q, Hq, G, row_tiles;
   float scale_log2;
@@ -64,6 +66,9 @@ __device__ __forceinline__ int length_of(const CacheAttnArgs& a, int s) {
 }
 // every segment has a unit, so that empty ones are stored too
 __device__ __forceinline__ int units_of(int len) { return max(1, (len + kUnit - 1) / kUnit); }
+
+// A part: numerators [kRows][D], then maxima [kRows] and sums [kRows].
+__host__ __device__ constexpr size_t part_floats(int D) { return (size_t)kRows * (D + 2); }
 
 template <typename T, int D, bool FP4>
 struct Keys {
@@ -93,8 +98,12 @@ __device__ __forceinline__ void load_words(const unsigned char* p, uint32_t* w) 
   }
 }
 
+// Registers: four waves per SIMD (128 each) for the 4-bit cache, so that four
+// workgroups' loads are in flight per CU; the native cache's step is four
+// (fp32: eight) times as many bytes and takes two.
 template <typename T, int D, bool FP4>
-__global__ __launch_bounds__(kThreads) void cache_attention_kernel(CacheAttnArgs a) {
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(FP4 ? 4 : 2)))
+void cache_attention_kernel(CacheAttnArgs a) {
   constexpr bool kB = Elem<T>::kBf16;
   using Raw = Keys<T, D, FP4>;
   constexpr int H2 = D / 64;
@@ -189,20 +198,32 @@ __global__ __launch_bounds__(kThreads) void cache_attention_kernel(CacheAttnArgs
 #pragma unroll
       for (int k = 0; k < 4; ++k) o[h][k] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-    for (int y = x; y < x_end; ++y) {
+    // ---- loads: the octet's page for values, the key rows' for keys ---------
+    // Pages are looked up one step before their rows are requested, and rows
+    // one step before they are used. Without a page (past the end, or a bad
+    // entry) a lane reads page 0, which exists, and its keys take no part.
+    struct Place {
+      int vpage, kpage;  // -1: none
+    };
+    auto lookup = [&](int y) {
+      Place p{-1, -1};
       const int key0 = y * kUnit + wave * kStep;
-      if (key0 >= len) break;
-      // ---- loads: the octet's page for values, the key rows' for keys -------
-      Raw raw;
+      if (y >= x_end || key0 >= len) return p;  // wave-uniform
+      const int32_t* row = a.cache.table + (size_t)s * a.cache.max_pages;
       const int vpos = key0 + 8 * g, kpos = key0 + 8 * (c / 4);
-      const unsigned char* vp = vpos < len ? page_of(a.cache, L.bytes, s, vpos, kvh) : nullptr;
-      const unsigned char* kp = kpos < len ? page_of(a.cache, L.bytes, s, kpos, kvh) : nullptr;
-      // without a page (past the end, or a bad entry) the lane reads page 0,
-      // which exists, and its keys take no part
-      const bool vok = vp != nullptr;
-      const unsigned char* none = a.cache.pool + (size_t)kvh * L.bytes;
-      if (!vp) vp = none;
-      if (!kp) kp = none;
+      if (vpos < len) p.vpage = row[vpos >> a.cache.ps_log2];
+      if (kpos < len) p.kpage = row[kpos >> a.cache.ps_log2];
+      if ((unsigned)p.vpage >= (unsigned)a.cache.n_pages) p.vpage = -1;
+      if ((unsigned)p.kpage >= (unsigned)a.cache.n_pages) p.kpage = -1;
+      return p;
+    };
+    auto request = [&](int y, const Place& pl, Raw& raw) {
+      const int key0 = y * kUnit + wave * kStep;
+      const int vpos = key0 + 8 * g, kpos = key0 + 8 * (c / 4);
+      const unsigned char* vp =
+          a.cache.pool + ((size_t)max(pl.vpage, 0) * a.cache.Hkv + kvh) * L.bytes;
+      const unsigned char* kp =
+          a.cache.pool + ((size_t)max(pl.kpage, 0) * a.cache.Hkv + kvh) * L.bytes;
       const int oct = (vpos & ps_mask) / 8, slot0 = (kpos & ps_mask) + c % 4;
 #pragma unroll
       for (int tt = 0; tt < 2; ++tt) {
@@ -227,6 +248,20 @@ __global__ __launch_bounds__(kThreads) void cache_attention_kernel(CacheAttnArgs
                               raw.v[h]);
         }
       }
+    };
+
+    Raw next;
+    Place here = lookup(x), ahead = lookup(x + 1);
+    if (x * kUnit + wave * kStep < len) request(x, here, next);
+    for (int y = x; y < x_end; ++y) {
+      const int key0 = y * kUnit + wave * kStep;
+      if (key0 >= len) break;
+      Raw raw = next;
+      const bool vok = here.vpage >= 0;
+      const int vpos = key0 + 8 * g;
+      here = ahead;
+      if (y + 1 < x_end && key0 + kUnit < len) request(y + 1, ahead, next);
+      ahead = lookup(y + 2);
 
       // ---- logits ----------------------------------------------------------
       f32x4 sc[2];
@@ -448,12 +483,14 @@ __global__ __launch_bounds__(kThreads) void cache_attention_kernel(CacheAttnArgs
         if (tid == 0) a.joins[2 * seg + 1] = 1;
       } else {
         const int slot = u == u_first ? 0 : 1;
-        float* part = a.parts + ((size_t)(2 * w + slot) * kRows + rr) * (D + 2);
+        float* part = a.parts + (size_t)(2 * w + slot) * part_floats(D);
+        if (out_row < rows_all) {
 #pragma unroll
-        for (int k = 0; k < C; ++k) part[d0 + k] = acc[k];
-        if (d0 == 0) {
-          part[D] = mm;
-          part[D + 1] = ll;
+          for (int k = 0; k < C; ++k) part[rr * D + d0 + k] = acc[k];
+          if (d0 == 0) {
+            part[kRows * D + rr] = mm;
+            part[kRows * D + kRows + rr] = ll;
+          }
         }
         if (tid == 0 && x == 0) {
           // the workgroup that holds unit v is ((v + 1) W - 1) / U
@@ -476,41 +513,71 @@ __global__ __launch_bounds__(kThreads) void cache_attention_kernel(CacheAttnArgs
   }
 }
 
-// Joins the parts of one segment: the first part is in the slot that joins
-// names, the others in slot 0 of the workgroups that follow.
+// Joins the parts of one row of one segment: the first part is in the slot
+// that joins names, the others in slot 0 of the workgroups that follow. All
+// maxima are read first, so that the numerators are plain weighted sums, read
+// by all threads (4 columns each) without waiting for one another.
 template <typename T, int D>
 __global__ __launch_bounds__(kThreads) void cache_join_kernel(CacheAttnArgs a) {
-  constexpr int C = D / 16;
-  const int seg = blockIdx.x;
+  constexpr int TPP = D / 4;              // threads per part
+  constexpr int PG = kThreads / TPP;      // parts in flight
+  __shared__ float s_f[kMaxWorkgroups];   // weight of each part
+  __shared__ float s_red[2 * kWaves];
+  __shared__ __attribute__((aligned(16))) float s_acc[PG][D];
+  const int seg = blockIdx.x, rr = blockIdx.y;
   const int n = a.joins[2 * seg + 1];
   if (n == 1) return;
   const int first = a.joins[2 * seg];
   const int heads = a.cache.Hkv * a.row_tiles;
   const int s = seg / heads, hr = seg % heads;
-  const int kvh = hr / a.row_tiles, row = hr % a.row_tiles * kRows + threadIdx.x / 16;
-  const int d0 = threadIdx.x % 16 * C;
+  const int kvh = hr / a.row_tiles, row = hr % a.row_tiles * kRows + rr;
   if (row >= a.n_q * a.G) return;
-  float m = kMaxFloor, l = 0.f, acc[C] = {};
-  for (int i = 0; i < n; ++i) {
-    const int slot = i == 0 ? first : 2 * (first / 2 + i);
-    const float* part = a.parts + ((size_t)slot * kRows + threadIdx.x / 16) * (D + 2);
-    const float pm = part[D], mn = fmaxf(m, pm);
-    const float f = exp2_hw(m - mn), pf = exp2_hw(pm - mn);
-    m = mn;
-    l = l * f + part[D + 1] * pf;
-#pragma unroll
-    for (int k = 0; k < C; ++k) acc[k] = acc[k] * f + part[d0 + k] * pf;
+  const int tid = threadIdx.x, wave = tid / kWave, lane = tid % kWave;
+  auto part = [&](int i) {
+    return a.parts + (size_t)(i == 0 ? first : 2 * (first / 2 + i)) * part_floats(D);
+  };
+  float m = kMaxFloor;
+  for (int i = tid; i < n; i += kThreads) {
+    s_f[i] = part(i)[kRows * D + rr];
+    m = fmaxf(m, s_f[i]);
   }
+#pragma unroll
+  for (int k = 1; k < kWave; k *= 2) m = fmaxf(m, __shfl_xor(m, k, kWave));
+  if (lane == 0) s_red[wave] = m;
+  __syncthreads();
+  for (int i = 0; i < kWaves; ++i) m = fmaxf(m, s_red[i]);
+  float l = 0.f;
+  for (int i = tid; i < n; i += kThreads) {
+    const float f = exp2_hw(s_f[i] - m);
+    s_f[i] = f;
+    l = fmaf(f, part(i)[kRows * D + kRows + rr], l);
+  }
+#pragma unroll
+  for (int k = 1; k < kWave; k *= 2) l += __shfl_xor(l, k, kWave);
+  if (lane == 0) s_red[kWaves + wave] = l;
+  __syncthreads();
+  l = 0.f;
+  for (int i = 0; i < kWaves; ++i) l += s_red[kWaves + i];
+  const int pg = tid / TPP, d0 = tid % TPP * 4;
+  f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int i = pg; i < n; i += PG)
+    acc += s_f[i] * *reinterpret_cast<const f32x4*>(part(i) + rr * D + d0);
+  *reinterpret_cast<f32x4*>(&s_acc[pg][d0]) = acc;
+  __syncthreads();
   const size_t at = ((size_t)s * a.n_q + row / a.G) * a.Hq + kvh * a.G + row % a.G;
   const float inv = l > 0.f ? 1.f / l : 0.f;
-  T* y = static_cast<T*>(a.Y) + at * D + d0;
+  if (tid < D) {
+    float y = 0.f;
 #pragma unroll
-  for (int k = 0; k < C; ++k) y[k] = (T)(acc[k] * inv);
-  if (a.lse && d0 == 0) a.lse[at] = l > 0.f ? (m + log2_hw(l)) * kLn2 : -INFINITY;
+    for (int i = 0; i < PG; ++i) y += s_acc[i][tid];
+    static_cast<T*>(a.Y)[at * D + tid] = (T)(y * inv);
+  }
+  if (a.lse && tid == 0) a.lse[at] = l > 0.f ? (m + log2_hw(l)) * kLn2 : -INFINITY;
 }
 
 int row_tiles_of(int n_q, int G) { return (n_q * G + kRows - 1) / kRows; }
-size_t parts_bytes(int D) { return (size_t)kMaxWorkgroups * 2 * kRows * (D + 2) * sizeof(float); }
+size_t parts_bytes(int D) { return kMaxWorkgroups * 2 * part_floats(D) * sizeof(float); }
 
 }  // namespace
 
@@ -536,14 +603,22 @@ hipError_t launch_cache_attention(const CacheShape& c, int S, int n_q, int Hq, f
   const long long segs = (long long)S * c.Hkv * a.row_tiles;
   const long long cap = ((long long)c.max_pages * c.page_size + kUnit - 1) / kUnit;
   const long long most = segs * (cap > 0 ? cap : 1);
-  const unsigned W = (unsigned)(most < kMaxWorkgroups ? most : kMaxWorkgroups);
+  // as many workgroups as run at once: one more would start when the first
+  // ends, after as long again
+  DeviceInfo dev;
+  hipError_t e = device_info(&dev);
+  if (e != hipSuccess) return e;
+  const long long slots = std::min(kMaxWorkgroups, dev.cus * (c.fp4 ? kPerCu : kPerCu / 2));
+  const unsigned W = (unsigned)std::min(most, slots);
   if (c.fp4)
     hipLaunchKernelGGL((cache_attention_kernel<T, D, true>), dim3(W), dim3(kThreads), 0, stream, a);
   else
     hipLaunchKernelGGL((cache_attention_kernel<T, D, false>), dim3(W), dim3(kThreads), 0, stream, a);
-  hipError_t e = hipGetLastError();
+  e = hipGetLastError();
   if (e != hipSuccess || cap <= 1) return e;  // segments of one unit are never in parts
-  hipLaunchKernelGGL((cache_join_kernel<T, D>), dim3((unsigned)segs), dim3(kThreads), 0, stream, a);
+  hipLaunchKernelGGL((cache_join_kernel<T, D>),
+                     dim3((unsigned)segs, (unsigned)std::min(kRows, n_q * a.G)), dim3(kThreads), 0,
+                     stream, a);
   return hipGetLastError();
 }
 
