@@ -40,7 +40,6 @@ constexpr int kRows = 16;                  // query rows per tile
 constexpr int kStep = 32;                  // keys per wave and step
 constexpr int kUnit = kStep * kWaves;      // keys per unit
 constexpr int kMaxWorkgroups = 1024;       // slots in the workspace
-constexpr int kPerCu = 4;                  // workgroups per CU, at most
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kLazy = 8.f;         // log2 units the running max may lag behind
 constexpr float kMaxFloor = -1e30f;  // finite start of the running max
@@ -98,11 +97,17 @@ __device__ __forceinline__ void load_words(const unsigned char* p, uint32_t* w) 
   }
 }
 
-// Registers: four waves per SIMD (128 each) for the 4-bit cache, so that four
-// workgroups' loads are in flight per CU; the native cache's step is four
-// (fp32: eight) times as many bytes and takes two.
+// Workgroups per CU: three (168 registers a lane), whose loads are in flight
+// while others compute; two where a step's rows fill the registers (fp32, d =
+// 128, native). Four, where they fit (4 bits), are a little slower: 64
+// sequences of up to 16000 positions 136.8 us with three, 140.8 with four;
+// the bf16 native cache at d = 128 spills with four (20.2 and 36.1 us for 16
+// sequences of 4 tokens).
 template <typename T, int D, bool FP4>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(FP4 ? 4 : 2)))
+constexpr int kPerCu = !Elem<T>::kBf16 && D == 128 && !FP4 ? 2 : 3;
+
+template <typename T, int D, bool FP4>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kPerCu<T, D, FP4>)))
 void cache_attention_kernel(CacheAttnArgs a) {
   constexpr bool kB = Elem<T>::kBf16;
   using Raw = Keys<T, D, FP4>;
@@ -199,9 +204,10 @@ void cache_attention_kernel(CacheAttnArgs a) {
       for (int k = 0; k < 4; ++k) o[h][k] = f32x4{0.f, 0.f, 0.f, 0.f};
 
     // ---- loads: the octet's page for values, the key rows' for keys ---------
-    // Pages are looked up one step before their rows are requested, and rows
-    // one step before they are used. Without a page (past the end, or a bad
-    // entry) a lane reads page 0, which exists, and its keys take no part.
+    // Pages are looked up one step ahead; rows are not requested ahead (a
+    // second set of registers costs a workgroup per CU: 141 against 137 us for
+    // 64 sequences in 4 bits). Without a page (past the end, or a bad entry) a
+    // lane reads page 0, which exists, and its keys take no part.
     struct Place {
       int vpage, kpage;  // -1: none
     };
@@ -250,18 +256,15 @@ void cache_attention_kernel(CacheAttnArgs a) {
       }
     };
 
-    Raw next;
-    Place here = lookup(x), ahead = lookup(x + 1);
-    if (x * kUnit + wave * kStep < len) request(x, here, next);
+    Place ahead = lookup(x);
     for (int y = x; y < x_end; ++y) {
       const int key0 = y * kUnit + wave * kStep;
       if (key0 >= len) break;
-      Raw raw = next;
-      const bool vok = here.vpage >= 0;
+      Raw raw;
+      request(y, ahead, raw);
+      const bool vok = ahead.vpage >= 0;
       const int vpos = key0 + 8 * g;
-      here = ahead;
-      if (y + 1 < x_end && key0 + kUnit < len) request(y + 1, ahead, next);
-      ahead = lookup(y + 2);
+      ahead = lookup(y + 1);
 
       // ---- logits ----------------------------------------------------------
       f32x4 sc[2];
@@ -608,7 +611,8 @@ hipError_t launch_cache_attention(const CacheShape& c, int S, int n_q, int Hq, f
   DeviceInfo dev;
   hipError_t e = device_info(&dev);
   if (e != hipSuccess) return e;
-  const long long slots = std::min(kMaxWorkgroups, dev.cus * (c.fp4 ? kPerCu : kPerCu / 2));
+  const long long slots = std::min(
+      kMaxWorkgroups, dev.cus * (c.fp4 ? kPerCu<T, D, true> : kPerCu<T, D, false>));
   const unsigned W = (unsigned)std::min(most, slots);
   if (c.fp4)
     hipLaunchKernelGGL((cache_attention_kernel<T, D, true>), dim3(W), dim3(kThreads), 0, stream, a);
