@@ -389,6 +389,13 @@ avq_status_t avq_codebook_update(avq_dtype_t dtype, int32_t B, int32_t H, int32_
  * sequences as they are; the sequence's own are unspecified.
  */
 
+/* Bytes of the workspace of avq_prompt_attention_fwd for these sizes: 0 where
+ * it needs none (enough query tiles to fill the device), -1 for unsupported
+ * sizes. Its contents need not be set and mean nothing afterwards; calls that
+ * may run at the same time need one each. */
+int64_t avq_prompt_attention_workspace(avq_dtype_t dtype, int32_t S, int32_t Tq, int32_t Tk,
+                                       int32_t Hq, int32_t d);
+
 /*
  * avq_prompt_attention_fwd - exact softmax attention (Eq. (standardattention))
  * of packed sequences.
@@ -405,7 +412,8 @@ avq_status_t avq_codebook_update(avq_dtype_t dtype, int32_t B, int32_t H, int32_
  *   cu_q, cu_k  [S + 1] int32 (they may be one array)
  *   Y      [Tq][Hq][d] dtype, contiguous, out
  *   lse    [Tq][Hq] fp32, out, nullable
- * Arithmetic as avq_attention_fwd: bf16 products with fp32 accumulation and
+ *   workspace  avq_prompt_attention_workspace() bytes, NULL allowed for 0
+ * One launch, two with a workspace. Arithmetic as avq_attention_fwd: bf16 products with fp32 accumulation and
  * fp32 softmax state, weights rounded to bf16 for the value product; fp32
  * throughout for fp32.
  */
@@ -414,7 +422,8 @@ avq_status_t avq_prompt_attention_fwd(avq_dtype_t dtype, int32_t S, int32_t Tq, 
                                       int32_t causal, const void* Q, int64_t q_stride,
                                       const void* K, int64_t k_stride, const void* V,
                                       int64_t v_stride, const int32_t* cu_q, const int32_t* cu_k,
-                                      void* Y, float* lse, void* stream);
+                                      void* Y, float* lse, void* workspace,
+                                      int64_t workspace_bytes, void* stream);
 
 /* Element format of a paged cache: the calls' dtype, or 4 bits. */
 typedef int32_t avq_cache_t;

@@ -28,6 +28,7 @@ SYMBOLS = ("avq_version", "avq_last_error", "avq_packed_bytes", "avq_assign",
            "avq_aggregate", "avq_attention_fwd", "avq_attention_fwd_tiled",
            "avq_codebook_update", "avq_attention_fwd_ordered", "avq_gilbert_order",
            "avq_pack_aggregates", "avq_assign_aggregate", "avq_prompt_attention_fwd",
+           "avq_prompt_attention_workspace",
            "avq_cache_page_bytes", "avq_cache_append", "avq_cache_gather",
            "avq_cache_attention_workspace", "avq_cache_attention_fwd")
 IMPORTANCE_TILE = 64  # parents per codeword tile of attention_fwd(tiled_importance=True)
@@ -72,7 +73,9 @@ def lib():
                                            vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
         i64, ci, cf = ctypes.c_int64, ctypes.c_int, ctypes.c_float
         L.avq_prompt_attention_fwd.argtypes = [ci, i32, i32, i32, i32, i32, i32, cf, i32, vp, i64,
-                                               vp, i64, vp, i64, vp, vp, vp, vp, vp]
+                                               vp, i64, vp, i64, vp, vp, vp, vp, vp, i64, vp]
+        L.avq_prompt_attention_workspace.argtypes = [ci] + [i32] * 5
+        L.avq_prompt_attention_workspace.restype = i64
         L.avq_cache_page_bytes.argtypes = [ci, ci, i32, i32]
         L.avq_cache_page_bytes.restype = i64
         L.avq_cache_append.argtypes = [ci, ci] + [i32] * 11 + [vp, i64, vp, i64, vp, i64] + [vp] * 9
@@ -382,15 +385,26 @@ def _rows(t: torch.Tensor, name: str, H=None, d=None, dtype=None) -> int:
     return t.stride(0) if T > 1 else h * w
 
 
+def prompt_attention_workspace(dtype, S: int, Tq: int, Tk: int, Hq: int, d: int) -> int:
+    """Bytes of the workspace of ``prompt_attention_fwd`` (0: none needed)."""
+    if dtype not in _DTYPES:
+        raise ValueError(f"unsupported dtype {dtype}: use float32 or bfloat16")
+    n = lib().avq_prompt_attention_workspace(_DTYPES[dtype], S, Tq, Tk, Hq, d)
+    if n < 0:
+        raise ValueError(f"unsupported sizes S={S} Tq={Tq} Tk={Tk} Hq={Hq} d={d}")
+    return n
+
+
 def prompt_attention_fwd(Q, K, V, cu_q, cu_k, scale: float, causal: bool = True, Y=None,
-                         with_lse: bool = False, lse=None, stream=None):
+                         with_lse: bool = False, lse=None, workspace=None, stream=None):
     """Exact attention of packed sequences (``avq_prompt_attention_fwd``).
 
     Q [Tq, Hq, d], K and V [Tk, Hkv, d]: packed token rows (a token's heads
     contiguous; slices of a fused projection are taken as they are). cu_q,
     cu_k: int32 [S + 1] on the GPU. With ``causal`` the queries are the last
     ones of their sequence's keys. Rows behind the last sequence are left as
-    they were. Returns Y [Tq, Hq, d], or (Y, lse) with ``with_lse`` (lse: fp32
+    they were. workspace: a uint8 tensor of ``prompt_attention_workspace(...)``
+    bytes (allocated if needed and not given). Returns Y [Tq, Hq, d], or (Y, lse) with ``with_lse`` (lse: fp32
     [Tq, Hq]).
     """
     q_stride = _rows(Q, "Q")
@@ -412,11 +426,18 @@ def prompt_attention_fwd(Q, K, V, cu_q, cu_k, scale: float, causal: bool = True,
         lse = _empty(stream, (Tq, Hq), torch.float32, Q.device)
     if lse is not None:
         _dev(lse, "lse", torch.float32, (Tq, Hq))
-    _same_device(Q, K=K, V=V, cu_q=cu_q, cu_k=cu_k, Y=Y, lse=lse)
+    S = cu_q.shape[0] - 1
+    if workspace is None:
+        n = prompt_attention_workspace(Q.dtype, S, Tq, Tk, Hq, d)
+        if n:
+            workspace = _empty(stream, (n,), torch.uint8, Q.device)
+    if workspace is not None:
+        _dev(workspace, "workspace", torch.uint8)
+    _same_device(Q, K=K, V=V, cu_q=cu_q, cu_k=cu_k, Y=Y, lse=lse, workspace=workspace)
     _check(lib().avq_prompt_attention_fwd(
-        _dtype_code(Q), cu_q.shape[0] - 1, Tq, Tk, Hq, Hkv, d, float(scale), int(bool(causal)),
+        _dtype_code(Q), S, Tq, Tk, Hq, Hkv, d, float(scale), int(bool(causal)),
         _ptr(Q), q_stride, _ptr(K), k_stride, _ptr(V), v_stride, _ptr(cu_q), _ptr(cu_k), _ptr(Y),
-        _ptr(lse), s.cuda_stream))
+        _ptr(lse), _ptr(workspace), 0 if workspace is None else workspace.numel(), s.cuda_stream))
     return (Y, lse) if with_lse else Y
 
 

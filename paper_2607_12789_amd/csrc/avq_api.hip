@@ -388,12 +388,22 @@ avq_status_t null_pointer(const char* name) {
 
 extern "C" {
 
+int64_t avq_prompt_attention_workspace(avq_dtype_t dtype, int32_t S, int32_t Tq, int32_t Tk,
+                                       int32_t Hq, int32_t d) {
+  if ((dtype != AVQ_F32 && dtype != AVQ_BF16) || (d != 64 && d != 128) || S < 1 ||
+      S > (1 << 20) || Hq < 1 || Hq > kMaxHeads || Tq < 0 || Tk < 0 || Tq > (1 << 24) ||
+      Tk > (1 << 24))
+    return -1;
+  return (int64_t)AVQ_BY_TYPE(prompt_attention_workspace, S, Tq, Tk, Hq);
+}
+
 avq_status_t avq_prompt_attention_fwd(avq_dtype_t dtype, int32_t S, int32_t Tq, int32_t Tk,
                                       int32_t Hq, int32_t Hkv, int32_t d, float scale,
                                       int32_t causal, const void* Q, int64_t q_stride,
                                       const void* K, int64_t k_stride, const void* V,
                                       int64_t v_stride, const int32_t* cu_q, const int32_t* cu_k,
-                                      void* Y, float* lse, void* stream) {
+                                      void* Y, float* lse, void* workspace,
+                                      int64_t workspace_bytes, void* stream) {
   const char* name = "avq_prompt_attention_fwd";
   avq_status_t st = check_heads(name, dtype, S, Hq, Hkv, d);
   if (st == AVQ_OK) st = check_stride(name, "q_stride", dtype, q_stride, Hq, d);
@@ -409,12 +419,16 @@ avq_status_t avq_prompt_attention_fwd(avq_dtype_t dtype, int32_t S, int32_t Tq, 
     return fail(AVQ_ERR_INVALID_ARG, "%s: causal=%d: must be 0 or 1", name, causal);
   if (!cu_q || !cu_k || (Tq > 0 && (!Q || !Y)) || (Tk > 0 && (!K || !V))) return null_pointer(name);
   if (!aligned16(Q) || !aligned16(K) || !aligned16(V) || !aligned16(cu_q) || !aligned16(cu_k) ||
-      !aligned16(Y) || !aligned16(lse))
+      !aligned16(Y) || !aligned16(lse) || !aligned16(workspace))
     return misaligned(name);
+  const int64_t need = avq_prompt_attention_workspace(dtype, S, Tq, Tk, Hq, d);
+  if (need > 0 && (!workspace || workspace_bytes < need))
+    return fail(AVQ_ERR_INVALID_ARG, "%s: workspace of %lld bytes, %lld are needed", name,
+                workspace ? (long long)workspace_bytes : 0LL, (long long)need);
   if (Tq == 0) return ok();
   hipStream_t s = static_cast<hipStream_t>(stream);
   return from_hip(AVQ_BY_TYPE(launch_prompt_attention, S, Tq, Tk, Hq, Hkv, scale, causal, Q,
-                              q_stride, K, k_stride, V, v_stride, cu_q, cu_k, Y, lse, s),
+                              q_stride, K, k_stride, V, v_stride, cu_q, cu_k, Y, lse, workspace, s),
                   "avq_prompt_attention_fwd launch");
 }
 

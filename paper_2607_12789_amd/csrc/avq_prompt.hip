@@ -20,15 +20,20 @@
 //
 // Lengths are known on the device only, so the grid has Tq / 128 + S tiles per
 // head, at least as many as the sequences need, and each workgroup finds its
-// sequence; those left over exit.
+// sequence; those left over exit. Where the tiles are too few to fill the
+// device (a chunk behind a long prefix), several workgroups share a tile's
+// keys and a second launch joins their sums.
 #include "avq_cache.hpp"
 #include "avq_launch.hpp"
 
+#include <algorithm>
 #include <type_traits>
 
 namespace avq {
 
 namespace {
+
+constexpr int kMaxSplits = 16;
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
@@ -49,9 +54,57 @@ struct PromptArgs {
   void* Y;
   float* lse;  // nullable
   int S, Tq, Tk, Hq, G, causal;
-  int tiles;  // query tiles per head
+  int tiles;   // query tiles per head, at most
+  int splits;  // workgroups that share a tile's keys
   float scale_log2;
+  float* parts;  // with splits: see part_floats
 };
+
+// What one of a tile's workgroups leaves when its keys are shared: numerators
+// [BM][D], maxima [BM], sums [BM]; tile t of head h has parts (t Hq + h) splits
+// + z.
+__host__ __device__ constexpr size_t part_floats(int BM, int D) { return (size_t)BM * (D + 2); }
+
+// Sequence and query tile of work item i. Up to one sequence per lane: by
+// levels, the last tiles of the longest sequences first (under the causal mask
+// a tile's work grows with its index, and a long tile that starts last runs
+// alone): N(L) = sum over the sequences of max(0, tiles - L) tiles have level
+// L or more, and the items of level L are those from N(L + 1) to N(L). More
+// sequences: from the last tile back, found in the closed form cu / BM + s.
+// Returns false if there is no such item.
+__device__ __forceinline__ bool find_tile(const int32_t* cu, int S, int T, int BM, int tiles, int i,
+                                          int lane, int& s, int& lt) {
+  if (S <= kWave) {
+    int nt = 0;
+    if (lane < S) {
+      int a, b;
+      packed_range(cu, lane, T, a, b);
+      nt = (b - a + BM - 1) / BM;
+    }
+    auto from = [&](int L) { return last_lane(wave_incl_scan(max(nt - L, 0))); };
+    if (i >= from(0)) return false;
+    int lo = 0, hi = tiles;  // N(lo) > i >= N(hi)
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) / 2;
+      if (from(mid) > i) lo = mid; else hi = mid;
+    }
+    // the level's sequences in order: the one with i - N(lo + 1) before it
+    const int rank = i - from(lo + 1);
+    const unsigned long long in = __ballot(nt > lo);
+    const unsigned long long at = __ballot(nt > lo && bits_below(in) == rank);
+    s = (int)__builtin_ctzll(at);
+    lt = lo;
+    return true;
+  }
+  const int tile = tiles - 1 - i;
+  s = find_sequence(S, tile, lane, [&](int k) {
+    return (long long)min(max(cu[k], 0), T) / BM + k;
+  });
+  int a, b;
+  packed_range(cu, s, T, a, b);
+  lt = tile - (a / BM + s);
+  return lt >= 0 && (long long)lt * BM < b - a;
+}
 
 template <typename T, int D>
 struct PromptCfg {
@@ -106,23 +159,19 @@ void prompt_kernel(PromptArgs a) {
   const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int h = lane / 32, c = lane % 32;
 
-  // later tiles of a sequence see more keys under the causal mask: first
-  const int tile = a.tiles - 1 - blockIdx.x / a.Hq;
+  const int item = blockIdx.x / a.Hq;
   int hq = blockIdx.x % a.Hq;
   // workgroup i runs on XCD i % 8: each XCD takes consecutive heads, which
   // share keys, of every tile
   if (a.Hq % 8 == 0) hq = hq % 8 * (a.Hq / 8) + hq / 8;
   const int hkv = hq / a.G;
 
-  const int s = find_sequence(a.S, tile, lane, [&](int i) {
-    return (long long)min(max(a.cu_q[i], 0), a.Tq) / BM + i;
-  });
+  int s, lt;
+  if (!find_tile(a.cu_q, a.S, a.Tq, BM, a.tiles, item, lane, s, lt)) return;
   int qa, qb, ka, kb;
   packed_range(a.cu_q, s, a.Tq, qa, qb);
   packed_range(a.cu_k, s, a.Tk, ka, kb);
   const int Lq = qb - qa, Lk = kb - ka;
-  const int lt = tile - (qa / BM + s);
-  if (lt < 0 || lt * BM >= Lq) return;
   const int off = Lk - Lq;  // key of query 0 on the diagonal
   const int row0 = lt * BM + 32 * wave;
   const int row = row0 + c;
@@ -132,7 +181,10 @@ void prompt_kernel(PromptArgs a) {
   const int wave_see = row0 >= Lq ? 0 : a.causal ? min(Lk, min(row0 + 31, Lq - 1) + off + 1) : Lk;
   const int wave_all = a.causal ? min(Lk, row0 + off + 1) : Lk;  // seen by all its rows
   const int tile_see = a.causal ? min(Lk, min(lt * BM + BM, Lq) + off) : Lk;
-  const int n_tiles = tile_see > 0 ? (tile_see + BN - 1) / BN : 0;
+  const int all_tiles = tile_see > 0 ? (tile_see + BN - 1) / BN : 0;
+  // key tiles of this workgroup's share
+  const int t_begin = (int)((long long)all_tiles * blockIdx.y / a.splits);
+  const int n_tiles = (int)((long long)all_tiles * (blockIdx.y + 1) / a.splits);
 
   // ---- query operand ---------------------------------------------------------
   Frag q[KQ];
@@ -185,8 +237,8 @@ void prompt_kernel(PromptArgs a) {
 #pragma unroll
   for (int i = 0; i < DT; ++i) o[i] = f32x16{};
 
-  if (n_tiles > 0) issue(0, 0);
-  for (int t = 0; t < n_tiles; ++t) {
+  if (t_begin < n_tiles) issue(t_begin, t_begin & 1);
+  for (int t = t_begin; t < n_tiles; ++t) {
     const int b = t & 1;
     __builtin_amdgcn_s_waitcnt(0);
     __syncthreads();  // tile t has landed, tile t - 1 is read
@@ -287,8 +339,25 @@ void prompt_kernel(PromptArgs a) {
     }
   }
 
-  // ---- Y = O / l -----------------------------------------------------------------------
   l = add_xor<32>(l);
+  if (a.splits > 1) {  // a part: nothing but the sum 0 for a row that saw no key
+    float* part = a.parts + (((size_t)item * a.Hq + hq) * a.splits + blockIdx.y) * part_floats(BM, D);
+    const int r0 = 32 * wave + c;
+    if (h == 0) {
+      part[BM * D + r0] = m;
+      part[BM * D + BM + r0] = l;
+    }
+    if (has_row && l > 0.f) {
+#pragma unroll
+      for (int i = 0; i < DT; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4)
+          *reinterpret_cast<f32x4*>(part + r0 * D + 32 * i + 2 * r + 4 * h) =
+              f32x4{o[i][r], o[i][r + 1], o[i][r + 2], o[i][r + 3]};
+    }
+    return;
+  }
+  // ---- Y = O / l -----------------------------------------------------------------------
   const float inv = l > 0.f ? 1.f / l : 0.f;
   if (!has_row) return;
   const size_t at = (size_t)(qa + row) * a.Hq + hq;
@@ -309,20 +378,96 @@ void prompt_kernel(PromptArgs a) {
   if (a.lse && h == 0) a.lse[at] = l > 0.f ? (m + log2_hw(l)) * kLn2 : -INFINITY;
 }
 
+// Joins the parts of a tile's rows: D / 4 threads per row, 4 columns each.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a) {
+  constexpr int BM = PromptCfg<T, D>::BM;
+  constexpr int TPR = D / 4, RPW = 256 / TPR;  // threads per row, rows per workgroup
+  constexpr float kLn2 = 0.6931471805599453f;
+  const int item = blockIdx.x / a.Hq, hq = blockIdx.x % a.Hq;
+  int s, lt, qa, qb;
+  if (!find_tile(a.cu_q, a.S, a.Tq, BM, a.tiles, item, threadIdx.x % kWave, s, lt)) return;
+  packed_range(a.cu_q, s, a.Tq, qa, qb);
+  const int r = blockIdx.y * RPW + threadIdx.x / TPR, d0 = threadIdx.x % TPR * 4;
+  const int row = lt * BM + r;
+  if (row >= qb - qa) return;
+  const size_t step = part_floats(BM, D);
+  const float* part = a.parts + ((size_t)item * a.Hq + hq) * a.splits * step;
+  float m = -1e30f, ms[kMaxSplits], ls[kMaxSplits];
+#pragma unroll
+  for (int z = 0; z < kMaxSplits; ++z) {
+    ls[z] = 0.f;
+    if (z < a.splits) {
+      ms[z] = part[z * step + BM * D + r];
+      ls[z] = part[z * step + BM * D + BM + r];
+    }
+  }
+#pragma unroll
+  for (int z = 0; z < kMaxSplits; ++z)
+    if (ls[z] > 0.f) m = fmaxf(m, ms[z]);
+  float l = 0.f;
+  f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int z = 0; z < kMaxSplits; ++z)
+    if (ls[z] > 0.f) {
+      const float f = exp2_hw(ms[z] - m);
+      l = fmaf(f, ls[z], l);
+      acc += f * *reinterpret_cast<const f32x4*>(part + z * step + r * D + d0);
+    }
+  const float inv = l > 0.f ? 1.f / l : 0.f;
+  const size_t at = (size_t)(qa + row) * a.Hq + hq;
+  T* y = static_cast<T*>(a.Y) + at * D + d0;
+  if constexpr (Elem<T>::kBf16)
+    *reinterpret_cast<bf16x4*>(y) = bf16x4{(bf16)(acc[0] * inv), (bf16)(acc[1] * inv),
+                                           (bf16)(acc[2] * inv), (bf16)(acc[3] * inv)};
+  else
+    *reinterpret_cast<f32x4*>(y) = acc * inv;
+  if (a.lse && d0 == 0) a.lse[at] = l > 0.f ? (m + log2_hw(l)) * kLn2 : -INFINITY;
+}
+
+long long tiles_of(long long Tq, int S, int BM) { return Tq / BM + S; }
+
+// Workgroups per tile: its keys are shared where the tiles leave more than
+// half of the device's workgroup slots (two per CU) idle, and the sequences'
+// mean length leaves each enough keys to pay for the joining launch.
+template <typename T, int D>
+int splits_of(int S, int Tq, int Tk, int Hq) {
+  using Cfg = PromptCfg<T, D>;
+  constexpr int kSlots = 512;
+  const long long n = tiles_of(Tq, S, Cfg::BM) * Hq;
+  const long long room = kSlots / n, keys = Tk / S / (4 * Cfg::BN);
+  return (int)std::max(1LL, std::min({room, keys, (long long)kMaxSplits}));
+}
+
 }  // namespace
+
+template <typename T, int D>
+size_t prompt_attention_workspace(int S, int Tq, int Tk, int Hq) {
+  using Cfg = PromptCfg<T, D>;
+  const int splits = splits_of<T, D>(S, Tq, Tk, Hq);
+  if (splits == 1) return 0;
+  return (size_t)tiles_of(Tq, S, Cfg::BM) * Hq * splits * part_floats(Cfg::BM, D) * sizeof(float);
+}
 
 template <typename T, int D>
 hipError_t launch_prompt_attention(int S, int Tq, int Tk, int Hq, int Hkv, float scale, int causal,
                                    const void* Q, int64_t q_stride, const void* K,
                                    int64_t k_stride, const void* V, int64_t v_stride,
                                    const int32_t* cu_q, const int32_t* cu_k, void* Y, float* lse,
-                                   hipStream_t stream) {
+                                   void* workspace, hipStream_t stream) {
   using Cfg = PromptCfg<T, D>;
-  const long long tiles = (long long)Tq / Cfg::BM + S;
+  const long long tiles = tiles_of(Tq, S, Cfg::BM);
+  const int splits = splits_of<T, D>(S, Tq, Tk, Hq);
   if (tiles * Hq > 0x7fffffff) return hipErrorInvalidConfiguration;
   PromptArgs a{Q, K, V, q_stride, k_stride, v_stride, cu_q, cu_k, Y, lse,
-               S, Tq, Tk, Hq, Hq / Hkv, causal, (int)tiles, scale * kLog2e};
-  hipLaunchKernelGGL((prompt_kernel<T, D>), dim3((unsigned)(tiles * Hq)), dim3(64 * Cfg::NW), 0,
+               S, Tq, Tk, Hq, Hq / Hkv, causal, (int)tiles, splits, scale * kLog2e,
+               static_cast<float*>(workspace)};
+  const unsigned grid = (unsigned)(tiles * Hq);
+  hipLaunchKernelGGL((prompt_kernel<T, D>), dim3(grid, (unsigned)splits), dim3(64 * Cfg::NW), 0,
+                     stream, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || splits == 1) return e;
+  hipLaunchKernelGGL((prompt_join_kernel<T, D>), dim3(grid, Cfg::BM * D / 4 / 256), dim3(256), 0,
                      stream, a);
   return hipGetLastError();
 }
@@ -330,7 +475,8 @@ hipError_t launch_prompt_attention(int S, int Tq, int Tk, int Hq, int Hkv, float
 #define AVQ_INSTANCE(T, D)                                                                        \
   template hipError_t launch_prompt_attention<T, D>(                                              \
       int, int, int, int, int, float, int, const void*, int64_t, const void*, int64_t, const void*, \
-      int64_t, const int32_t*, const int32_t*, void*, float*, hipStream_t);
+      int64_t, const int32_t*, const int32_t*, void*, float*, void*, hipStream_t);                \
+  template size_t prompt_attention_workspace<T, D>(int, int, int, int);
 AVQ_INSTANCE(bf16, 64)
 AVQ_INSTANCE(bf16, 128)
 AVQ_INSTANCE(float, 64)

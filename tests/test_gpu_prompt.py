@@ -145,6 +145,29 @@ def test_one_long_sequence():
         check_attention(Y[at, h], lse[at, h], Q[at, h], K[:, 0], V[:, 0], 1 / math.sqrt(d), at + 1)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("d,Hq,causal", [(64, 2, True), (128, 7, False), (128, 1, True)])
+@pytest.mark.parametrize("lens_q,lens_k", [([5], [3000]), ([130, 1], [2000, 2600]),
+                                           ([300, 4], [290, 3])])
+def test_few_queries_many_keys(lens_q, lens_k, d, Hq, causal, dtype):
+    """Tiles whose keys several workgroups share (rows without keys among them)."""
+    scale = 1 / math.sqrt(d)
+    n = avq.prompt_attention_workspace(dtype, len(lens_q), sum(lens_q), sum(lens_k), Hq, d)
+    assert n > 0 or lens_k[-1] == 3
+    Q, K, V = make(lens_q, lens_k, Hq, 1, d, dtype, 7)
+    Y, lse = run(Q, K, V, lens_q, lens_k, scale, causal)
+    check_prompt(Y, lse, Q, K, V, lens_q, lens_k, scale, causal)
+
+
+@pytest.mark.parametrize("S", [63, 64, 65, 300])
+def test_many_sequences(S):
+    """One sequence per lane and more: both orders of the tiles."""
+    lens = [1 + 37 * s % 300 if s % 3 else 0 for s in range(S)]
+    Q, K, V = make(lens, lens, 1, 1, 64, BF16, 12)
+    Y, lse = run(Q, K, V, lens, lens, 0.2, True)
+    check_prompt(Y, lse, Q, K, V, lens, lens, 0.2, True)
+
+
 def test_offsets_past_32_bits():
     """Token rows 2^22 elements apart: 700 of them span 5.9 GB."""
     n, stride = 700, 1 << 22

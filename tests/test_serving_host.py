@@ -19,9 +19,9 @@ def L():
 
 
 def prompt(L, dtype=BF16, S=2, Tq=8, Tk=8, Hq=4, Hkv=2, d=64, scale=1.0, causal=1, qs=256, ks=128,
-           vs=128, Q=FAKE, K=FAKE, V=FAKE, cu_q=FAKE, cu_k=FAKE, Y=FAKE, lse=None):
+           vs=128, Q=FAKE, K=FAKE, V=FAKE, cu_q=FAKE, cu_k=FAKE, Y=FAKE, lse=None, ws=None, ws_bytes=0):
     return L.avq_prompt_attention_fwd(dtype, S, Tq, Tk, Hq, Hkv, d, scale, causal, Q, qs, K, ks, V,
-                                      vs, cu_q, cu_k, Y, lse, None)
+                                      vs, cu_q, cu_k, Y, lse, ws, ws_bytes, None)
 
 
 def append(L, dtype=BF16, fmt=1, S=2, T=8, Hq=4, Hkv=2, d=64, n_pages=4, ps=16, max_pages=2, rot=0,
@@ -62,7 +62,9 @@ CASES = {
         (dict(Q=None), INVALID), (dict(K=None), INVALID), (dict(V=None), INVALID),
         (dict(cu_q=None), INVALID), (dict(cu_k=None), INVALID), (dict(Y=None), INVALID),
         (dict(Q=ODD), INVALID), (dict(V=ODD), INVALID), (dict(lse=ODD), INVALID),
-        (dict(cu_k=ODD), INVALID), (dict(Tq=0, Q=None, Y=None), OK)],
+        (dict(cu_k=ODD), INVALID), (dict(ws=ODD), INVALID),
+        (dict(Tk=1 << 20), INVALID), (dict(Tk=1 << 20, ws=FAKE, ws_bytes=1000), INVALID),
+        (dict(Tq=0, Q=None, Y=None), OK)],
     append: HEADS + CACHE + [
         (dict(T=-1), INVALID), (dict(T=(1 << 24) + 1), UNSUPPORTED), (dict(cu=None), INVALID),
         (dict(rot=8), INVALID), (dict(rot=80), INVALID), (dict(rot=-16), INVALID),
@@ -111,6 +113,11 @@ def test_page_bytes(L):
 
 
 def test_workspace_bytes(L):
+    assert avq.prompt_attention_workspace(torch.bfloat16, 4, 1 << 16, 1 << 16, 16, 128) == 0
+    assert avq.prompt_attention_workspace(torch.bfloat16, 1, 300, 1 << 16, 4, 128) > 0
+    for bad in ((9, 1, 8, 8, 4, 64), (BF16, 0, 8, 8, 4, 64), (BF16, 1, -1, 8, 4, 64),
+                (BF16, 1, 8, 8, 4, 96)):
+        assert L.avq_prompt_attention_workspace(*bad) == -1
     small = avq.cache_attention_workspace(1, 1, 8, 8, 64)
     assert 0 < small < avq.cache_attention_workspace(4096, 16, 32, 8, 64)
     for bad in ((0, 1, 8, 8, 64), (1, 17, 8, 8, 64), (1, 1, 8, 3, 64), (1, 1, 8, 8, 80)):
