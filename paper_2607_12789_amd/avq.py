@@ -344,14 +344,15 @@ def gilbert_order(width: int, height: int):
 # ---- exact attention of packed prompts, and the paged cache ------------------
 
 
-def _launch_stream(stream, device: torch.device):
-    """The stream a call runs on, which must be one of the tensors' device: the
-    library launches on the current device."""
-    s = torch.cuda.current_stream() if stream is None else stream
-    if s.device != device or torch.cuda.current_device() != device.index:
-        raise ValueError(f"tensors on {device}: the current device is "
-                         f"cuda:{torch.cuda.current_device()}, the stream's {s.device}")
-    return s
+def _launch_stream(stream, device: torch.device) -> int:
+    """The handle of the stream a call runs on, which must be one of the
+    tensors' device: the library launches on the current device."""
+    current = torch.cuda.current_device()
+    if device.index != current or (stream is not None and stream.device != device):
+        raise ValueError(f"tensors on {device}: the current device is cuda:{current}"
+                         + (f", the stream's {stream.device}" if stream is not None else ""))
+    # the current stream's handle without a Stream object: 0.1 us instead of 2.6
+    return torch._C._cuda_getCurrentRawStream(current) if stream is None else stream.cuda_stream
 
 
 def _same_device(ref: torch.Tensor, **tensors) -> None:
@@ -437,7 +438,7 @@ def prompt_attention_fwd(Q, K, V, cu_q, cu_k, scale: float, causal: bool = True,
     _check(lib().avq_prompt_attention_fwd(
         _dtype_code(Q), S, Tq, Tk, Hq, Hkv, d, float(scale), int(bool(causal)),
         _ptr(Q), q_stride, _ptr(K), k_stride, _ptr(V), v_stride, _ptr(cu_q), _ptr(cu_k), _ptr(Y),
-        _ptr(lse), _ptr(workspace), 0 if workspace is None else workspace.numel(), s.cuda_stream))
+        _ptr(lse), _ptr(workspace), 0 if workspace is None else workspace.numel(), s))
     return (Y, lse) if with_lse else Y
 
 
@@ -531,7 +532,7 @@ def cache_append(K, V, cache, block_table, start, page_size: int, cu=None, Q=Non
         _dtype_code(K), int(bool(fp4)), S, T, Hq, Hkv, d, n_pages, page_size, max_pages, rot, n_pos,
         int(bool(interleaved)), _ptr(Q), q_stride, _ptr(K), k_stride, _ptr(V), v_stride, _ptr(cu),
         _ptr(start), _ptr(block_table), _ptr(cos), _ptr(sin), _ptr(cache), _ptr(Q_out),
-        _ptr(K_out), s.cuda_stream))
+        _ptr(K_out), s))
     return Q_out, K_out
 
 
@@ -552,7 +553,7 @@ def cache_gather(cache, block_table, start, cu, T: int, page_size: int, dtype, d
     _same_device(cache, block_table=block_table, start=start, cu=cu, K=K, V=V)
     _check(lib().avq_cache_gather(
         _DTYPES[dtype], int(bool(fp4)), S, T, Hkv, d, n_pages, page_size, max_pages, _ptr(cache),
-        _ptr(cu), _ptr(start), _ptr(block_table), _ptr(K), _ptr(V), s.cuda_stream))
+        _ptr(cu), _ptr(start), _ptr(block_table), _ptr(K), _ptr(V), s))
     return K, V
 
 
@@ -604,5 +605,5 @@ def cache_attention_fwd(Q, cache, block_table, lens, page_size: int, scale: floa
     _check(lib().avq_cache_attention_fwd(
         _dtype_code(Q), int(bool(fp4)), S, n_q, Hq, Hkv, d, n_pages, page_size, max_pages,
         float(scale), _ptr(Q), q_stride, _ptr(cache), _ptr(lens), _ptr(block_table), _ptr(Y),
-        _ptr(lse), _ptr(workspace), workspace.numel(), s.cuda_stream))
+        _ptr(lse), _ptr(workspace), workspace.numel(), s))
     return (Y, lse) if with_lse else Y

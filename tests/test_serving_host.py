@@ -144,14 +144,13 @@ def test_binding_refuses_another_device(monkeypatch):
     dev = torch.device("cuda", 1)
     stream = SimpleNamespace(device=dev, cuda_stream=0)
     monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
-    monkeypatch.setattr(torch.cuda, "current_stream",
-                        lambda *a: SimpleNamespace(device=torch.device("cuda", 0), cuda_stream=0))
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda i: 77, raising=False)
     for s in (None, stream):
         with pytest.raises(ValueError):
             avq._launch_stream(s, dev)
     with pytest.raises(ValueError):
         avq._launch_stream(stream, torch.device("cuda", 0))
-    assert avq._launch_stream(None, torch.device("cuda", 0)).cuda_stream == 0
+    assert avq._launch_stream(None, torch.device("cuda", 0)) == 77
     a, b = SimpleNamespace(device=dev), SimpleNamespace(device=torch.device("cuda", 0))
     with pytest.raises(ValueError):
         avq._same_device(a, other=b)
