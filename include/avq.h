@@ -526,7 +526,7 @@ int64_t avq_cache_attention_workspace(int32_t S, int32_t n_q, int32_t Hq, int32_
  *   cache, block_table  as above; lens [S] int32
  *   Y            [S][n_q][Hq][d] dtype, out;  lse [S][n_q][Hq] fp32, nullable
  *   workspace    avq_cache_attention_workspace() bytes
- * Two launches (one where no sequence can hold more than 128 positions). What
+ * Two launches (one where no sequence can hold more than 512 positions). What
  * lies in cache slots behind a sequence's length has no effect, whatever it is.
  */
 avq_status_t avq_cache_attention_fwd(avq_dtype_t dtype, avq_cache_t format, int32_t S, int32_t n_q,

@@ -17,7 +17,8 @@
 //
 // Division of the work: lengths are known on the device only. A unit is 128
 // keys (one step of the workgroup's four waves) of one (row tile, head,
-// sequence); the units lie in one line, (row tile, head) slowest, then the
+// sequence), or all of its keys where the cache has room for 512 at most;
+// the units lie in one line, (row tile, head) slowest, then the
 // sequences, and each workgroup takes an equal run of it, whatever the
 // lengths. A run covers parts of one or more segments (a segment is all of
 // one (row tile, head, sequence)): a whole segment is normalised and stored,
@@ -38,7 +39,8 @@ constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
 constexpr int kRows = 16;                  // query rows per tile
 constexpr int kStep = 32;                  // keys per wave and step
-constexpr int kUnit = kStep * kWaves;      // keys per unit
+constexpr int kUnit = kStep * kWaves;      // keys per step of a workgroup
+constexpr int kWholeSteps = 4;             // steps of sequences that are not divided
 constexpr int kMaxWorkgroups = 1024;       // slots in the workspace
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kLazy = 8.f;         // log2 units the running max may lag behind
@@ -54,6 +56,7 @@ struct CacheAttnArgs {
   float* parts;         // [workgroups][2] of part_floats(D): see there
   int32_t* joins;       // [segments][2]: first workgroup and its slot, parts
   int S, n_q, Hq, G, row_tiles;
+  int unit;  // keys per unit, a multiple of kUnit
   float scale_log2;
 };
 
@@ -64,7 +67,9 @@ __device__ __forceinline__ int length_of(const CacheAttnArgs& a, int s) {
   return (long long)n < cap ? n : (int)cap;
 }
 // every segment has a unit, so that empty ones are stored too
-__device__ __forceinline__ int units_of(int len) { return max(1, (len + kUnit - 1) / kUnit); }
+__device__ __forceinline__ int units_of(int len, int unit) {
+  return max(1, (len + unit - 1) / unit);
+}
 
 // A part: numerators [kRows][D], then maxima [kRows] and sums [kRows].
 __host__ __device__ constexpr size_t part_floats(int D) { return (size_t)kRows * (D + 2); }
@@ -129,7 +134,7 @@ void cache_attention_kernel(CacheAttnArgs a) {
   int mine = 0;
   for (int i = 0; i < per; ++i) {
     const int s = tid * per + i;
-    if (s < a.S) mine += units_of(length_of(a, s));
+    if (s < a.S) mine += units_of(length_of(a, s), a.unit);
   }
   const int incl = wave_incl_scan(mine);
   if (lane == kWave - 1) s_wave[wave] = incl;
@@ -158,12 +163,12 @@ void cache_attention_kernel(CacheAttnArgs a) {
     if (t + step < kThreads && s_units[t + step] <= x) t += step;
   int s = t * per;
   x -= s_units[t];
-  int len = length_of(a, s), n_units = units_of(len);
+  int len = length_of(a, s), n_units = units_of(len, a.unit);
   while (x >= n_units && s + 1 < a.S) {
     x -= n_units;
     ++s;
     len = length_of(a, s);
-    n_units = units_of(len);
+    n_units = units_of(len, a.unit);
   }
 
   const PageLayout L = page_layout(FP4, sizeof(T), 1 << a.cache.ps_log2, D);
@@ -173,6 +178,7 @@ void cache_attention_kernel(CacheAttnArgs a) {
   while (true) {
     // ---- one segment: units [x, x_end) of sequence s, head hr ---------------
     const int x_end = (int)min((long long)n_units, x + (u_end - u));
+    const int steps = a.unit / kUnit, y_end = x_end * steps;  // steps of kUnit keys
     const int kvh = hr / a.row_tiles, row0 = hr % a.row_tiles * kRows;
     const int row = row0 + c;                    // the lane's query
     const bool has_row = row < rows_all;
@@ -214,7 +220,7 @@ void cache_attention_kernel(CacheAttnArgs a) {
     auto lookup = [&](int y) {
       Place p{-1, -1};
       const int key0 = y * kUnit + wave * kStep;
-      if (y >= x_end || key0 >= len) return p;  // wave-uniform
+      if (y >= y_end || key0 >= len) return p;  // wave-uniform
       const int32_t* row = a.cache.table + (size_t)s * a.cache.max_pages;
       const int vpos = key0 + 8 * g, kpos = key0 + 8 * (c / 4);
       if (vpos < len) p.vpage = row[vpos >> a.cache.ps_log2];
@@ -256,8 +262,8 @@ void cache_attention_kernel(CacheAttnArgs a) {
       }
     };
 
-    Place ahead = lookup(x);
-    for (int y = x; y < x_end; ++y) {
+    Place ahead = lookup(x * steps);
+    for (int y = x * steps; y < y_end; ++y) {
       const int key0 = y * kUnit + wave * kStep;
       if (key0 >= len) break;
       Raw raw;
@@ -512,7 +518,7 @@ void cache_attention_kernel(CacheAttnArgs a) {
       ++hr;
     }
     len = length_of(a, s);
-    n_units = units_of(len);
+    n_units = units_of(len, a.unit);
   }
 }
 
@@ -604,8 +610,12 @@ hipError_t launch_cache_attention(const CacheShape& c, int S, int n_q, int Hq, f
   a.row_tiles = row_tiles_of(n_q, a.G);
   a.scale_log2 = scale * kLog2e;
   const long long segs = (long long)S * c.Hkv * a.row_tiles;
-  const long long cap = ((long long)c.max_pages * c.page_size + kUnit - 1) / kUnit;
-  const long long most = segs * (cap > 0 ? cap : 1);
+  // Short sequences are not divided: four steps take less than the joining
+  // launch that dividing them needs.
+  const long long room = ((long long)c.max_pages * c.page_size + kUnit - 1) / kUnit;
+  a.unit = kUnit * (room <= kWholeSteps ? (int)room : 1);
+  const long long cap = room <= kWholeSteps ? 1 : room;  // units of a segment, at most
+  const long long most = segs * cap;
   // as many workgroups as run at once: one more would start when the first
   // ends, after as long again
   DeviceInfo dev;
@@ -619,7 +629,7 @@ hipError_t launch_cache_attention(const CacheShape& c, int S, int n_q, int Hq, f
   else
     hipLaunchKernelGGL((cache_attention_kernel<T, D, false>), dim3(W), dim3(kThreads), 0, stream, a);
   e = hipGetLastError();
-  if (e != hipSuccess || cap <= 1) return e;  // segments of one unit are never in parts
+  if (e != hipSuccess || cap == 1) return e;  // segments of one unit are never in parts
   hipLaunchKernelGGL((cache_join_kernel<T, D>),
                      dim3((unsigned)segs, (unsigned)std::min(kRows, n_q * a.G)), dim3(kThreads), 0,
                      stream, a);
