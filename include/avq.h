@@ -394,7 +394,7 @@ avq_status_t avq_codebook_update(avq_dtype_t dtype, int32_t B, int32_t H, int32_
  * sizes. Its contents need not be set and mean nothing afterwards; calls that
  * may run at the same time need one each. */
 int64_t avq_prompt_attention_workspace(avq_dtype_t dtype, int32_t S, int32_t Tq, int32_t Tk,
-                                       int32_t Hq, int32_t d);
+                                       int32_t Hq, int32_t d, int32_t causal);
 
 /*
  * avq_prompt_attention_fwd - exact softmax attention (Eq. (standardattention))

@@ -74,7 +74,7 @@ def lib():
         i64, ci, cf = ctypes.c_int64, ctypes.c_int, ctypes.c_float
         L.avq_prompt_attention_fwd.argtypes = [ci, i32, i32, i32, i32, i32, i32, cf, i32, vp, i64,
                                                vp, i64, vp, i64, vp, vp, vp, vp, vp, i64, vp]
-        L.avq_prompt_attention_workspace.argtypes = [ci] + [i32] * 5
+        L.avq_prompt_attention_workspace.argtypes = [ci] + [i32] * 6
         L.avq_prompt_attention_workspace.restype = i64
         L.avq_cache_page_bytes.argtypes = [ci, ci, i32, i32]
         L.avq_cache_page_bytes.restype = i64
@@ -386,11 +386,12 @@ def _rows(t: torch.Tensor, name: str, H=None, d=None, dtype=None) -> int:
     return t.stride(0) if T > 1 else h * w
 
 
-def prompt_attention_workspace(dtype, S: int, Tq: int, Tk: int, Hq: int, d: int) -> int:
+def prompt_attention_workspace(dtype, S: int, Tq: int, Tk: int, Hq: int, d: int,
+                               causal: bool = True) -> int:
     """Bytes of the workspace of ``prompt_attention_fwd`` (0: none needed)."""
     if dtype not in _DTYPES:
         raise ValueError(f"unsupported dtype {dtype}: use float32 or bfloat16")
-    n = lib().avq_prompt_attention_workspace(_DTYPES[dtype], S, Tq, Tk, Hq, d)
+    n = lib().avq_prompt_attention_workspace(_DTYPES[dtype], S, Tq, Tk, Hq, d, int(bool(causal)))
     if n < 0:
         raise ValueError(f"unsupported sizes S={S} Tq={Tq} Tk={Tk} Hq={Hq} d={d}")
     return n
@@ -429,7 +430,7 @@ def prompt_attention_fwd(Q, K, V, cu_q, cu_k, scale: float, causal: bool = True,
         _dev(lse, "lse", torch.float32, (Tq, Hq))
     S = cu_q.shape[0] - 1
     if workspace is None:
-        n = prompt_attention_workspace(Q.dtype, S, Tq, Tk, Hq, d)
+        n = prompt_attention_workspace(Q.dtype, S, Tq, Tk, Hq, d, causal)
         if n:
             workspace = _empty(stream, (n,), torch.uint8, Q.device)
     if workspace is not None:

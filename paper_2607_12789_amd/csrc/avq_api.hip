@@ -389,12 +389,12 @@ avq_status_t null_pointer(const char* name) {
 extern "C" {
 
 int64_t avq_prompt_attention_workspace(avq_dtype_t dtype, int32_t S, int32_t Tq, int32_t Tk,
-                                       int32_t Hq, int32_t d) {
+                                       int32_t Hq, int32_t d, int32_t causal) {
   if ((dtype != AVQ_F32 && dtype != AVQ_BF16) || (d != 64 && d != 128) || S < 1 ||
       S > (1 << 20) || Hq < 1 || Hq > kMaxHeads || Tq < 0 || Tk < 0 || Tq > (1 << 24) ||
-      Tk > (1 << 24))
+      Tk > (1 << 24) || (causal != 0 && causal != 1))
     return -1;
-  return (int64_t)AVQ_BY_TYPE(prompt_attention_workspace, S, Tq, Tk, Hq);
+  return (int64_t)AVQ_BY_TYPE(prompt_attention_workspace, S, Tq, Tk, Hq, causal);
 }
 
 avq_status_t avq_prompt_attention_fwd(avq_dtype_t dtype, int32_t S, int32_t Tq, int32_t Tk,
@@ -421,7 +421,7 @@ avq_status_t avq_prompt_attention_fwd(avq_dtype_t dtype, int32_t S, int32_t Tq, 
   if (!aligned16(Q) || !aligned16(K) || !aligned16(V) || !aligned16(cu_q) || !aligned16(cu_k) ||
       !aligned16(Y) || !aligned16(lse) || !aligned16(workspace))
     return misaligned(name);
-  const int64_t need = avq_prompt_attention_workspace(dtype, S, Tq, Tk, Hq, d);
+  const int64_t need = avq_prompt_attention_workspace(dtype, S, Tq, Tk, Hq, d, causal);
   if (need > 0 && (!workspace || workspace_bytes < need))
     return fail(AVQ_ERR_INVALID_ARG, "%s: workspace of %lld bytes, %lld are needed", name,
                 workspace ? (long long)workspace_bytes : 0LL, (long long)need);

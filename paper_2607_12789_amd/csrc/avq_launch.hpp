@@ -46,7 +46,7 @@ hipError_t launch_prompt_attention(int S, int Tq, int Tk, int Hq, int Hkv, float
                                    const int32_t* cu_q, const int32_t* cu_k, void* Y, float* lse,
                                    void* workspace, hipStream_t stream);
 template <typename T, int D>
-size_t prompt_attention_workspace(int S, int Tq, int Tk, int Hq);
+size_t prompt_attention_workspace(int S, int Tq, int Tk, int Hq, int causal);
 template <typename T, int D>
 hipError_t launch_cache_append(const CacheShape& c, int S, int T_, int Hq, int rot, int n_pos,
                                int interleaved, const void* Q, int64_t q_stride, const void* K,

@@ -18,11 +18,9 @@
 // transpose read (bf16: 4 keys of 16 columns per 16 lanes; fp32 needs one key
 // per lane and no transpose).
 //
-// Lengths are known on the device only, so the grid has Tq / 128 + S tiles per
-// head, at least as many as the sequences need, and each workgroup finds its
-// sequence; those left over exit. Where the tiles are too few to fill the
-// device (a chunk behind a long prefix), several workgroups share a tile's
-// keys and a second launch joins their sums.
+// Lengths are known on the device only: the grid has Tq / 128 + S tiles per
+// head, at least as many as the sequences need, each workgroup finds its tile
+// and those left over exit; or the tiles' keys are dealt out in equal runs.
 #include "avq_cache.hpp"
 #include "avq_launch.hpp"
 
@@ -33,7 +31,10 @@ namespace avq {
 
 namespace {
 
-constexpr int kMaxSplits = 16;
+constexpr int kLeast = 4;  // key tiles of a run, at least
+constexpr float kLazy = 8.f;         // log2 units the running max may lag behind
+constexpr float kMaxFloor = -1e30f;  // finite start of the running max
+constexpr float kLn2 = 0.6931471805599453f;
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
@@ -54,57 +55,12 @@ struct PromptArgs {
   void* Y;
   float* lse;  // nullable
   int S, Tq, Tk, Hq, G, causal;
-  int tiles;   // query tiles per head, at most
-  int splits;  // workgroups that share a tile's keys
+  int tiles;  // query tiles per head, at most
   float scale_log2;
-  float* parts;  // with splits: see part_floats
+  // equal runs: see part_floats and Runs
+  float* parts;
+  int32_t* joins;  // [tiles][Hq][2]: first part, number of parts
 };
-
-// What one of a tile's workgroups leaves when its keys are shared: numerators
-// [BM][D], maxima [BM], sums [BM]; tile t of head h has parts (t Hq + h) splits
-// + z.
-__host__ __device__ constexpr size_t part_floats(int BM, int D) { return (size_t)BM * (D + 2); }
-
-// Sequence and query tile of work item i. Up to one sequence per lane: by
-// levels, the last tiles of the longest sequences first (under the causal mask
-// a tile's work grows with its index, and a long tile that starts last runs
-// alone): N(L) = sum over the sequences of max(0, tiles - L) tiles have level
-// L or more, and the items of level L are those from N(L + 1) to N(L). More
-// sequences: from the last tile back, found in the closed form cu / BM + s.
-// Returns false if there is no such item.
-__device__ __forceinline__ bool find_tile(const int32_t* cu, int S, int T, int BM, int tiles, int i,
-                                          int lane, int& s, int& lt) {
-  if (S <= kWave) {
-    int nt = 0;
-    if (lane < S) {
-      int a, b;
-      packed_range(cu, lane, T, a, b);
-      nt = (b - a + BM - 1) / BM;
-    }
-    auto from = [&](int L) { return last_lane(wave_incl_scan(max(nt - L, 0))); };
-    if (i >= from(0)) return false;
-    int lo = 0, hi = tiles;  // N(lo) > i >= N(hi)
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) / 2;
-      if (from(mid) > i) lo = mid; else hi = mid;
-    }
-    // the level's sequences in order: the one with i - N(lo + 1) before it
-    const int rank = i - from(lo + 1);
-    const unsigned long long in = __ballot(nt > lo);
-    const unsigned long long at = __ballot(nt > lo && bits_below(in) == rank);
-    s = (int)__builtin_ctzll(at);
-    lt = lo;
-    return true;
-  }
-  const int tile = tiles - 1 - i;
-  s = find_sequence(S, tile, lane, [&](int k) {
-    return (long long)min(max(cu[k], 0), T) / BM + k;
-  });
-  int a, b;
-  packed_range(cu, s, T, a, b);
-  lt = tile - (a / BM + s);
-  return lt >= 0 && (long long)lt * BM < b - a;
-}
 
 template <typename T, int D>
 struct PromptCfg {
@@ -120,8 +76,102 @@ struct PromptCfg {
   static constexpr int COPIES = TILE / 1024;   // wave copies per tile
   static constexpr int CPW = COPIES / NW;
   static constexpr int RPC = 64 / U;           // rows per wave copy
-  static constexpr int LDS_BYTES = 4 * TILE;   // K and V, two buffers
   static_assert(COPIES % NW == 0, "copies split evenly over the waves");
+};
+
+// ---- division of the work --------------------------------------------------------
+// Whole tiles (one workgroup each) where there are enough of them; otherwise
+// equal runs: the key tiles of all query tiles, in the order head, sequence,
+// query tile, key tile, are cut into as many equal runs as workgroups run at
+// once. A run covers parts of one or more query tiles: a whole one is stored, a
+// part leaves its numerators, maxima and sums, and a second launch joins the
+// parts. At most a run's first and last tile are parts.
+
+// A part: numerators [BM][D], maxima [BM], sums [BM]; run i has parts 2 i and
+// 2 i + 1.
+__host__ __device__ constexpr size_t part_floats(int BM, int D) { return (size_t)BM * (D + 2); }
+
+struct Tile {
+  int s, lt;           // sequence, tile of its queries
+  int qa, ka, Lq, Lk;  // its rows
+  __device__ __forceinline__ void rows_of(const PromptArgs& a) {
+    int b;
+    packed_range(a.cu_q, s, a.Tq, qa, b);
+    Lq = b - qa;
+    packed_range(a.cu_k, s, a.Tk, ka, b);
+    Lk = b - ka;
+  }
+};
+
+// Key tiles that query tile lt reads.
+template <int BM, int BN>
+__device__ __forceinline__ int key_tiles(int lt, int Lq, int Lk, int causal) {
+  const int keys = causal ? max(0, min(Lk, min((lt + 1) * BM, Lq) + Lk - Lq)) : Lk;
+  return (keys + BN - 1) / BN;
+}
+
+// Whole tiles: tile of work item i, false if there is none. Up to one sequence
+// per lane: by levels, the last tiles of the longest sequences first (under
+// the causal mask a tile's work grows with its index, and a long tile that
+// starts last runs alone): N(L) = sum over the sequences of max(0, tiles - L)
+// tiles have level L or more, and the items of level L are those from N(L + 1)
+// to N(L). More sequences: from the last tile back, found in the closed form
+// cu / BM + s.
+template <int BM>
+__device__ __forceinline__ bool find_tile(const PromptArgs& a, int i, int lane, Tile& t) {
+  if (a.S <= kWave) {
+    int nt = 0;
+    if (lane < a.S) {
+      int b, e;
+      packed_range(a.cu_q, lane, a.Tq, b, e);
+      nt = (e - b + BM - 1) / BM;
+    }
+    auto from = [&](int L) { return last_lane(wave_incl_scan(max(nt - L, 0))); };
+    if (i >= from(0)) return false;
+    int lo = 0, hi = a.tiles;  // N(lo) > i >= N(hi)
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) / 2;
+      if (from(mid) > i) lo = mid; else hi = mid;
+    }
+    // the level's sequences in order: the one with i - N(lo + 1) before it
+    const int rank = i - from(lo + 1);
+    const unsigned long long in = __ballot(nt > lo);
+    const unsigned long long at = __ballot(nt > lo && bits_below(in) == rank);
+    t.s = (int)__builtin_ctzll(at);
+    t.lt = lo;
+    t.rows_of(a);
+    return true;
+  }
+  const int tile = a.tiles - 1 - i;
+  t.s = find_sequence(a.S, tile, lane, [&](int k) {
+    return (long long)min(max(a.cu_q[k], 0), a.Tq) / BM + k;
+  });
+  t.rows_of(a);
+  t.lt = tile - (t.qa / BM + t.s);
+  return t.lt >= 0 && (long long)t.lt * BM < t.Lq;
+}
+
+// Equal runs. A unit is a key tile of a query tile; a query tile that reads
+// none has one unit too, so that its rows are stored.
+template <int BM, int BN>
+struct Runs {
+  // Units of the tiles 0 .. n - 1 of a sequence: tile L reads the keys up to
+  // BM (L + 1) + off (causal), so Q (L + 1) + o key tiles, but the last tile,
+  // and every one without a mask, all.
+  static __device__ __forceinline__ int before(int n, int Lq, int Lk, int causal) {
+    constexpr int Q = BM / BN;
+    const int nt = (Lq + BM - 1) / BM, all = max(1, (Lk + BN - 1) / BN);
+    if (!causal) return n * all;
+    const int off = Lk - Lq, o = off >= 0 ? (off + BN - 1) / BN : -(-off / BN);  // ceil(off / BN)
+    const int m = min(n, nt - 1);
+    // tiles below one have no key: Q (L + 1) + o < 1
+    const int one = min(m, o >= 1 - Q ? 0 : (Q - o) / Q - 1);
+    const int sum = one + Q * ((m * (m + 1) - one * (one + 1)) / 2) + o * (m - one);
+    return n < nt || nt == 0 ? sum : sum + all;
+  }
+  static __device__ __forceinline__ int total(int Lq, int Lk, int causal) {
+    return Lq > 0 ? before((Lq + BM - 1) / BM, Lq, Lk, causal) : 0;
+  }
 };
 
 // Positions of the 16-byte units of a staged row. Keys: 32 rows read one unit
@@ -142,49 +192,30 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc(const void* p) {
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), (short)0, 0x7fffffff, 0x00020000);
 }
 
+// The key tiles t_begin .. t_end - 1 of one query tile and head; part: where a
+// part goes, null for a whole tile.
 template <typename T, int D>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2)))
-void prompt_kernel(PromptArgs a) {
+__device__ __forceinline__ void attend(const PromptArgs& a, const Tile& tile, int hq, int t_begin,
+                                       int t_end, float* part, unsigned char* lds, int wave,
+                                       int lane) {
   using Cfg = PromptCfg<T, D>;
   constexpr bool kB = Cfg::kB;
   constexpr int BM = Cfg::BM, BN = Cfg::BN, KT = Cfg::KT, DT = Cfg::DT, U = Cfg::U,
                 ESZ = Cfg::ESZ, CPW = Cfg::CPW, RPC = Cfg::RPC, TILE = Cfg::TILE;
   constexpr int KQ = kB ? D / 16 : D / 2;
   using Frag = typename std::conditional<kB, bf16x8, float>::type;
-  constexpr float kLazy = 8.f, kMaxFloor = -1e30f, kLn2 = 0.6931471805599453f;
-
-  __shared__ __attribute__((aligned(16))) unsigned char lds[Cfg::LDS_BYTES];  // K0 K1 V0 V1
-
-  const int tid = threadIdx.x, lane = tid % kWave;
-  const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int h = lane / 32, c = lane % 32;
-
-  const int item = blockIdx.x / a.Hq;
-  int hq = blockIdx.x % a.Hq;
-  // workgroup i runs on XCD i % 8: each XCD takes consecutive heads, which
-  // share keys, of every tile
-  if (a.Hq % 8 == 0) hq = hq % 8 * (a.Hq / 8) + hq / 8;
+  const int qa = tile.qa, ka = tile.ka, Lq = tile.Lq, Lk = tile.Lk, lt = tile.lt;
   const int hkv = hq / a.G;
-
-  int s, lt;
-  if (!find_tile(a.cu_q, a.S, a.Tq, BM, a.tiles, item, lane, s, lt)) return;
-  int qa, qb, ka, kb;
-  packed_range(a.cu_q, s, a.Tq, qa, qb);
-  packed_range(a.cu_k, s, a.Tk, ka, kb);
-  const int Lq = qb - qa, Lk = kb - ka;
   const int off = Lk - Lq;  // key of query 0 on the diagonal
   const int row0 = lt * BM + 32 * wave;
   const int row = row0 + c;
   const bool has_row = row < Lq;
-  // keys that the row, the wave's last row and the workgroup's last row see
+  // keys that the row, some row of the wave, and all its rows see
   const int see = a.causal ? min(Lk, row + off + 1) : Lk;
   const int wave_see = row0 >= Lq ? 0 : a.causal ? min(Lk, min(row0 + 31, Lq - 1) + off + 1) : Lk;
-  const int wave_all = a.causal ? min(Lk, row0 + off + 1) : Lk;  // seen by all its rows
-  const int tile_see = a.causal ? min(Lk, min(lt * BM + BM, Lq) + off) : Lk;
-  const int all_tiles = tile_see > 0 ? (tile_see + BN - 1) / BN : 0;
-  // key tiles of this workgroup's share
-  const int t_begin = (int)((long long)all_tiles * blockIdx.y / a.splits);
-  const int n_tiles = (int)((long long)all_tiles * (blockIdx.y + 1) / a.splits);
+  const int wave_all = a.causal ? min(Lk, row0 + off + 1) : Lk;
+  const int n_tiles = t_end;
 
   // ---- query operand ---------------------------------------------------------
   Frag q[KQ];
@@ -340,14 +371,13 @@ void prompt_kernel(PromptArgs a) {
   }
 
   l = add_xor<32>(l);
-  if (a.splits > 1) {  // a part: nothing but the sum 0 for a row that saw no key
-    float* part = a.parts + (((size_t)item * a.Hq + hq) * a.splits + blockIdx.y) * part_floats(BM, D);
+  if (part) {
     const int r0 = 32 * wave + c;
     if (h == 0) {
       part[BM * D + r0] = m;
       part[BM * D + BM + r0] = l;
     }
-    if (has_row && l > 0.f) {
+    if (has_row) {
 #pragma unroll
       for (int i = 0; i < DT; ++i)
 #pragma unroll
@@ -378,44 +408,143 @@ void prompt_kernel(PromptArgs a) {
   if (a.lse && h == 0) a.lse[at] = l > 0.f ? (m + log2_hw(l)) * kLn2 : -INFINITY;
 }
 
-// Joins the parts of a tile's rows: D / 4 threads per row, 4 columns each.
+template <typename T, int D>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2)))
+void prompt_kernel(PromptArgs a) {
+  using Cfg = PromptCfg<T, D>;
+  __shared__ __attribute__((aligned(16))) unsigned char lds[4 * Cfg::TILE];  // K0 K1 V0 V1
+  const int lane = threadIdx.x % kWave;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  int hq = blockIdx.x % a.Hq;
+  // workgroup i runs on XCD i % 8: each XCD takes consecutive heads, which
+  // share keys, of every tile
+  if (a.Hq % 8 == 0) hq = hq % 8 * (a.Hq / 8) + hq / 8;
+  Tile t;
+  if (!find_tile<Cfg::BM>(a, blockIdx.x / a.Hq, lane, t)) return;
+  attend<T, D>(a, t, hq, 0, key_tiles<Cfg::BM, Cfg::BN>(t.lt, t.Lq, t.Lk, a.causal), nullptr, lds,
+               wave, lane);
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2)))
+void prompt_runs_kernel(PromptArgs a) {
+  using Cfg = PromptCfg<T, D>;
+  constexpr int BM = Cfg::BM, BN = Cfg::BN;
+  using R = Runs<BM, BN>;
+  __shared__ __attribute__((aligned(16))) unsigned char lds[4 * Cfg::TILE];  // K0 K1 V0 V1
+  const int lane = threadIdx.x % kWave;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+
+  // units of the lane's sequences (consecutive ones) and of those before them
+  const int per = (a.S + kWave - 1) / kWave;
+  Tile t;
+  int mine = 0;
+  for (int i = 0; i < per; ++i) {
+    t.s = lane * per + i;
+    if (t.s >= a.S) break;
+    t.rows_of(a);
+    mine += R::total(t.Lq, t.Lk, a.causal);
+  }
+  const int incl = wave_incl_scan(mine);
+  const int per_head = last_lane(incl);
+  const long long U = (long long)per_head * a.Hq;
+  // each run has kLeast units at least; consecutive runs on one XCD, so that it
+  // takes consecutive heads, which share keys
+  const int W = (int)min((long long)gridDim.x, (U + kLeast - 1) / kLeast);
+  const int w = xcd_remap(blockIdx.x, gridDim.x);
+  if (w >= W) return;
+  long long u = U * w / W;
+  const long long u_first = u, u_end = U * (w + 1) / W;
+
+  // head, sequence and tile of the run's first unit
+  int hq = __builtin_amdgcn_readfirstlane((int)(u / per_head));
+  int x = __builtin_amdgcn_readfirstlane((int)(u % per_head));  // units before it in the head
+  const int owner = __popcll(__ballot(incl <= x));  // the first lane with more units up to it
+  x -= __builtin_amdgcn_readlane(incl - mine, owner);
+  t.s = owner * per;
+  t.rows_of(a);
+  for (int n = R::total(t.Lq, t.Lk, a.causal); x >= n && t.s + 1 < a.S;
+       n = R::total(t.Lq, t.Lk, a.causal)) {
+    x -= n;
+    ++t.s;
+    t.rows_of(a);
+  }
+  int lo = 0, hi = (t.Lq + BM - 1) / BM;  // before(lo) <= x < before(hi)
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) / 2;
+    if (R::before(mid, t.Lq, t.Lk, a.causal) <= x) lo = mid; else hi = mid;
+  }
+  t.lt = lo;
+  x -= R::before(lo, t.Lq, t.Lk, a.causal);
+
+  while (true) {
+    const int tiles = key_tiles<BM, BN>(t.lt, t.Lq, t.Lk, a.causal), units = max(1, tiles);
+    const int x_end = (int)min((long long)units, x + (u_end - u));
+    const int slot = u == u_first ? 0 : 1;
+    const bool whole = x == 0 && x_end == units;
+    if (x == 0 && threadIdx.x == 0) {
+      // the run that holds unit v is ((v + 1) W - 1) / U
+      const long long w_last = ((u + units) * W - 1) / U;
+      int32_t* join = a.joins + 2 * ((size_t)(t.qa / BM + t.s + t.lt) * a.Hq + hq);
+      join[0] = 2 * w + slot;
+      join[1] = whole ? 1 : (int)(w_last - w) + 1;
+    }
+    attend<T, D>(a, t, hq, x, min(x_end, tiles),
+                 whole ? nullptr : a.parts + (size_t)(2 * w + slot) * part_floats(BM, D), lds, wave,
+                 lane);
+    u += x_end - x;
+    if (u >= u_end) break;
+    __syncthreads();  // the tiles in LDS are read
+    x = 0;
+    if ((++t.lt) * BM >= t.Lq) {  // the next sequence that has queries
+      t.lt = 0;
+      do {
+        if (++t.s == a.S) {
+          t.s = 0;
+          ++hq;
+        }
+        t.rows_of(a);
+      } while (t.Lq == 0);
+    }
+  }
+}
+
+// Joins the parts of a tile's rows (D / 4 threads per row, 4 columns each): the
+// first part is the one that joins names, the others are the first ones of the
+// runs that follow.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a) {
   constexpr int BM = PromptCfg<T, D>::BM;
   constexpr int TPR = D / 4, RPW = 256 / TPR;  // threads per row, rows per workgroup
-  constexpr float kLn2 = 0.6931471805599453f;
-  const int item = blockIdx.x / a.Hq, hq = blockIdx.x % a.Hq;
-  int s, lt, qa, qb;
-  if (!find_tile(a.cu_q, a.S, a.Tq, BM, a.tiles, item, threadIdx.x % kWave, s, lt)) return;
-  packed_range(a.cu_q, s, a.Tq, qa, qb);
+  const int tile = blockIdx.x / a.Hq, hq = blockIdx.x % a.Hq;
+  Tile t;  // tile qa / BM + s + lt; ids that belong to none have no entry in joins
+  t.s = find_sequence(a.S, tile, threadIdx.x % kWave, [&](int k) {
+    return (long long)min(max(a.cu_q[k], 0), a.Tq) / BM + k;
+  });
+  t.rows_of(a);
+  t.lt = tile - (t.qa / BM + t.s);
+  if (t.lt < 0 || (long long)t.lt * BM >= t.Lq) return;
+  const int first = a.joins[2 * (size_t)blockIdx.x], n = a.joins[2 * (size_t)blockIdx.x + 1];
+  if (n == 1) return;
   const int r = blockIdx.y * RPW + threadIdx.x / TPR, d0 = threadIdx.x % TPR * 4;
-  const int row = lt * BM + r;
-  if (row >= qb - qa) return;
-  const size_t step = part_floats(BM, D);
-  const float* part = a.parts + ((size_t)item * a.Hq + hq) * a.splits * step;
-  float m = -1e30f, ms[kMaxSplits], ls[kMaxSplits];
-#pragma unroll
-  for (int z = 0; z < kMaxSplits; ++z) {
-    ls[z] = 0.f;
-    if (z < a.splits) {
-      ms[z] = part[z * step + BM * D + r];
-      ls[z] = part[z * step + BM * D + BM + r];
-    }
-  }
-#pragma unroll
-  for (int z = 0; z < kMaxSplits; ++z)
-    if (ls[z] > 0.f) m = fmaxf(m, ms[z]);
-  float l = 0.f;
+  const int row = t.lt * BM + r;
+  if (row >= t.Lq) return;
+  auto part = [&](int i) {
+    return a.parts + (size_t)(i == 0 ? first : 2 * (first / 2 + i)) * part_floats(BM, D);
+  };
+  float m = kMaxFloor, l = 0.f;
+#pragma unroll 8
+  for (int i = 0; i < n; ++i) m = fmaxf(m, part(i)[BM * D + r]);
   f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-  for (int z = 0; z < kMaxSplits; ++z)
-    if (ls[z] > 0.f) {
-      const float f = exp2_hw(ms[z] - m);
-      l = fmaf(f, ls[z], l);
-      acc += f * *reinterpret_cast<const f32x4*>(part + z * step + r * D + d0);
-    }
+#pragma unroll 8
+  for (int i = 0; i < n; ++i) {
+    const float* p = part(i);
+    const float f = exp2_hw(p[BM * D + r] - m);
+    l = fmaf(f, p[BM * D + BM + r], l);
+    acc += f * *reinterpret_cast<const f32x4*>(p + r * D + d0);
+  }
   const float inv = l > 0.f ? 1.f / l : 0.f;
-  const size_t at = (size_t)(qa + row) * a.Hq + hq;
+  const size_t at = (size_t)(t.qa + row) * a.Hq + hq;
   T* y = static_cast<T*>(a.Y) + at * D + d0;
   if constexpr (Elem<T>::kBf16)
     *reinterpret_cast<bf16x4*>(y) = bf16x4{(bf16)(acc[0] * inv), (bf16)(acc[1] * inv),
@@ -427,26 +556,28 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a) {
 
 long long tiles_of(long long Tq, int S, int BM) { return Tq / BM + S; }
 
-// Workgroups per tile: its keys are shared where the tiles leave more than
-// half of the device's workgroup slots (two per CU) idle, and the sequences'
-// mean length leaves each enough keys to pay for the joining launch.
+// Equal runs, or 0 for whole tiles. Whole tiles leave CUs idle where they are
+// few, by as much as the longest exceeds the mean: under the causal mask about
+// twice below 768 tiles, without one below 384. The mean length has to be worth
+// the joining launch. Two workgroups run per CU; fp32, whose products alone
+// fill the matrix units, takes one run per CU (half the parts).
 template <typename T, int D>
-int splits_of(int S, int Tq, int Tk, int Hq) {
+int runs_of(int S, int Tq, int Tk, int Hq, int causal) {
   using Cfg = PromptCfg<T, D>;
-  constexpr int kSlots = 512;
-  const long long n = tiles_of(Tq, S, Cfg::BM) * Hq;
-  const long long room = kSlots / n, keys = Tk / S / (4 * Cfg::BN);
-  return (int)std::max(1LL, std::min({room, keys, (long long)kMaxSplits}));
+  const long long tiles = tiles_of(Tq, S, Cfg::BM) * Hq;
+  if (tiles > (causal ? 768 : 384) || Tk / S < 2 * kLeast * Cfg::BN) return 0;
+  return Cfg::kB ? 512 : 256;
 }
 
 }  // namespace
 
 template <typename T, int D>
-size_t prompt_attention_workspace(int S, int Tq, int Tk, int Hq) {
+size_t prompt_attention_workspace(int S, int Tq, int Tk, int Hq, int causal) {
   using Cfg = PromptCfg<T, D>;
-  const int splits = splits_of<T, D>(S, Tq, Tk, Hq);
-  if (splits == 1) return 0;
-  return (size_t)tiles_of(Tq, S, Cfg::BM) * Hq * splits * part_floats(Cfg::BM, D) * sizeof(float);
+  const int runs = runs_of<T, D>(S, Tq, Tk, Hq, causal);
+  if (runs == 0) return 0;
+  return 2 * (size_t)runs * part_floats(Cfg::BM, D) * sizeof(float) +
+         (size_t)tiles_of(Tq, S, Cfg::BM) * Hq * 2 * sizeof(int32_t);
 }
 
 template <typename T, int D>
@@ -457,16 +588,20 @@ hipError_t launch_prompt_attention(int S, int Tq, int Tk, int Hq, int Hkv, float
                                    void* workspace, hipStream_t stream) {
   using Cfg = PromptCfg<T, D>;
   const long long tiles = tiles_of(Tq, S, Cfg::BM);
-  const int splits = splits_of<T, D>(S, Tq, Tk, Hq);
   if (tiles * Hq > 0x7fffffff) return hipErrorInvalidConfiguration;
+  const int runs = runs_of<T, D>(S, Tq, Tk, Hq, causal);
+  float* parts = static_cast<float*>(workspace);
   PromptArgs a{Q, K, V, q_stride, k_stride, v_stride, cu_q, cu_k, Y, lse,
-               S, Tq, Tk, Hq, Hq / Hkv, causal, (int)tiles, splits, scale * kLog2e,
-               static_cast<float*>(workspace)};
-  const unsigned grid = (unsigned)(tiles * Hq);
-  hipLaunchKernelGGL((prompt_kernel<T, D>), dim3(grid, (unsigned)splits), dim3(64 * Cfg::NW), 0,
-                     stream, a);
+               S, Tq, Tk, Hq, Hq / Hkv, causal, (int)tiles, scale * kLog2e, parts,
+               reinterpret_cast<int32_t*>(parts + 2 * (size_t)runs * part_floats(Cfg::BM, D))};
+  const unsigned grid = (unsigned)(tiles * Hq), threads = 64 * Cfg::NW;
+  if (runs == 0) {
+    hipLaunchKernelGGL((prompt_kernel<T, D>), dim3(grid), dim3(threads), 0, stream, a);
+    return hipGetLastError();
+  }
+  hipLaunchKernelGGL((prompt_runs_kernel<T, D>), dim3(runs), dim3(threads), 0, stream, a);
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || splits == 1) return e;
+  if (e != hipSuccess) return e;
   hipLaunchKernelGGL((prompt_join_kernel<T, D>), dim3(grid, Cfg::BM * D / 4 / 256), dim3(256), 0,
                      stream, a);
   return hipGetLastError();
@@ -476,7 +611,7 @@ hipError_t launch_prompt_attention(int S, int Tq, int Tk, int Hq, int Hkv, float
   template hipError_t launch_prompt_attention<T, D>(                                              \
       int, int, int, int, int, float, int, const void*, int64_t, const void*, int64_t, const void*, \
       int64_t, const int32_t*, const int32_t*, void*, float*, void*, hipStream_t);                \
-  template size_t prompt_attention_workspace<T, D>(int, int, int, int);
+  template size_t prompt_attention_workspace<T, D>(int, int, int, int, int);
 AVQ_INSTANCE(bf16, 64)
 AVQ_INSTANCE(bf16, 128)
 AVQ_INSTANCE(float, 64)

@@ -152,7 +152,7 @@ def test_one_long_sequence():
 def test_few_queries_many_keys(lens_q, lens_k, d, Hq, causal, dtype):
     """Tiles whose keys several workgroups share (rows without keys among them)."""
     scale = 1 / math.sqrt(d)
-    n = avq.prompt_attention_workspace(dtype, len(lens_q), sum(lens_q), sum(lens_k), Hq, d)
+    n = avq.prompt_attention_workspace(dtype, len(lens_q), sum(lens_q), sum(lens_k), Hq, d, causal)
     assert n > 0 or lens_k[-1] == 3
     Q, K, V = make(lens_q, lens_k, Hq, 1, d, dtype, 7)
     Y, lse = run(Q, K, V, lens_q, lens_k, scale, causal)
