@@ -377,13 +377,17 @@ def _rows(t: torch.Tensor, name: str, H=None, d=None, dtype=None) -> int:
         raise ValueError(f"{name} must be a tensor on the GPU")
     if dtype is not None and t.dtype != dtype:
         raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
-    if t.dim() != 3 or (H is not None and t.shape[1] != H) or (d is not None and t.shape[2] != d):
-        raise ValueError(f"{name} must be [tokens, {'heads' if H is None else H}, "
-                         f"{'d' if d is None else d}], got {tuple(t.shape)}")
-    T, h, w = t.shape
-    if (w > 1 and t.stride(2) != 1) or (h > 1 and t.stride(1) != w):
-        raise ValueError(f"{name}: the heads of a token must be contiguous")
-    return t.stride(0) if T > 1 else h * w
+    shape = t.shape
+    if len(shape) == 3 and (H is None or shape[1] == H) and (d is None or shape[2] == d):
+        T, h, w = shape
+        if t.is_contiguous():
+            return h * w
+        s = t.stride()
+        if (w > 1 and s[2] != 1) or (h > 1 and s[1] != w):
+            raise ValueError(f"{name}: the heads of a token must be contiguous")
+        return s[0] if T > 1 else h * w
+    raise ValueError(f"{name} must be [tokens, {'heads' if H is None else H}, "
+                     f"{'d' if d is None else d}], got {tuple(shape)}")
 
 
 def prompt_attention_workspace(dtype, S: int, Tq: int, Tk: int, Hq: int, d: int,
@@ -438,8 +442,8 @@ def prompt_attention_fwd(Q, K, V, cu_q, cu_k, scale: float, causal: bool = True,
     _same_device(Q, K=K, V=V, cu_q=cu_q, cu_k=cu_k, Y=Y, lse=lse, workspace=workspace)
     _check(lib().avq_prompt_attention_fwd(
         _dtype_code(Q), S, Tq, Tk, Hq, Hkv, d, float(scale), int(bool(causal)),
-        _ptr(Q), q_stride, _ptr(K), k_stride, _ptr(V), v_stride, _ptr(cu_q), _ptr(cu_k), _ptr(Y),
-        _ptr(lse), _ptr(workspace), 0 if workspace is None else workspace.numel(), s))
+        Q.data_ptr(), q_stride, K.data_ptr(), k_stride, V.data_ptr(), v_stride, cu_q.data_ptr(),
+        cu_k.data_ptr(), Y.data_ptr(), _ptr(lse), _ptr(workspace), 0 if workspace is None else workspace.numel(), s))
     return (Y, lse) if with_lse else Y
 
 
@@ -460,17 +464,19 @@ _cache_page_bytes_of = functools.lru_cache(maxsize=256)(cache_page_bytes)
 def _cache(cache, block_table, dtype, page_size, d, fp4, S=None):
     """Checks a cache and its block table; returns (n_pages, Hkv, S, max_pages)."""
     _dev(cache, "cache", torch.uint8)
-    if cache.dim() != 3:
-        raise ValueError(f"cache must be [pages, heads, page bytes], got {tuple(cache.shape)}")
-    n_pages, Hkv, E = cache.shape
+    shape = cache.shape
+    if len(shape) != 3:
+        raise ValueError(f"cache must be [pages, heads, page bytes], got {tuple(shape)}")
+    n_pages, Hkv, E = shape
     need = _cache_page_bytes_of(dtype, page_size, d, bool(fp4))
     if E != need:
         raise ValueError(f"cache holds {E} bytes per page and head, expected {need}")
     _dev(block_table, "block_table", torch.int32)
-    if block_table.dim() != 2 or (S is not None and block_table.shape[0] != S):
+    table = block_table.shape
+    if len(table) != 2 or (S is not None and table[0] != S):
         raise ValueError(f"block_table must be [{'sequences' if S is None else S}, pages], "
-                         f"got {tuple(block_table.shape)}")
-    return n_pages, Hkv, block_table.shape[0], block_table.shape[1]
+                         f"got {tuple(table)}")
+    return n_pages, Hkv, table[0], table[1]
 
 
 def cache_append(K, V, cache, block_table, start, page_size: int, cu=None, Q=None, cos=None,
@@ -531,9 +537,9 @@ def cache_append(K, V, cache, block_table, start, page_size: int, cu=None, Q=Non
                  sin=sin, Q_out=Q_out, K_out=K_out)
     _check(lib().avq_cache_append(
         _dtype_code(K), int(bool(fp4)), S, T, Hq, Hkv, d, n_pages, page_size, max_pages, rot, n_pos,
-        int(bool(interleaved)), _ptr(Q), q_stride, _ptr(K), k_stride, _ptr(V), v_stride, _ptr(cu),
-        _ptr(start), _ptr(block_table), _ptr(cos), _ptr(sin), _ptr(cache), _ptr(Q_out),
-        _ptr(K_out), s))
+        int(bool(interleaved)), _ptr(Q), q_stride, K.data_ptr(), k_stride, V.data_ptr(), v_stride,
+        _ptr(cu), start.data_ptr(), block_table.data_ptr(), _ptr(cos), _ptr(sin),
+        cache.data_ptr(), _ptr(Q_out), _ptr(K_out), s))
     return Q_out, K_out
 
 
@@ -553,8 +559,9 @@ def cache_gather(cache, block_table, start, cu, T: int, page_size: int, dtype, d
     _dev(V, "V", dtype, (T, Hkv, d))
     _same_device(cache, block_table=block_table, start=start, cu=cu, K=K, V=V)
     _check(lib().avq_cache_gather(
-        _DTYPES[dtype], int(bool(fp4)), S, T, Hkv, d, n_pages, page_size, max_pages, _ptr(cache),
-        _ptr(cu), _ptr(start), _ptr(block_table), _ptr(K), _ptr(V), s))
+        _DTYPES[dtype], int(bool(fp4)), S, T, Hkv, d, n_pages, page_size, max_pages,
+        cache.data_ptr(), cu.data_ptr(), start.data_ptr(), block_table.data_ptr(), K.data_ptr(),
+        V.data_ptr(), s))
     return K, V
 
 
@@ -585,9 +592,12 @@ def cache_attention_fwd(Q, cache, block_table, lens, page_size: int, scale: floa
     if Q.dim() != 4:
         raise ValueError(f"Q must be [sequences, tokens, heads, d], got {tuple(Q.shape)}")
     S, n_q, Hq, d = Q.shape
-    if S > 1 and n_q > 1 and Q.stride(0) != n_q * Q.stride(1):
+    if Q.is_contiguous():
+        q_stride = Hq * d
+    elif S > 1 and n_q > 1 and Q.stride(0) != n_q * Q.stride(1):
         raise ValueError("Q: the tokens must be evenly spaced")
-    q_stride = _rows(Q.flatten(0, 1) if n_q == 1 or S == 1 else Q.view(S * n_q, Hq, d), "Q")
+    else:
+        q_stride = _rows(Q.view(S * n_q, Hq, d), "Q")
     n_pages, Hkv, _, max_pages = _cache(cache, block_table, Q.dtype, page_size, d, fp4, S)
     _dev(lens, "lens", torch.int32, (S,))
     s = _launch_stream(stream, Q.device)
@@ -605,6 +615,6 @@ def cache_attention_fwd(Q, cache, block_table, lens, page_size: int, scale: floa
                  workspace=workspace)
     _check(lib().avq_cache_attention_fwd(
         _dtype_code(Q), int(bool(fp4)), S, n_q, Hq, Hkv, d, n_pages, page_size, max_pages,
-        float(scale), _ptr(Q), q_stride, _ptr(cache), _ptr(lens), _ptr(block_table), _ptr(Y),
-        _ptr(lse), _ptr(workspace), workspace.numel(), s))
+        float(scale), Q.data_ptr(), q_stride, cache.data_ptr(), lens.data_ptr(),
+        block_table.data_ptr(), Y.data_ptr(), _ptr(lse), workspace.data_ptr(), workspace.numel(), s))
     return (Y, lse) if with_lse else Y

@@ -453,3 +453,19 @@ def test_refusals():
     for kw in (dict(scale=0.0), dict(workspace=torch.empty(64, dtype=torch.uint8, device="cuda"))):
         with pytest.raises(avq.AvqError):
             avq.cache_attention_fwd(**(base | kw))
+
+
+def test_query_strides():
+    """Queries as a slice of a fused projection; tokens must be evenly spaced."""
+    t = Setup([60, 33, 5], [0, 0, 0], 2, 2, 64, BF16, True, 16)
+    cache, table, n = fill(t)
+    for n_q in (1, 3):
+        fused = torch.randn(3, n_q, 6, 64, generator=torch.Generator().manual_seed(3)).to(BF16).cuda()
+        Q = fused[:, :, :4]
+        assert not Q.is_contiguous()
+        Y = avq.cache_attention_fwd(Q, cache, table, n, 16, 0.3, fp4=True)
+        assert torch.equal(Y, avq.cache_attention_fwd(Q.contiguous(), cache, table, n, 16, 0.3, fp4=True))
+    with pytest.raises(ValueError):
+        avq.cache_attention_fwd(fused[:, :2, :4], cache, table, n, 16, 0.3, fp4=True)
+    with pytest.raises(ValueError):
+        avq.cache_attention_fwd(fused.transpose(1, 2)[:, :4], cache, table, n, 16, 0.3, fp4=True)
