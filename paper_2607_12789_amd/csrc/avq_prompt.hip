@@ -120,12 +120,9 @@ __device__ __forceinline__ int key_tiles(int lt, int Lq, int Lk, int causal) {
 template <int BM>
 __device__ __forceinline__ bool find_tile(const PromptArgs& a, int i, int lane, Tile& t) {
   if (a.S <= kWave) {
-    int nt = 0;
-    if (lane < a.S) {
-      int b, e;
-      packed_range(a.cu_q, lane, a.Tq, b, e);
-      nt = (e - b + BM - 1) / BM;
-    }
+    Tile mine{lane, 0, 0, 0, 0, 0};  // the lane's sequence
+    if (lane < a.S) mine.rows_of(a);
+    const int nt = (mine.Lq + BM - 1) / BM;
     auto from = [&](int L) { return last_lane(wave_incl_scan(max(nt - L, 0))); };
     if (i >= from(0)) return false;
     int lo = 0, hi = a.tiles;  // N(lo) > i >= N(hi)
@@ -139,7 +136,10 @@ __device__ __forceinline__ bool find_tile(const PromptArgs& a, int i, int lane, 
     const unsigned long long at = __ballot(nt > lo && bits_below(in) == rank);
     t.s = (int)__builtin_ctzll(at);
     t.lt = lo;
-    t.rows_of(a);
+    t.qa = __builtin_amdgcn_readlane(mine.qa, t.s);
+    t.ka = __builtin_amdgcn_readlane(mine.ka, t.s);
+    t.Lq = __builtin_amdgcn_readlane(mine.Lq, t.s);
+    t.Lk = __builtin_amdgcn_readlane(mine.Lk, t.s);
     return true;
   }
   const int tile = a.tiles - 1 - i;
