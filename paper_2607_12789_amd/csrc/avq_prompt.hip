@@ -31,7 +31,6 @@ namespace avq {
 
 namespace {
 
-constexpr int kLeast = 4;  // key tiles of a run, at least
 constexpr float kLazy = 8.f;         // log2 units the running max may lag behind
 constexpr float kMaxFloor = -1e30f;  // finite start of the running max
 constexpr float kLn2 = 0.6931471805599453f;
@@ -67,7 +66,13 @@ struct PromptCfg {
   static constexpr bool kB = Elem<T>::kBf16;
   static constexpr int NW = 4;            // waves
   static constexpr int BM = 32 * NW;      // queries per workgroup
-  static constexpr int BN = kB ? 64 : 32;  // keys per tile
+  // Keys per tile: 64, but 32 for bf16 at d = 128, where three workgroups then
+  // fit a CU (168 registers, 32 KB of LDS) instead of two (18 packed prompts
+  // 156 to 149 us, 16384 tokens 1026 to 1011; d = 64: 27.4 us with 64, 28.7 with
+  // 32 for 8 x 784 patches), and for fp32 (LDS)
+  static constexpr int BN = kB && D == 64 ? 64 : 32;
+  static constexpr int kLeast = (kB ? 256 : 128) / BN;  // key tiles of a run, at least
+  static constexpr int kPerCu = kB && D == 128 ? 3 : 2;  // waves per SIMD, at least
   static constexpr int KT = BN / 32;
   static constexpr int DT = D / 32;
   static constexpr int ESZ = sizeof(T);
@@ -409,7 +414,7 @@ __device__ __forceinline__ void attend(const PromptArgs& a, const Tile& tile, in
 }
 
 template <typename T, int D>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2)))
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(PromptCfg<T, D>::kPerCu)))
 void prompt_kernel(PromptArgs a) {
   using Cfg = PromptCfg<T, D>;
   __shared__ __attribute__((aligned(16))) unsigned char lds[4 * Cfg::TILE];  // K0 K1 V0 V1
@@ -426,7 +431,7 @@ void prompt_kernel(PromptArgs a) {
 }
 
 template <typename T, int D>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2)))
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(PromptCfg<T, D>::kPerCu)))
 void prompt_runs_kernel(PromptArgs a) {
   using Cfg = PromptCfg<T, D>;
   constexpr int BM = Cfg::BM, BN = Cfg::BN;
@@ -450,7 +455,7 @@ void prompt_runs_kernel(PromptArgs a) {
   const long long U = (long long)per_head * a.Hq;
   // each run has kLeast units at least; consecutive runs on one XCD, so that it
   // takes consecutive heads, which share keys
-  const int W = (int)min((long long)gridDim.x, (U + kLeast - 1) / kLeast);
+  const int W = (int)min((long long)gridDim.x, (U + Cfg::kLeast - 1) / Cfg::kLeast);
   const int w = xcd_remap(blockIdx.x, gridDim.x);
   if (w >= W) return;
   long long u = U * w / W;
@@ -556,17 +561,23 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a) {
 
 long long tiles_of(long long Tq, int S, int BM) { return Tq / BM + S; }
 
-// Equal runs, or 0 for whole tiles. Whole tiles leave CUs idle where they are
-// few, by as much as the longest exceeds the mean: under the causal mask about
-// twice below 768 tiles, without one below 384. The mean length has to be worth
-// the joining launch. Two workgroups run per CU; fp32, whose products alone
-// fill the matrix units, takes one run per CU (half the parts).
+// Equal runs (workgroups), or 0 for whole tiles. With whole tiles the longest
+// tile's chain of keys bounds the time; with runs it is the mean work, which is
+// tiles / 1024 of it under the causal mask (tiles / 512 without one, two tiles
+// per CU), and the parts: 15 to 20 us for writing and joining them. So runs are
+// taken where the chain exceeds the mean by enough keys, the sequences' mean
+// length standing for all. Measured, us whole / runs (d = 128): one sequence of
+// 8192 tokens and 8 heads 188 / 170, 4096 and 16 98 / 100, 6144 and 16 173 /
+// 190, 2048 and 32 53 / 68, 1024 and 8 25 / 27, chunks of 512 and 300 behind
+// 15872 and 4001 300 / 118 (d = 64: 219 / 76); fp32, d = 64, 2048 and 8 146 / 52.
+// fp32's products alone fill the matrix units: one run per CU, half the parts.
 template <typename T, int D>
 int runs_of(int S, int Tq, int Tk, int Hq, int causal) {
   using Cfg = PromptCfg<T, D>;
-  const long long tiles = tiles_of(Tq, S, Cfg::BM) * Hq;
-  if (tiles > (causal ? 768 : 384) || Tk / S < 2 * kLeast * Cfg::BN) return 0;
-  return Cfg::kB ? 512 : 256;
+  const long long tiles = tiles_of(Tq, S, Cfg::BM) * Hq, full = causal ? 1024 : 512;
+  const long long excess = (full - tiles) * (Tk / S) / full;
+  if (excess < (Cfg::kB ? 2500 : 250)) return 0;
+  return Cfg::kB ? 768 : 256;
 }
 
 }  // namespace

@@ -147,16 +147,53 @@ def test_one_long_sequence():
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("d,Hq,causal", [(64, 2, True), (128, 7, False), (128, 1, True)])
-@pytest.mark.parametrize("lens_q,lens_k", [([5], [3000]), ([130, 1], [2000, 2600]),
-                                           ([300, 4], [290, 3])])
+@pytest.mark.parametrize("lens_q,lens_k", [([5], [3000]), ([130, 1], [3100, 2700]),
+                                           ([300, 0, 0, 4, 0], [290, 9000, 0, 6000, 0])])
 def test_few_queries_many_keys(lens_q, lens_k, d, Hq, causal, dtype):
-    """Tiles whose keys several workgroups share (rows without keys among them)."""
+    """Tiles whose keys several workgroups share (rows without keys among them,
+    and sequences without queries)."""
     scale = 1 / math.sqrt(d)
     n = avq.prompt_attention_workspace(dtype, len(lens_q), sum(lens_q), sum(lens_k), Hq, d, causal)
-    assert n > 0 or lens_k[-1] == 3
+    assert n > 0
     Q, K, V = make(lens_q, lens_k, Hq, 1, d, dtype, 7)
     Y, lse = run(Q, K, V, lens_q, lens_k, scale, causal)
     check_prompt(Y, lse, Q, K, V, lens_q, lens_k, scale, causal)
+
+
+@pytest.mark.parametrize("S", [64, 70, 130])
+def test_many_sequences_with_many_keys(S):
+    """Shared tiles of more sequences than lanes."""
+    lens_q, lens_k = [s % 3 for s in range(S)], [2600 + 17 * (s % 40) for s in range(S)]
+    assert avq.prompt_attention_workspace(BF16, S, sum(lens_q), sum(lens_k), 1, 64) > 0
+    Q, K, V = make(lens_q, lens_k, 1, 1, 64, BF16, 13)
+    Y, lse = run(Q, K, V, lens_q, lens_k, 0.2, True)
+    check_prompt(Y, lse, Q, K, V, lens_q, lens_k, 0.2, True)
+
+
+def test_shared_tiles_captured_with_one_workspace():
+    """Two graphs with one workspace, replayed in turn with eager calls between,
+    for lengths that change."""
+    g = torch.Generator().manual_seed(8)
+    Q = torch.randn(200, 4, 64, generator=g).to(BF16).cuda()
+    K, V = (torch.randn(9000, 2, 64, generator=g).to(BF16).cuda() for _ in range(2))
+    cq, ck = cu([100, 100]), cu([4500, 4500])
+    n = avq.prompt_attention_workspace(BF16, 2, 200, 9000, 4, 64)
+    ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+    outs = [torch.empty(200, 4, 64, dtype=BF16, device="cuda") for _ in range(2)]
+    avq.prompt_attention_fwd(Q, K, V, cq, ck, 0.3, Y=outs[0], workspace=ws)
+    torch.cuda.synchronize()
+    graphs = []
+    for Y in outs:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            avq.prompt_attention_fwd(Q, K, V, cq, ck, 0.3, Y=Y, workspace=ws)
+    for i, (a, b) in enumerate([([100, 100], [4500, 4500]), ([1, 199], [8000, 1000]),
+                                ([128, 72], [0, 9000]), ([0, 200], [3000, 6000])] * 2):
+        cq.copy_(cu(a)), ck.copy_(cu(b))
+        want = avq.prompt_attention_fwd(Q, K, V, cq, ck, 0.3)
+        graphs[i % 2].replay()
+        torch.cuda.synchronize()
+        assert torch.equal(outs[i % 2], want), i
 
 
 @pytest.mark.parametrize("S", [63, 64, 65, 300])

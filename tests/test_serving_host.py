@@ -115,6 +115,7 @@ def test_page_bytes(L):
 def test_workspace_bytes(L):
     assert avq.prompt_attention_workspace(torch.bfloat16, 4, 1 << 16, 1 << 16, 16, 128) == 0
     assert avq.prompt_attention_workspace(torch.bfloat16, 1, 300, 1 << 16, 4, 128) > 0
+    assert avq.prompt_attention_workspace(torch.bfloat16, 1, 300, 300, 4, 128) == 0
     for bad in ((9, 1, 8, 8, 4, 64, 1), (BF16, 0, 8, 8, 4, 64, 1), (BF16, 1, -1, 8, 4, 64, 1),
                 (BF16, 1, 8, 8, 4, 96, 1), (BF16, 1, 8, 8, 4, 64, 2)):
         assert L.avq_prompt_attention_workspace(*bad) == -1
