@@ -3,7 +3,7 @@
 //
 // Bound by the cache: every byte of it is read once and each key takes 4 d
 // flop per query row, so the rows of one key-value head (n_q tokens x Hq/Hkv
-// heads) are processed together, 16 to a tile. Everything is computed
+// heads) are processed together, 16 or 32 at once. Everything is computed
 // transposed, keys x queries, with 16x16x32 bf16 (16x16x4 fp32) MFMA, from
 // registers: nothing is staged in LDS. A wave takes 32 keys per step. Row 4 g
 // + r of logit tile t is key 8 g + 4 t + r, so lane (g, c) ends up with the
@@ -37,7 +37,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
-constexpr int kRows = 16;                  // query rows per tile
+constexpr int kRows = 16;                  // query rows per MFMA tile
 constexpr int kStep = 32;                  // keys per wave and step
 constexpr int kUnit = kStep * kWaves;      // keys per step of a workgroup
 constexpr int kWholeSteps = 4;             // steps of sequences that are not divided
@@ -71,8 +71,8 @@ __device__ __forceinline__ int units_of(int len, int unit) {
   return max(1, (len + unit - 1) / unit);
 }
 
-// A part: numerators [kRows][D], then maxima [kRows] and sums [kRows].
-__host__ __device__ constexpr size_t part_floats(int D) { return (size_t)kRows * (D + 2); }
+// A part: numerators [rows][D], then maxima [rows] and sums [rows].
+__host__ __device__ constexpr size_t part_floats(int rows, int D) { return (size_t)rows * (D + 2); }
 
 template <typename T, int D, bool FP4>
 struct Keys {
@@ -108,15 +108,18 @@ __device__ __forceinline__ void load_words(const unsigned char* p, uint32_t* w) 
 // sequences of up to 16000 positions 136.8 us with three, 140.8 with four;
 // the bf16 native cache at d = 128 spills with four (20.2 and 36.1 us for 16
 // sequences of 4 tokens).
-template <typename T, int D, bool FP4>
-constexpr int kPerCu = !Elem<T>::kBf16 && D == 128 && !FP4 ? 2 : 3;
+// NT: MFMA tiles of query rows that share a step's keys. Two where there are
+// more than 16 rows: the cache is then read, and 4 bits decoded, half as often
+// (fp32's products bound it either way: always one).
+template <typename T, int D, bool FP4, int NT>
+constexpr int kPerCu = NT == 2 || (!Elem<T>::kBf16 && D == 128 && !FP4) ? 2 : 3;
 
-template <typename T, int D, bool FP4>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kPerCu<T, D, FP4>)))
+template <typename T, int D, bool FP4, int NT>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kPerCu<T, D, FP4, NT>)))
 void cache_attention_kernel(CacheAttnArgs a) {
   constexpr bool kB = Elem<T>::kBf16;
   using Raw = Keys<T, D, FP4>;
-  constexpr int H2 = D / 64;
+  constexpr int H2 = D / 64, R = NT * kRows;
   constexpr int KQ = kB ? D / 32 : D / 4;  // k-steps of the logit product
   using QFrag = typename std::conditional<kB, bf16x8, float>::type;
 
@@ -179,35 +182,40 @@ void cache_attention_kernel(CacheAttnArgs a) {
     // ---- one segment: units [x, x_end) of sequence s, head hr ---------------
     const int x_end = (int)min((long long)n_units, x + (u_end - u));
     const int steps = a.unit / kUnit, y_end = x_end * steps;  // steps of kUnit keys
-    const int kvh = hr / a.row_tiles, row0 = hr % a.row_tiles * kRows;
-    const int row = row0 + c;                    // the lane's query
-    const bool has_row = row < rows_all;
-    const int qi = has_row ? row / a.G : 0;
-    const int hq = kvh * a.G + (has_row ? row % a.G : 0);
-    const int last = has_row ? len - a.n_q + qi + 1 : 0;  // keys the row sees
-    const int all_see = len - a.n_q + 1;                  // keys every row sees
-
-    QFrag q[KQ];
-    {
+    const int kvh = hr / a.row_tiles, row0 = hr % a.row_tiles * R;
+    const int all_see = len - a.n_q + 1;  // keys every row sees
+    int last[NT];                         // keys the lane's rows see
+    QFrag q[NT][KQ];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const int row = row0 + kRows * n + c;
+      const bool has_row = row < rows_all;
+      const int qi = has_row ? row / a.G : 0;
+      const int hq = kvh * a.G + (has_row ? row % a.G : 0);
+      last[n] = has_row ? len - a.n_q + qi + 1 : 0;
       const T* qp = static_cast<const T*>(a.Q) + ((size_t)s * a.n_q + qi) * a.q_stride +
                     (size_t)hq * D;
 #pragma unroll
       for (int k = 0; k < KQ; ++k) {
         if constexpr (kB) {
           const int d0 = FP4 ? D / 4 * g + 8 * k : 32 * k + 8 * g;
-          q[k] = *reinterpret_cast<const bf16x8*>(qp + d0);
+          q[n][k] = *reinterpret_cast<const bf16x8*>(qp + d0);
         } else {
-          q[k] = qp[FP4 ? D / 4 * g + k : 16 * (k / 4) + 4 * g + k % 4];
+          q[n][k] = qp[FP4 ? D / 4 * g + k : 16 * (k / 4) + 4 * g + k % 4];
         }
       }
     }
 
-    float m = kMaxFloor, l = 0.f;
-    f32x4 o[H2][4];
+    float m[NT], l[NT];
+    f32x4 o[NT][H2][4];
 #pragma unroll
-    for (int h = 0; h < H2; ++h)
+    for (int n = 0; n < NT; ++n) {
+      m[n] = kMaxFloor, l[n] = 0.f;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) o[h][k] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int h = 0; h < H2; ++h)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) o[n][h][k] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
 
     // ---- loads: the octet's page for values, the key rows' for keys ---------
     // Pages are looked up one step ahead; rows are not requested ahead (a
@@ -272,11 +280,21 @@ void cache_attention_kernel(CacheAttnArgs a) {
       const int vpos = key0 + 8 * g;
       ahead = lookup(y + 1);
 
-      // ---- logits ----------------------------------------------------------
-      f32x4 sc[2];
+      // ---- logits: tile tt, keys 8 g + 4 tt + r ------------------------------
+      f32x4 sc[NT][2];
 #pragma unroll
       for (int tt = 0; tt < 2; ++tt) {
-        f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int n = 0; n < NT; ++n) sc[n][tt] = f32x4{0.f, 0.f, 0.f, 0.f};
+        auto product = [&](int k, auto key) {  // step k of the contraction
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            if constexpr (kB)
+              sc[n][tt] = mfma_bf16(key, q[n][k], sc[n][tt]);
+            else
+              sc[n][tt] = mfma_f32(key, q[n][k], sc[n][tt]);
+          }
+        };
         if constexpr (FP4) {
           const float scale = __uint_as_float(raw.ks[tt] << 23);
 #pragma unroll
@@ -287,8 +305,7 @@ void cache_attention_kernel(CacheAttnArgs a) {
               const bf16x2 p1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(wd, scale, 1);
               const bf16x2 p2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(wd, scale, 2);
               const bf16x2 p3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(wd, scale, 3);
-              acc = mfma_bf16(bf16x8{p0[0], p0[1], p1[0], p1[1], p2[0], p2[1], p3[0], p3[1]},
-                              q[k], acc);
+              product(k, bf16x8{p0[0], p0[1], p1[0], p1[1], p2[0], p2[1], p3[0], p3[1]});
             } else {
               const auto p0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(wd, scale, 0);
               const auto p1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(wd, scale, 1);
@@ -296,56 +313,55 @@ void cache_attention_kernel(CacheAttnArgs a) {
               const auto p3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(wd, scale, 3);
               const float e[8] = {p0[0], p0[1], p1[0], p1[1], p2[0], p2[1], p3[0], p3[1]};
 #pragma unroll
-              for (int i = 0; i < 8; ++i) acc = mfma_f32(e[i], q[8 * k + i], acc);
+              for (int i = 0; i < 8; ++i) product(8 * k + i, e[i]);
             }
           }
         } else {
 #pragma unroll
           for (int k = 0; k < Raw::KW / 4; ++k) {
             if constexpr (kB) {
-              acc = mfma_bf16(__builtin_bit_cast(bf16x8, *reinterpret_cast<uint4*>(&raw.k[tt][4 * k])),
-                              q[k], acc);
+              product(k, __builtin_bit_cast(bf16x8, *reinterpret_cast<uint4*>(&raw.k[tt][4 * k])));
             } else {
 #pragma unroll
-              for (int i = 0; i < 4; ++i)
-                acc = mfma_f32(__uint_as_float(raw.k[tt][4 * k + i]), q[4 * k + i], acc);
+              for (int i = 0; i < 4; ++i) product(4 * k + i, __uint_as_float(raw.k[tt][4 * k + i]));
             }
           }
         }
-        sc[tt] = acc;
       }
 
-      // ---- masks: only where a key of the step is not seen by every row ------
-      float p[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) p[i] = sc[i / 4][i % 4] * a.scale_log2;
+      // ---- masks (only where a key of the step is not seen by every row), running
+      // max, weights
       const bool masked = key0 + kStep > all_see || __any(!vok);
-      if (masked) {
+      float p[NT][8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (!vok || vpos + i >= last) p[i] = -INFINITY;
-      }
-
-      // ---- running max, weights ---------------------------------------------
-      float mx = fmaxf(fmaxf(fmaxf(p[0], p[1]), fmaxf(p[2], p[3])),
-                       fmaxf(fmaxf(p[4], p[5]), fmaxf(p[6], p[7])));
-      if (__any(mx > m + kLazy)) {
-        mx = max_xor<32>(max_xor<16>(mx));
-        const float mn = fmaxf(m, mx);
-        const float f = exp2_hw(m - mn);
-        m = mn;
-        l *= f;
+      for (int n = 0; n < NT; ++n) {
 #pragma unroll
-        for (int h = 0; h < H2; ++h)
+        for (int i = 0; i < 8; ++i) p[n][i] = sc[n][i / 4][i % 4] * a.scale_log2;
+        if (masked) {
 #pragma unroll
-          for (int k = 0; k < 4; ++k)
+          for (int i = 0; i < 8; ++i)
+            if (!vok || vpos + i >= last[n]) p[n][i] = -INFINITY;
+        }
+        float mx = fmaxf(fmaxf(fmaxf(p[n][0], p[n][1]), fmaxf(p[n][2], p[n][3])),
+                         fmaxf(fmaxf(p[n][4], p[n][5]), fmaxf(p[n][6], p[n][7])));
+        if (__any(mx > m[n] + kLazy)) {
+          mx = max_xor<32>(max_xor<16>(mx));
+          const float mn = fmaxf(m[n], mx);
+          const float f = exp2_hw(m[n] - mn);
+          m[n] = mn;
+          l[n] *= f;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) o[h][k][r] *= f;
-      }
+          for (int h = 0; h < H2; ++h)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        p[i] = exp2_hw(p[i] - m);
-        l += p[i];
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+              for (int r = 0; r < 4; ++r) o[n][h][k][r] *= f;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          p[n][i] = exp2_hw(p[n][i] - m[n]);
+          l[n] += p[n][i];
+        }
       }
 
       // ---- values ------------------------------------------------------------
@@ -377,8 +393,15 @@ void cache_attention_kernel(CacheAttnArgs a) {
         }
       }
       if constexpr (kB) {
-        const bf16x8 pb = {(bf16)p[0], (bf16)p[1], (bf16)p[2], (bf16)p[3],
-                           (bf16)p[4], (bf16)p[5], (bf16)p[6], (bf16)p[7]};
+        bf16x8 pb[NT];
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) pb[n][i] = (bf16)p[n][i];
+        auto product = [&](int h, int k, const bf16x8& v) {  // columns 64 h + 4 c + k
+#pragma unroll
+          for (int n = 0; n < NT; ++n) o[n][h][k] = mfma_bf16(v, pb[n], o[n][h][k]);
+        };
 #pragma unroll
         for (int h = 0; h < H2; ++h) {
           if constexpr (FP4) {
@@ -399,20 +422,20 @@ void cache_attention_kernel(CacheAttnArgs a) {
               }
 #pragma unroll
               for (int b = 0; b < 2; ++b)
-                o[h][2 * pr + b] =
-                    mfma_bf16(bf16x8{e[0][b], e[1][b], e[2][b], e[3][b], e[4][b], e[5][b],
-                                     e[6][b], e[7][b]},
-                              pb, o[h][2 * pr + b]);
+                product(h, 2 * pr + b,
+                        bf16x8{e[0][b], e[1][b], e[2][b], e[3][b], e[4][b], e[5][b], e[6][b], e[7][b]});
             }
           } else {
 #pragma unroll
             for (int k = 0; k < 4; ++k)
-              o[h][k] = mfma_bf16(
-                  __builtin_bit_cast(bf16x8, *reinterpret_cast<uint4*>(&raw.v[h][4 * k])), pb,
-                  o[h][k]);
+              product(h, k, __builtin_bit_cast(bf16x8, *reinterpret_cast<uint4*>(&raw.v[h][4 * k])));
           }
         }
       } else {
+        auto product = [&](int h, int k, int i, float v) {  // key i of the octet
+#pragma unroll
+          for (int n = 0; n < NT; ++n) o[n][h][k] = mfma_f32(v, p[n][i], o[n][h][k]);
+        };
 #pragma unroll
         for (int h = 0; h < H2; ++h) {
           if constexpr (FP4) {
@@ -431,40 +454,48 @@ void cache_attention_kernel(CacheAttnArgs a) {
                 const auto e3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(wd, f[i + 3], 3);
 #pragma unroll
                 for (int b = 0; b < 2; ++b) {
-                  f32x4 acc = o[h][2 * pr + b];
-                  acc = mfma_f32(e0[b], p[i], acc);
-                  acc = mfma_f32(e1[b], p[i + 1], acc);
-                  acc = mfma_f32(e2[b], p[i + 2], acc);
-                  acc = mfma_f32(e3[b], p[i + 3], acc);
-                  o[h][2 * pr + b] = acc;
+                  product(h, 2 * pr + b, i, e0[b]);
+                  product(h, 2 * pr + b, i + 1, e1[b]);
+                  product(h, 2 * pr + b, i + 2, e2[b]);
+                  product(h, 2 * pr + b, i + 3, e3[b]);
                 }
               }
           } else {
 #pragma unroll
             for (int k = 0; k < 4; ++k)
 #pragma unroll
-              for (int i = 0; i < 8; ++i)
-                o[h][k] = mfma_f32(__uint_as_float(raw.v[h][8 * k + i]), p[i], o[h][k]);
+              for (int i = 0; i < 8; ++i) product(h, k, i, __uint_as_float(raw.v[h][8 * k + i]));
           }
         }
       }
     }
 
-    // ---- the four waves joined ------------------------------------------------
-    l = add_xor<32>(add_xor<16>(l));
-    if (g == 0) {
-      s_m[wave][c] = m;
-      s_l[wave][c] = l;
+    // ---- the four waves joined, 16 rows at a time -------------------------------
+    const long long seg = (long long)s * heads + hr;
+    const int slot = u == u_first ? 0 : 1;
+    const bool whole = x == 0 && x_end == n_units;
+    if (tid == 0 && x == 0) {
+      // the workgroup that holds unit v is ((v + 1) W - 1) / U
+      const long long w_last = ((u + n_units) * W - 1) / U;
+      a.joins[2 * seg] = 2 * w + slot;
+      a.joins[2 * seg + 1] = whole ? 1 : (int)(w_last - w) + 1;
     }
-    // row 4 g + r of value tile k of half h is column 64 h + 4 (4 g + r) + k
 #pragma unroll
-    for (int h = 0; h < H2; ++h)
+    for (int n = 0; n < NT; ++n) {
+      if (n > 0) __syncthreads();  // the exchange area is used again
+      const float ln = add_xor<32>(add_xor<16>(l[n]));
+      if (g == 0) {
+        s_m[wave][c] = m[n];
+        s_l[wave][c] = ln;
+      }
+      // row 4 g + r of value tile k of half h is column 64 h + 4 (4 g + r) + k
 #pragma unroll
-      for (int r = 0; r < 4; ++r)
-        *reinterpret_cast<f32x4*>(&s_o[wave][c][64 * h + 16 * g + 4 * r]) =
-            f32x4{o[h][0][r], o[h][1][r], o[h][2][r], o[h][3][r]};
-    __syncthreads();
-    {
+      for (int h = 0; h < H2; ++h)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          *reinterpret_cast<f32x4*>(&s_o[wave][c][64 * h + 16 * g + 4 * r]) =
+              f32x4{o[n][h][0][r], o[n][h][1][r], o[n][h][2][r], o[n][h][3][r]};
+      __syncthreads();
       constexpr int C = D / 16;  // columns per thread
       const int rr = tid / 16, d0 = tid % 16 * C;
       float mm = s_m[0][rr];
@@ -476,11 +507,9 @@ void cache_attention_kernel(CacheAttnArgs a) {
 #pragma unroll
         for (int k = 0; k < C; ++k) acc[k] = fmaf(f, s_o[i][rr][d0 + k], acc[k]);
       }
-      const long long seg = (long long)s * heads + hr;
-      const long long seg_u = u - x;  // unit where the segment starts
-      const int out_row = row0 + rr;
-      if (x == 0 && x_end == n_units) {
-        if (out_row < rows_all) {
+      const int row = kRows * n + rr, out_row = row0 + row;
+      if (out_row < rows_all) {
+        if (whole) {
           const int oi = out_row / a.G, oh = kvh * a.G + out_row % a.G;
           const size_t at = ((size_t)s * a.n_q + oi) * a.Hq + oh;
           const float inv = ll > 0.f ? 1.f / ll : 0.f;
@@ -488,24 +517,14 @@ void cache_attention_kernel(CacheAttnArgs a) {
 #pragma unroll
           for (int k = 0; k < C; ++k) y[k] = (T)(acc[k] * inv);
           if (a.lse && d0 == 0) a.lse[at] = ll > 0.f ? (mm + log2_hw(ll)) * kLn2 : -INFINITY;
-        }
-        if (tid == 0) a.joins[2 * seg + 1] = 1;
-      } else {
-        const int slot = u == u_first ? 0 : 1;
-        float* part = a.parts + (size_t)(2 * w + slot) * part_floats(D);
-        if (out_row < rows_all) {
+        } else {
+          float* part = a.parts + (size_t)(2 * w + slot) * part_floats(R, D);
 #pragma unroll
-          for (int k = 0; k < C; ++k) part[rr * D + d0 + k] = acc[k];
+          for (int k = 0; k < C; ++k) part[row * D + d0 + k] = acc[k];
           if (d0 == 0) {
-            part[kRows * D + rr] = mm;
-            part[kRows * D + kRows + rr] = ll;
+            part[R * D + row] = mm;
+            part[R * D + R + row] = ll;
           }
-        }
-        if (tid == 0 && x == 0) {
-          // the workgroup that holds unit v is ((v + 1) W - 1) / U
-          const long long w_last = ((seg_u + n_units) * W - 1) / U;
-          a.joins[2 * seg] = 2 * w + slot;
-          a.joins[2 * seg + 1] = (int)(w_last - w) + 1;
         }
       }
     }
@@ -526,8 +545,9 @@ void cache_attention_kernel(CacheAttnArgs a) {
 // that joins names, the others in slot 0 of the workgroups that follow. All
 // maxima are read first, so that the numerators are plain weighted sums, read
 // by all threads (4 columns each) without waiting for one another.
-template <typename T, int D>
+template <typename T, int D, int NT>
 __global__ __launch_bounds__(kThreads) void cache_join_kernel(CacheAttnArgs a) {
+  constexpr int R = NT * kRows;
   constexpr int TPP = D / 4;              // threads per part
   constexpr int PG = kThreads / TPP;      // parts in flight
   __shared__ float s_f[kMaxWorkgroups];   // weight of each part
@@ -539,15 +559,15 @@ __global__ __launch_bounds__(kThreads) void cache_join_kernel(CacheAttnArgs a) {
   const int first = a.joins[2 * seg];
   const int heads = a.cache.Hkv * a.row_tiles;
   const int s = seg / heads, hr = seg % heads;
-  const int kvh = hr / a.row_tiles, row = hr % a.row_tiles * kRows + rr;
+  const int kvh = hr / a.row_tiles, row = hr % a.row_tiles * R + rr;
   if (row >= a.n_q * a.G) return;
   const int tid = threadIdx.x, wave = tid / kWave, lane = tid % kWave;
   auto part = [&](int i) {
-    return a.parts + (size_t)(i == 0 ? first : 2 * (first / 2 + i)) * part_floats(D);
+    return a.parts + (size_t)(i == 0 ? first : 2 * (first / 2 + i)) * part_floats(R, D);
   };
   float m = kMaxFloor;
   for (int i = tid; i < n; i += kThreads) {
-    s_f[i] = part(i)[kRows * D + rr];
+    s_f[i] = part(i)[R * D + rr];
     m = fmaxf(m, s_f[i]);
   }
 #pragma unroll
@@ -559,7 +579,7 @@ __global__ __launch_bounds__(kThreads) void cache_join_kernel(CacheAttnArgs a) {
   for (int i = tid; i < n; i += kThreads) {
     const float f = exp2_hw(s_f[i] - m);
     s_f[i] = f;
-    l = fmaf(f, part(i)[kRows * D + kRows + rr], l);
+    l = fmaf(f, part(i)[R * D + R + rr], l);
   }
 #pragma unroll
   for (int k = 1; k < kWave; k *= 2) l += __shfl_xor(l, k, kWave);
@@ -585,13 +605,40 @@ __global__ __launch_bounds__(kThreads) void cache_join_kernel(CacheAttnArgs a) {
   if (a.lse && tid == 0) a.lse[at] = l > 0.f ? (m + log2_hw(l)) * kLn2 : -INFINITY;
 }
 
-int row_tiles_of(int n_q, int G) { return (n_q * G + kRows - 1) / kRows; }
-size_t parts_bytes(int D) { return kMaxWorkgroups * 2 * part_floats(D) * sizeof(float); }
+int row_tiles_of(int n_q, int G, int NT) { return (n_q * G + NT * kRows - 1) / (NT * kRows); }
+// Two tiles run on half as many workgroups.
+size_t parts_bytes(int D) { return kMaxWorkgroups * 2 * part_floats(kRows, D) * sizeof(float); }
+
+template <typename T, int D, bool FP4, int NT>
+hipError_t launch_tiles(CacheAttnArgs& a, hipStream_t stream) {
+  a.row_tiles = row_tiles_of(a.n_q, a.G, NT);
+  const long long segs = (long long)a.S * a.cache.Hkv * a.row_tiles;
+  // Short sequences are not divided: four steps take less than the joining
+  // launch that dividing them needs.
+  const long long room =
+      (((long long)a.cache.max_pages << a.cache.ps_log2) + kUnit - 1) / kUnit;
+  a.unit = kUnit * (room <= kWholeSteps ? (int)room : 1);
+  const long long cap = room <= kWholeSteps ? 1 : room;  // units of a segment, at most
+  // as many workgroups as run at once: one more would start when the first
+  // ends, after as long again
+  DeviceInfo dev;
+  hipError_t e = device_info(&dev);
+  if (e != hipSuccess) return e;
+  const long long slots = std::min(kMaxWorkgroups / NT, dev.cus * kPerCu<T, D, FP4, NT>);
+  const unsigned W = (unsigned)std::min(segs * cap, slots);
+  hipLaunchKernelGGL((cache_attention_kernel<T, D, FP4, NT>), dim3(W), dim3(kThreads), 0, stream, a);
+  e = hipGetLastError();
+  if (e != hipSuccess || cap == 1) return e;  // segments of one unit are never in parts
+  hipLaunchKernelGGL((cache_join_kernel<T, D, NT>),
+                     dim3((unsigned)segs, (unsigned)std::min(NT * kRows, a.n_q * a.G)),
+                     dim3(kThreads), 0, stream, a);
+  return hipGetLastError();
+}
 
 }  // namespace
 
 size_t cache_attention_workspace(int S, int n_q, int Hq, int Hkv, int d) {
-  const size_t segs = (size_t)S * Hkv * row_tiles_of(n_q, Hq / Hkv);
+  const size_t segs = (size_t)S * Hkv * row_tiles_of(n_q, Hq / Hkv, 1);
   return parts_bytes(d) + segs * 2 * sizeof(int32_t);
 }
 
@@ -607,33 +654,12 @@ hipError_t launch_cache_attention(const CacheShape& c, int S, int n_q, int Hq, f
   a.parts = static_cast<float*>(workspace);
   a.joins = reinterpret_cast<int32_t*>(static_cast<unsigned char*>(workspace) + parts_bytes(D));
   a.S = S, a.n_q = n_q, a.Hq = Hq, a.G = Hq / c.Hkv;
-  a.row_tiles = row_tiles_of(n_q, a.G);
   a.scale_log2 = scale * kLog2e;
-  const long long segs = (long long)S * c.Hkv * a.row_tiles;
-  // Short sequences are not divided: four steps take less than the joining
-  // launch that dividing them needs.
-  const long long room = ((long long)c.max_pages * c.page_size + kUnit - 1) / kUnit;
-  a.unit = kUnit * (room <= kWholeSteps ? (int)room : 1);
-  const long long cap = room <= kWholeSteps ? 1 : room;  // units of a segment, at most
-  const long long most = segs * cap;
-  // as many workgroups as run at once: one more would start when the first
-  // ends, after as long again
-  DeviceInfo dev;
-  hipError_t e = device_info(&dev);
-  if (e != hipSuccess) return e;
-  const long long slots = std::min(
-      kMaxWorkgroups, dev.cus * (c.fp4 ? kPerCu<T, D, true> : kPerCu<T, D, false>));
-  const unsigned W = (unsigned)std::min(most, slots);
-  if (c.fp4)
-    hipLaunchKernelGGL((cache_attention_kernel<T, D, true>), dim3(W), dim3(kThreads), 0, stream, a);
-  else
-    hipLaunchKernelGGL((cache_attention_kernel<T, D, false>), dim3(W), dim3(kThreads), 0, stream, a);
-  e = hipGetLastError();
-  if (e != hipSuccess || cap == 1) return e;  // segments of one unit are never in parts
-  hipLaunchKernelGGL((cache_join_kernel<T, D>),
-                     dim3((unsigned)segs, (unsigned)std::min(kRows, n_q * a.G)), dim3(kThreads), 0,
-                     stream, a);
-  return hipGetLastError();
+  if constexpr (Elem<T>::kBf16) {
+    if (n_q * a.G > kRows)
+      return c.fp4 ? launch_tiles<T, D, true, 2>(a, stream) : launch_tiles<T, D, false, 2>(a, stream);
+  }
+  return c.fp4 ? launch_tiles<T, D, true, 1>(a, stream) : launch_tiles<T, D, false, 1>(a, stream);
 }
 
 #define AVQ_INSTANCE(T, D)                                                                         \
