@@ -380,8 +380,9 @@ avq_status_t avq_codebook_update(avq_dtype_t dtype, int32_t B, int32_t H, int32_
  * v_stride elements from one token's row to the next (at least H*d, a multiple
  * of 16 bytes, at most 2^22: slices of a fused projection need no copy).
  * cu [S + 1] (int32, device): sequence s owns rows cu[s] .. cu[s + 1] - 1; cu
- * must not decrease and may leave rows behind cu[S], whose outputs are left as
- * they were. Values outside [0, T] are taken as the nearest of 0 and T.
+ * must not decrease (if it does, outputs are unspecified) and may leave rows
+ * behind cu[S], whose outputs are left as they were. Values outside [0, T] are
+ * taken as the nearest of 0 and T.
  * Hq query heads share Hkv key-value heads: head h reads h / (Hq / Hkv).
  * Sizes: d in {64, 128}; Hq <= 1024, a multiple of Hkv; S <= 2^20; T <= 2^24
  * packed tokens, 0 included (nothing is then written). Element counts may pass
@@ -519,7 +520,7 @@ int64_t avq_cache_attention_workspace(int32_t S, int32_t n_q, int32_t Hq, int32_
  * j < lens[s] - (n_q - 1 - i). Y and lse as in avq_prompt_attention_fwd; a
  * token that sees no position (lens[s] = 0: an idle entry of a padded batch)
  * gets 0 and -inf. lens is taken as at least 0 and at most
- * max_pages * page_size.
+ * max_pages * page_size; S * max_pages * page_size <= 2^37.
  *
  *   n_q          1 .. 16
  *   Q            [S * n_q] rows of [Hq][d], dtype, q_stride as above

@@ -526,6 +526,11 @@ avq_status_t avq_cache_attention_fwd(avq_dtype_t dtype, avq_cache_t format, int3
   if (n_q > kMaxDrafts)
     return fail(AVQ_ERR_UNSUPPORTED, "%s: n_q=%d: at most %d tokens per sequence", name, n_q,
                 kMaxDrafts);
+  const int64_t segments = (int64_t)S * Hkv * ((n_q * (Hq / Hkv) + 15) / 16);
+  if (segments > 0x7fffffff)
+    return fail(AVQ_ERR_UNSUPPORTED, "%s: S=%d sequences of Hkv=%d heads: too many", name, S, Hkv);
+  if ((int64_t)S * (((int64_t)max_pages * page_size + 127) / 128) > (1LL << 30))
+    return fail(AVQ_ERR_UNSUPPORTED, "%s: S * max_pages * page_size: at most 2^37 positions", name);
   if (!Q || !cache || !lens || !block_table || !Y || !workspace) return null_pointer(name);
   if (!aligned16(Q) || !aligned16(cache) || !aligned16(lens) || !aligned16(block_table) ||
       !aligned16(Y) || !aligned16(lse) || !aligned16(workspace))

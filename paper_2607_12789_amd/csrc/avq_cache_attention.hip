@@ -44,7 +44,7 @@ constexpr int kWholeSteps = 4;             // steps of sequences that are not di
 constexpr int kMaxWorkgroups = 1024;       // slots in the workspace
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kLazy = 8.f;         // log2 units the running max may lag behind
-constexpr float kMaxFloor = -1e30f;  // finite start of the running max
+constexpr float kMaxFloor = -3e38f;  // finite start of the running max
 
 struct CacheAttnArgs {
   CacheArgs cache;
@@ -336,7 +336,8 @@ void cache_attention_kernel(CacheAttnArgs a) {
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) p[n][i] = sc[n][i / 4][i % 4] * a.scale_log2;
+        for (int i = 0; i < 8; ++i)
+          p[n][i] = scaled_less(sc[n][i / 4][i % 4], a.scale_log2, 0.f);
         if (masked) {
 #pragma unroll
           for (int i = 0; i < 8; ++i)

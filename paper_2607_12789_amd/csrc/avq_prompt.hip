@@ -32,7 +32,8 @@ namespace avq {
 namespace {
 
 constexpr float kLazy = 8.f;         // log2 units the running max may lag behind
-constexpr float kMaxFloor = -1e30f;  // finite start of the running max
+constexpr float kMaxFloor = -3e38f;  // finite start of the running max
+constexpr float kFused = 0x1p24f;    // largest |max scale| at which s scale - max scale is one fma
 constexpr float kLn2 = 0.6931471805599453f;
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
@@ -56,9 +57,11 @@ struct PromptArgs {
   int S, Tq, Tk, Hq, G, causal;
   int tiles;  // query tiles per head, at most
   float scale_log2;
+  float lazy;  // kLazy / scale_log2
   // equal runs: see part_floats and Runs
   float* parts;
-  int32_t* joins;  // [tiles][Hq][2]: first part, number of parts
+  int32_t* joins;  // [tiles][Hq][2]: first part, number of parts; before it, one
+                   // entry that says whether joins is filled
 };
 
 template <typename T, int D>
@@ -268,7 +271,14 @@ __device__ __forceinline__ void attend(const PromptArgs& a, const Tile& tile, in
     }
   };
 
-  float m = kMaxFloor, l = 0.f;
+  // m: the running max of s. The weights exp2((s - m) scale) are one fma with
+  // ms = m scale and exp2. It leaves the rounding error of ms, up to |ms| / 2^24,
+  // in the exponent: one factor for all weights of a row while that is at most
+  // 1, but beyond float's range for the largest s. Once a row has such a max
+  // its wave subtracts m first, in the branch of the new max (which is then
+  // taken for every tile), and ms is 0: the usual path has no more work.
+  float m = kMaxFloor, ms = kMaxFloor, limit = kMaxFloor, l = 0.f;
+  bool fused = true;
   f32x16 o[DT];
 #pragma unroll
   for (int i = 0; i < DT; ++i) o[i] = f32x16{};
@@ -317,11 +327,23 @@ __device__ __forceinline__ void attend(const PromptArgs& a, const Tile& tile, in
     for (int i = 0; i < KT; ++i)
 #pragma unroll
       for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sc[i][r]);
-    mx *= a.scale_log2;
-    if (__any(mx > m + kLazy)) {
-      const float mn = fmaxf(m, max_xor<32>(mx));
-      const float f = exp2_hw(m - mn);
+    if (__any(mx > limit)) {
+      const float mn = fmaxf(m, max_xor<32>(mx)), mns = fmaxf(mn * a.scale_log2, kMaxFloor);
+      const bool was = fused;
+      fused = was && !__any(fabsf(mns) > kFused && mn > kMaxFloor);
+      const float f = mn == kMaxFloor ? 1.f
+                                      : exp2_hw(fused ? ms - mns
+                                                : was ? fmaf(-mn, a.scale_log2, ms)
+                                                      : (m - mn) * a.scale_log2);
       m = mn;
+      ms = fused ? mns : 0.f;
+      limit = fused ? mn + a.lazy : -INFINITY;
+      if (!fused) {
+#pragma unroll
+        for (int i = 0; i < KT; ++i)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) sc[i][r] -= m;
+      }
       l *= f;
 #pragma unroll
       for (int i = 0; i < DT; ++i)
@@ -332,7 +354,7 @@ __device__ __forceinline__ void attend(const PromptArgs& a, const Tile& tile, in
     for (int i = 0; i < KT; ++i)
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        sc[i][r] = exp2_hw(fmaf(sc[i][r], a.scale_log2, -m));
+        sc[i][r] = exp2_hw(fmaf(sc[i][r], a.scale_log2, -ms));
         l += sc[i][r];
       }
 
@@ -376,10 +398,11 @@ __device__ __forceinline__ void attend(const PromptArgs& a, const Tile& tile, in
   }
 
   l = add_xor<32>(l);
+  if (!fused) ms = m * a.scale_log2;
   if (part) {
     const int r0 = 32 * wave + c;
     if (h == 0) {
-      part[BM * D + r0] = m;
+      part[BM * D + r0] = ms;
       part[BM * D + BM + r0] = l;
     }
     if (has_row) {
@@ -410,7 +433,7 @@ __device__ __forceinline__ void attend(const PromptArgs& a, const Tile& tile, in
         *reinterpret_cast<f32x4*>(y + d0) =
             f32x4{o[i][r] * inv, o[i][r + 1] * inv, o[i][r + 2] * inv, o[i][r + 3] * inv};
     }
-  if (a.lse && h == 0) a.lse[at] = l > 0.f ? (m + log2_hw(l)) * kLn2 : -INFINITY;
+  if (a.lse && h == 0) a.lse[at] = l > 0.f ? (ms + log2_hw(l)) * kLn2 : -INFINITY;
 }
 
 template <typename T, int D>
@@ -444,12 +467,18 @@ void prompt_runs_kernel(PromptArgs a) {
   const int per = (a.S + kWave - 1) / kWave;
   Tile t;
   int mine = 0;
+  bool fine = true;
   for (int i = 0; i < per; ++i) {
     t.s = lane * per + i;
     if (t.s >= a.S) break;
     t.rows_of(a);
     mine += R::total(t.Lq, t.Lk, a.causal);
+    fine = fine && a.cu_q[t.s] <= a.cu_q[t.s + 1];
   }
+  // sequences that overlap would have more tiles than joins has room for
+  fine = __all(fine);
+  if (blockIdx.x == 0 && threadIdx.x == 0) a.joins[-1] = fine;
+  if (!fine) return;
   const int incl = wave_incl_scan(mine);
   const int per_head = last_lane(incl);
   const long long U = (long long)per_head * a.Hq;
@@ -529,6 +558,7 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a) {
   t.rows_of(a);
   t.lt = tile - (t.qa / BM + t.s);
   if (t.lt < 0 || (long long)t.lt * BM >= t.Lq) return;
+  if (a.joins[-1] == 0) return;
   const int first = a.joins[2 * (size_t)blockIdx.x], n = a.joins[2 * (size_t)blockIdx.x + 1];
   if (n == 1) return;
   const int r = blockIdx.y * RPW + threadIdx.x / TPR, d0 = threadIdx.x % TPR * 4;
@@ -588,7 +618,7 @@ size_t prompt_attention_workspace(int S, int Tq, int Tk, int Hq, int causal) {
   const int runs = runs_of<T, D>(S, Tq, Tk, Hq, causal);
   if (runs == 0) return 0;
   return 2 * (size_t)runs * part_floats(Cfg::BM, D) * sizeof(float) +
-         (size_t)tiles_of(Tq, S, Cfg::BM) * Hq * 2 * sizeof(int32_t);
+         ((size_t)tiles_of(Tq, S, Cfg::BM) * Hq * 2 + 4) * sizeof(int32_t);
 }
 
 template <typename T, int D>
@@ -603,8 +633,8 @@ hipError_t launch_prompt_attention(int S, int Tq, int Tk, int Hq, int Hkv, float
   const int runs = runs_of<T, D>(S, Tq, Tk, Hq, causal);
   float* parts = static_cast<float*>(workspace);
   PromptArgs a{Q, K, V, q_stride, k_stride, v_stride, cu_q, cu_k, Y, lse,
-               S, Tq, Tk, Hq, Hq / Hkv, causal, (int)tiles, scale * kLog2e, parts,
-               reinterpret_cast<int32_t*>(parts + 2 * (size_t)runs * part_floats(Cfg::BM, D))};
+               S, Tq, Tk, Hq, Hq / Hkv, causal, (int)tiles, scale * kLog2e, kLazy / (scale * kLog2e), parts,
+               reinterpret_cast<int32_t*>(parts + 2 * (size_t)runs * part_floats(Cfg::BM, D)) + 4};
   const unsigned grid = (unsigned)(tiles * Hq), threads = 64 * Cfg::NW;
   if (runs == 0) {
     hipLaunchKernelGGL((prompt_kernel<T, D>), dim3(grid), dim3(threads), 0, stream, a);

@@ -469,3 +469,15 @@ def test_query_strides():
         avq.cache_attention_fwd(fused[:, :2, :4], cache, table, n, 16, 0.3, fp4=True)
     with pytest.raises(ValueError):
         avq.cache_attention_fwd(fused.transpose(1, 2)[:, :4], cache, table, n, 16, 0.3, fp4=True)
+
+
+@pytest.mark.parametrize("fp4", [False, True])
+def test_equal_logits_of_any_size(fp4):
+    for n, size in ((70, 2.0 ** 50), (700, -(2.0 ** 50))):
+        t = Setup([n], [0], 1, 1, 64, F32, fp4, 16)
+        t.K = torch.full((n, 1, 64), size)
+        cache, table, lens = fill(t)
+        Q = torch.full((1, 1, 1, 64), 2.0 ** 56).cuda()
+        Y = avq.cache_attention_fwd(Q, cache, table, lens, 16, 1.0, fp4=fp4).cpu()
+        v = read_cache(t.cache, t.table, 0, n, F32, fp4, 16, 64)[1][0]
+        assert ((Y[0, 0, 0].double() - v.mean(0)).abs() <= n * 2.0 ** -24 * 2 * v.abs().mean(0)).all()

@@ -270,3 +270,33 @@ def test_refusals():
             avq.prompt_attention_fwd(**a)
     with pytest.raises(avq.AvqError):
         avq.prompt_attention_fwd(Q, K, V, c, c, -1.0)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_equal_logits_of_any_size(dtype):
+    """Equal logits give the mean of the values, however far from 0 they lie."""
+    for n, size in ((70, 1e15), (70, -1e15), (3000, -1e15)):
+        Q = torch.full((2, 1, 64), 1e17).to(dtype)
+        K = torch.full((n, 1, 64), size).to(dtype)
+        V = make([1], [n], 1, 1, 64, dtype)[2]
+        Y, _ = run(Q, K, V, [2], [n], 1.0, False)
+        half = 2.0 ** -8 if dtype == BF16 else n * 2.0 ** -24
+        mean, size_ = V[:, 0].double().mean(0), V[:, 0].double().abs().mean(0)
+        assert ((Y[:, 0].double() - mean).abs() <= half * (mean.abs() + size_)).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("n", [300, 3000])
+def test_one_huge_key_among_ordinary_ones(n, dtype):
+    """A wave with a row of equal logits, one that sees a huge logit, and ones
+    that see it with the other sign (weight 0) among ordinary ones."""
+    Q, K, V = make([34], [n], 1, 1, 64, dtype, 9)
+    Q = -Q.abs()
+    Q[0], Q[1] = 0, 1
+    K[200] = 2.0 ** 40
+    Y, lse = run(Q, K, V, [34], [n], 0.125, False)
+    check_attention(Y[:1, 0], lse[:1, 0], Q[:1, 0], K[:, 0], V[:, 0], 0.125, seen_of(1, n, False))
+    assert torch.equal(Y[1, 0], V[200, 0])
+    rest = torch.arange(n) != 200
+    check_attention(Y[2:, 0], lse[2:, 0], Q[2:, 0], K[rest, 0], V[rest, 0], 0.125,
+                    seen_of(32, n - 1, False))
