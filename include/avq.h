@@ -414,9 +414,10 @@ int64_t avq_prompt_attention_workspace(avq_dtype_t dtype, int32_t S, int32_t Tq,
  *   Y      [Tq][Hq][d] dtype, contiguous, out
  *   lse    [Tq][Hq] fp32, out, nullable
  *   workspace  avq_prompt_attention_workspace() bytes, NULL allowed for 0
- * One launch, two with a workspace. Arithmetic as avq_attention_fwd: bf16 products with fp32 accumulation and
- * fp32 softmax state, weights rounded to bf16 for the value product; fp32
- * throughout for fp32.
+ * (Tq / 128 + S) * Hq < 2^24. One launch, two with a workspace. Arithmetic as
+ * avq_attention_fwd: bf16 products with fp32 accumulation and fp32 softmax
+ * state, weights rounded to bf16 for the value product; fp32 throughout for
+ * fp32.
  */
 avq_status_t avq_prompt_attention_fwd(avq_dtype_t dtype, int32_t S, int32_t Tq, int32_t Tk,
                                       int32_t Hq, int32_t Hkv, int32_t d, float scale,
@@ -520,7 +521,8 @@ int64_t avq_cache_attention_workspace(int32_t S, int32_t n_q, int32_t Hq, int32_
  * j < lens[s] - (n_q - 1 - i). Y and lse as in avq_prompt_attention_fwd; a
  * token that sees no position (lens[s] = 0: an idle entry of a padded batch)
  * gets 0 and -inf. lens is taken as at least 0 and at most
- * max_pages * page_size; S * max_pages * page_size <= 2^37.
+ * max_pages * page_size; S * max_pages * page_size <= 2^37 and
+ * S * Hkv * ceil(n_q * Hq / Hkv / 16) < 2^24.
  *
  *   n_q          1 .. 16
  *   Q            [S * n_q] rows of [Hq][d], dtype, q_stride as above

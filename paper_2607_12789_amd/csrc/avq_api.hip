@@ -322,6 +322,12 @@ constexpr int64_t kMaxStride = 1 << 22;  // elements between tokens: 64 rows sta
 constexpr int kMaxHeads = 1024;
 constexpr int kMaxDrafts = 16;
 
+// Workgroups of 256 threads along one dimension of a launch: less than this.
+constexpr int64_t kMaxBlocks = 1 << 24;
+int64_t cache_segments(int32_t S, int32_t n_q, int32_t Hq, int32_t Hkv) {
+  return (int64_t)S * Hkv * ((n_q * (Hq / Hkv) + 15) / 16);
+}
+
 avq_status_t check_heads(const char* name, avq_dtype_t dtype, int32_t S, int32_t Hq, int32_t Hkv,
                          int32_t d) {
   if (dtype != AVQ_F32 && dtype != AVQ_BF16)
@@ -392,7 +398,8 @@ int64_t avq_prompt_attention_workspace(avq_dtype_t dtype, int32_t S, int32_t Tq,
                                        int32_t Hq, int32_t d, int32_t causal) {
   if ((dtype != AVQ_F32 && dtype != AVQ_BF16) || (d != 64 && d != 128) || S < 1 ||
       S > (1 << 20) || Hq < 1 || Hq > kMaxHeads || Tq < 0 || Tk < 0 || Tq > (1 << 24) ||
-      Tk > (1 << 24) || (causal != 0 && causal != 1))
+      Tk > (1 << 24) || (causal != 0 && causal != 1) ||
+      ((int64_t)Tq / 128 + S) * Hq >= kMaxBlocks)
     return -1;
   return (int64_t)AVQ_BY_TYPE(prompt_attention_workspace, S, Tq, Tk, Hq, causal);
 }
@@ -415,6 +422,9 @@ avq_status_t avq_prompt_attention_fwd(avq_dtype_t dtype, int32_t S, int32_t Tq, 
     return fail(AVQ_ERR_INVALID_ARG, "%s: Tq=%d and Tk=%d must not be negative", name, Tq, Tk);
   if (Tq > (1 << 24) || Tk > (1 << 24))
     return fail(AVQ_ERR_UNSUPPORTED, "%s: Tq=%d, Tk=%d: at most 2^24 tokens", name, Tq, Tk);
+  if (((int64_t)Tq / 128 + S) * Hq >= kMaxBlocks)
+    return fail(AVQ_ERR_UNSUPPORTED, "%s: Tq=%d tokens of S=%d sequences and Hq=%d heads: too many",
+                name, Tq, S, Hq);
   if (causal != 0 && causal != 1)
     return fail(AVQ_ERR_INVALID_ARG, "%s: causal=%d: must be 0 or 1", name, causal);
   if (!cu_q || !cu_k || (Tq > 0 && (!Q || !Y)) || (Tk > 0 && (!K || !V))) return null_pointer(name);
@@ -504,7 +514,8 @@ avq_status_t avq_cache_gather(avq_dtype_t dtype, avq_cache_t format, int32_t S, 
 
 int64_t avq_cache_attention_workspace(int32_t S, int32_t n_q, int32_t Hq, int32_t Hkv, int32_t d) {
   if (S < 1 || S > (1 << 20) || n_q < 1 || n_q > kMaxDrafts || Hq < 1 || Hkv < 1 ||
-      Hq > kMaxHeads || Hq % Hkv != 0 || (d != 64 && d != 128))
+      Hq > kMaxHeads || Hq % Hkv != 0 || (d != 64 && d != 128) ||
+      cache_segments(S, n_q, Hq, Hkv) >= kMaxBlocks)
     return -1;
   return (int64_t)avq::cache_attention_workspace(S, n_q, Hq, Hkv, d);
 }
@@ -526,9 +537,9 @@ avq_status_t avq_cache_attention_fwd(avq_dtype_t dtype, avq_cache_t format, int3
   if (n_q > kMaxDrafts)
     return fail(AVQ_ERR_UNSUPPORTED, "%s: n_q=%d: at most %d tokens per sequence", name, n_q,
                 kMaxDrafts);
-  const int64_t segments = (int64_t)S * Hkv * ((n_q * (Hq / Hkv) + 15) / 16);
-  if (segments > 0x7fffffff)
-    return fail(AVQ_ERR_UNSUPPORTED, "%s: S=%d sequences of Hkv=%d heads: too many", name, S, Hkv);
+  if (cache_segments(S, n_q, Hq, Hkv) >= kMaxBlocks)
+    return fail(AVQ_ERR_UNSUPPORTED, "%s: S=%d sequences of Hq=%d, Hkv=%d heads: too many", name, S,
+                Hq, Hkv);
   if ((int64_t)S * (((int64_t)max_pages * page_size + 127) / 128) > (1LL << 30))
     return fail(AVQ_ERR_UNSUPPORTED, "%s: S * max_pages * page_size: at most 2^37 positions", name);
   if (!Q || !cache || !lens || !block_table || !Y || !workspace) return null_pointer(name);

@@ -20,6 +20,7 @@
 #include "avq_cache.hpp"
 #include "avq_launch.hpp"
 
+#include <algorithm>
 #include <type_traits>
 
 namespace avq {
@@ -29,6 +30,12 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
 constexpr int kRowSteps = 4;  // pieces of a token that a wave takes
+
+// Workgroups lie in rows of kGridRow: a launch has fewer than 2^32 threads along x.
+constexpr long long kGridRow = 1 << 22;
+__device__ __forceinline__ int block_of() {
+  return (int)(blockIdx.y * (unsigned)kGridRow + blockIdx.x);
+}
 
 struct TokenArgs {
   const int32_t* cu;     // [S + 1], null: one token per sequence
@@ -129,7 +136,7 @@ template <typename T, int D, bool FP4>
 __device__ __forceinline__ void append_rows(const AppendArgs& a) {
   constexpr int LPR = D / 8, HPS = kWave / LPR;  // lanes per row, heads per piece
   const int lane = threadIdx.x % kWave;
-  const int wave = __builtin_amdgcn_readfirstlane(blockIdx.x * kWaves + threadIdx.x / kWave);
+  const int wave = __builtin_amdgcn_readfirstlane(block_of() * kWaves + threadIdx.x / kWave);
   const int t = wave / a.groups;
   if (t >= a.tok.T) return;
   const int first = wave % a.groups * a.steps;
@@ -258,7 +265,7 @@ template <typename T, int D, bool FP4>
 __device__ __forceinline__ void append_values(const AppendArgs& a) {
   constexpr int LPR = D / 8, HPS = kWave / LPR;
   const int lane = threadIdx.x % kWave;
-  const long long wave = (long long)(blockIdx.x - a.row_blocks) * kWaves +
+  const long long wave = (long long)(block_of() - a.row_blocks) * kWaves +
                          __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int Hkv = a.cache.Hkv, HG = (Hkv + HPS - 1) / HPS;
   const long long slot = wave / HG;
@@ -347,7 +354,7 @@ __device__ __forceinline__ void append_values(const AppendArgs& a) {
 
 template <typename T, int D, bool FP4>
 __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a) {
-  if ((int)blockIdx.x < a.row_blocks)
+  if (block_of() < a.row_blocks)
     append_rows<T, D, FP4>(a);
   else
     append_values<T, D, FP4>(a);
@@ -376,7 +383,7 @@ template <typename T, int D, bool FP4>
 __device__ __forceinline__ void gather_keys(const GatherArgs& a) {
   constexpr int LPR = D / 8, HPS = kWave / LPR;
   const int lane = threadIdx.x % kWave;
-  const int wave = __builtin_amdgcn_readfirstlane(blockIdx.x * kWaves + threadIdx.x / kWave);
+  const int wave = __builtin_amdgcn_readfirstlane(block_of() * kWaves + threadIdx.x / kWave);
   const int t0 = wave / a.groups * a.tokens;
   if (t0 >= a.tok.T) return;
   const int first = wave % a.groups * a.steps;
@@ -427,7 +434,7 @@ template <typename T, int D, bool FP4>
 __device__ __forceinline__ void gather_values(const GatherArgs& a) {
   constexpr int LPR = D / 8, HPS = kWave / LPR;
   const int lane = threadIdx.x % kWave;
-  const long long wave = (long long)(blockIdx.x - a.row_blocks) * kWaves +
+  const long long wave = (long long)(block_of() - a.row_blocks) * kWaves +
                          __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int Hkv = a.cache.Hkv, HG = (Hkv + HPS - 1) / HPS;
   const long long slot = wave / HG;
@@ -485,7 +492,7 @@ __device__ __forceinline__ void gather_values(const GatherArgs& a) {
 
 template <typename T, int D, bool FP4>
 __global__ __launch_bounds__(kThreads) void gather_kernel(GatherArgs a) {
-  if ((int)blockIdx.x < a.row_blocks)
+  if (block_of() < a.row_blocks)
     gather_keys<T, D, FP4>(a);
   else
     gather_values<T, D, FP4>(a);
@@ -511,6 +518,9 @@ void share_rows(Args& a, int pieces) {
   const int most = (long long)a.tok.T * pieces < 1024 ? 1 : kRowSteps;
   a.groups = (pieces + most - 1) / most;
   a.steps = (pieces + a.groups - 1) / a.groups;
+}
+dim3 grid_of(long long blocks) {
+  return dim3((unsigned)std::min(blocks, kGridRow), (unsigned)((blocks + kGridRow - 1) / kGridRow));
 }
 template <int D>
 long long octet_blocks(const TokenArgs& t, int Hkv) {
@@ -539,12 +549,12 @@ hipError_t launch_cache_append(const CacheShape& c, int S, int T_, int Hq, int r
   share_rows(a, a.q_steps + a.k_steps);
   const long long rows = ((long long)T_ * a.groups + kWaves - 1) / kWaves;
   const long long grid = rows + octet_blocks<D>(a.tok, c.Hkv);
-  if (grid * kWaves > 0x7fffffff) return hipErrorInvalidConfiguration;
+  if ((grid + kGridRow) * kWaves > 0x7fffffff) return hipErrorInvalidConfiguration;
   a.row_blocks = (int)rows;
   if (c.fp4)
-    hipLaunchKernelGGL((append_kernel<T, D, true>), dim3((unsigned)grid), dim3(kThreads), 0, stream, a);
+    hipLaunchKernelGGL((append_kernel<T, D, true>), grid_of(grid), dim3(kThreads), 0, stream, a);
   else
-    hipLaunchKernelGGL((append_kernel<T, D, false>), dim3((unsigned)grid), dim3(kThreads), 0, stream, a);
+    hipLaunchKernelGGL((append_kernel<T, D, false>), grid_of(grid), dim3(kThreads), 0, stream, a);
   return hipGetLastError();
 }
 
@@ -563,12 +573,12 @@ hipError_t launch_cache_gather(const CacheShape& c, int S, int T_, const void* c
   a.tokens = (long long)T_ * a.groups < 16384 ? 1 : kRowSteps / a.steps;
   const long long rows = (((long long)T_ + a.tokens - 1) / a.tokens * a.groups + kWaves - 1) / kWaves;
   const long long grid = rows + octet_blocks<D>(a.tok, c.Hkv);
-  if (grid * kWaves > 0x7fffffff) return hipErrorInvalidConfiguration;
+  if ((grid + kGridRow) * kWaves > 0x7fffffff) return hipErrorInvalidConfiguration;
   a.row_blocks = (int)rows;
   if (c.fp4)
-    hipLaunchKernelGGL((gather_kernel<T, D, true>), dim3((unsigned)grid), dim3(kThreads), 0, stream, a);
+    hipLaunchKernelGGL((gather_kernel<T, D, true>), grid_of(grid), dim3(kThreads), 0, stream, a);
   else
-    hipLaunchKernelGGL((gather_kernel<T, D, false>), dim3((unsigned)grid), dim3(kThreads), 0, stream, a);
+    hipLaunchKernelGGL((gather_kernel<T, D, false>), grid_of(grid), dim3(kThreads), 0, stream, a);
   return hipGetLastError();
 }
 

@@ -555,9 +555,9 @@ __global__ __launch_bounds__(kThreads) void cache_join_kernel(CacheAttnArgs a) {
   __shared__ float s_red[2 * kWaves];
   __shared__ __attribute__((aligned(16))) float s_acc[PG][D];
   const int seg = blockIdx.x, rr = blockIdx.y;
-  const int n = a.joins[2 * seg + 1];
+  const int n = a.joins[2 * (size_t)seg + 1];
   if (n == 1) return;
-  const int first = a.joins[2 * seg];
+  const int first = a.joins[2 * (size_t)seg];
   const int heads = a.cache.Hkv * a.row_tiles;
   const int s = seg / heads, hr = seg % heads;
   const int kvh = hr / a.row_tiles, row = hr % a.row_tiles * R + rr;

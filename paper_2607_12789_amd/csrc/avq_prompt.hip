@@ -629,11 +629,11 @@ hipError_t launch_prompt_attention(int S, int Tq, int Tk, int Hq, int Hkv, float
                                    void* workspace, hipStream_t stream) {
   using Cfg = PromptCfg<T, D>;
   const long long tiles = tiles_of(Tq, S, Cfg::BM);
-  if (tiles * Hq > 0x7fffffff) return hipErrorInvalidConfiguration;
   const int runs = runs_of<T, D>(S, Tq, Tk, Hq, causal);
   float* parts = static_cast<float*>(workspace);
   PromptArgs a{Q, K, V, q_stride, k_stride, v_stride, cu_q, cu_k, Y, lse,
-               S, Tq, Tk, Hq, Hq / Hkv, causal, (int)tiles, scale * kLog2e, kLazy / (scale * kLog2e), parts,
+               S, Tq, Tk, Hq, Hq / Hkv, causal, (int)tiles, scale * kLog2e,
+               kLazy / (scale * kLog2e), parts,
                reinterpret_cast<int32_t*>(parts + 2 * (size_t)runs * part_floats(Cfg::BM, D)) + 4};
   const unsigned grid = (unsigned)(tiles * Hq), threads = 64 * Cfg::NW;
   if (runs == 0) {

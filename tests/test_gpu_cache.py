@@ -481,3 +481,25 @@ def test_equal_logits_of_any_size(fp4):
         Y = avq.cache_attention_fwd(Q, cache, table, lens, 16, 1.0, fp4=fp4).cpu()
         v = read_cache(t.cache, t.table, 0, n, F32, fp4, 16, 64)[1][0]
         assert ((Y[0, 0, 0].double() - v.mean(0)).abs() <= n * 2.0 ** -24 * 2 * v.abs().mean(0)).all()
+
+
+def test_the_most_tokens_of_one_call():
+    """2^24 packed tokens: their launch has more than one row of workgroups."""
+    lens, T, ps = [(1 << 24) - 100, 60, 40], 1 << 24, 64
+    K = torch.zeros(T, 1, 64, dtype=BF16, device="cuda")
+    V = torch.zeros(T, 1, 64, dtype=BF16, device="cuda")
+    K[-1000:], V[-1000:] = torch.randn(2, 1000, 1, 64, device="cuda").to(BF16)
+    c = torch.tensor([0, lens[0], T - 40, T], dtype=torch.int32, device="cuda")
+    start = torch.zeros(3, dtype=torch.int32, device="cuda")
+    table = torch.full((3, T // ps), -1, dtype=torch.int32)
+    first = (lens[0] - 500) // ps  # the long sequence: its last pages
+    table[0, first:(lens[0] + ps - 1) // ps] = torch.arange((lens[0] + ps - 1) // ps - first)
+    table[1, 0], table[2, 0] = 20, 21
+    table = table.cuda()
+    cache = torch.zeros(22, 1, avq.cache_page_bytes(BF16, ps, 64), dtype=torch.uint8, device="cuda")
+    avq.cache_append(K, V, cache, table, start, ps, cu=c)
+    K2, V2 = avq.cache_gather(cache, table, start, c, T, ps, BF16, 64)
+    n = lens[0] - first * ps + 100  # positions before them have no page and read as 0
+    for a, b in ((K, K2), (V, V2)):
+        assert torch.equal(a[-n:], b[-n:])
+        assert not b[:-n].any()

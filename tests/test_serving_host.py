@@ -64,6 +64,7 @@ CASES = {
         (dict(Q=ODD), INVALID), (dict(V=ODD), INVALID), (dict(lse=ODD), INVALID),
         (dict(cu_k=ODD), INVALID), (dict(ws=ODD), INVALID),
         (dict(Tk=1 << 20), INVALID), (dict(Tk=1 << 20, ws=FAKE, ws_bytes=1000), INVALID),
+        (dict(S=1 << 20, Hq=16, Hkv=16, qs=1024, ks=1024, vs=1024), UNSUPPORTED),
         (dict(Tq=0, Q=None, Y=None), OK)],
     append: HEADS + CACHE + [
         (dict(T=-1), INVALID), (dict(T=(1 << 24) + 1), UNSUPPORTED), (dict(cu=None), INVALID),
@@ -85,7 +86,8 @@ CASES = {
         (dict(Q=None), INVALID), (dict(cache=None), INVALID), (dict(lens=None), INVALID),
         (dict(table=None), INVALID), (dict(Y=None), INVALID), (dict(ws=None), INVALID),
         (dict(ws_bytes=64), INVALID), (dict(Y=ODD), INVALID), (dict(ws=ODD), INVALID),
-        (dict(S=1024, ps=256, max_pages=1 << 20), UNSUPPORTED)],
+        (dict(S=1024, ps=256, max_pages=1 << 20), UNSUPPORTED),
+        (dict(S=1 << 20, Hq=16, Hkv=16, qs=16 * 64), UNSUPPORTED)],
 }
 
 
@@ -118,11 +120,13 @@ def test_workspace_bytes(L):
     assert avq.prompt_attention_workspace(torch.bfloat16, 1, 300, 1 << 16, 4, 128) > 0
     assert avq.prompt_attention_workspace(torch.bfloat16, 1, 300, 300, 4, 128) == 0
     for bad in ((9, 1, 8, 8, 4, 64, 1), (BF16, 0, 8, 8, 4, 64, 1), (BF16, 1, -1, 8, 4, 64, 1),
-                (BF16, 1, 8, 8, 4, 96, 1), (BF16, 1, 8, 8, 4, 64, 2)):
+                (BF16, 1, 8, 8, 4, 96, 1), (BF16, 1, 8, 8, 4, 64, 2),
+                (BF16, 1 << 20, 8, 8, 16, 64, 1)):
         assert L.avq_prompt_attention_workspace(*bad) == -1
     small = avq.cache_attention_workspace(1, 1, 8, 8, 64)
     assert 0 < small < avq.cache_attention_workspace(4096, 16, 32, 8, 64)
-    for bad in ((0, 1, 8, 8, 64), (1, 17, 8, 8, 64), (1, 1, 8, 3, 64), (1, 1, 8, 8, 80)):
+    for bad in ((0, 1, 8, 8, 64), (1, 17, 8, 8, 64), (1, 1, 8, 3, 64), (1, 1, 8, 8, 80),
+                (1 << 20, 1, 16, 16, 64)):
         assert L.avq_cache_attention_workspace(*bad) == -1
 
 
