@@ -183,9 +183,11 @@ struct Runs {
 };
 
 // Positions of the 16-byte units of a staged row. Keys: 32 rows read one unit
-// each, so consecutive rows permute their units. Values: the transpose read
-// takes 32 bytes (a pair of units) of 4 consecutive keys per 16 lanes, so
-// those keys permute their pairs, and keys 4 apart swap halves of the row.
+// each, so consecutive rows permute their units. Values: 32 lanes of the
+// transpose read take 64 bytes (four units) of 4 consecutive keys, 256 bytes
+// and one pass over the 64 banks if these lie in different quarters: of 256
+// bytes, one row at d = 128 (permuting pairs of units instead leaves two keys
+// in one quarter: a third of the LDS cycles were conflicts) and two at d = 64.
 template <int U>
 __device__ __forceinline__ int key_swizzle(int r) {
   return U >= 16 ? r & 15 : (r >> 1) & 7;
@@ -193,7 +195,7 @@ __device__ __forceinline__ int key_swizzle(int r) {
 template <int U, bool kB>
 __device__ __forceinline__ int value_swizzle(int r) {
   if constexpr (!kB) return (r >> 2 & 1) << 3;
-  return ((r & 3) << 1) | (U >= 16 ? (r >> 2 & 1) << 3 : 0);
+  return U >= 16 ? (r & 3) << 2 : (r & 3) << 1;
 }
 
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc(const void* p) {
