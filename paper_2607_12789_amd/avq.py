@@ -340,7 +340,6 @@ def gilbert_order(width: int, height: int):
     return order, rank
 
 
-
 # ---- exact attention of packed prompts, and the paged cache ------------------
 
 
@@ -353,6 +352,10 @@ def _launch_stream(stream, device: torch.device) -> int:
                          + (f", the stream's {stream.device}" if stream is not None else ""))
     # the current stream's handle without a Stream object: 0.1 us instead of 2.6
     return torch._C._cuda_getCurrentRawStream(current) if stream is None else stream.cuda_stream
+
+
+def _elsewhere(t: Optional[torch.Tensor], at: int) -> bool:
+    return t is not None and t.get_device() != at
 
 
 def _same_device(ref: torch.Tensor, **tensors) -> None:
@@ -401,6 +404,10 @@ def prompt_attention_workspace(dtype, S: int, Tq: int, Tk: int, Hq: int, d: int,
     return n
 
 
+# Sizes only; the call costs as much as the checks of two tensors.
+_prompt_workspace_of = functools.lru_cache(maxsize=256)(prompt_attention_workspace)
+
+
 def prompt_attention_fwd(Q, K, V, cu_q, cu_k, scale: float, causal: bool = True, Y=None,
                          with_lse: bool = False, lse=None, workspace=None, stream=None):
     """Exact attention of packed sequences (``avq_prompt_attention_fwd``).
@@ -410,8 +417,8 @@ def prompt_attention_fwd(Q, K, V, cu_q, cu_k, scale: float, causal: bool = True,
     cu_k: int32 [S + 1] on the GPU. With ``causal`` the queries are the last
     ones of their sequence's keys. Rows behind the last sequence are left as
     they were. workspace: a uint8 tensor of ``prompt_attention_workspace(...)``
-    bytes (allocated if needed and not given). Returns Y [Tq, Hq, d], or (Y, lse) with ``with_lse`` (lse: fp32
-    [Tq, Hq]).
+    bytes (allocated if needed and not given). Returns Y [Tq, Hq, d], or
+    (Y, lse) with ``with_lse`` (lse: fp32 [Tq, Hq]).
     """
     q_stride = _rows(Q, "Q")
     Tq, Hq, d = Q.shape
@@ -427,23 +434,28 @@ def prompt_attention_fwd(Q, K, V, cu_q, cu_k, scale: float, causal: bool = True,
     s = _launch_stream(stream, Q.device)
     if Y is None:
         Y = _empty(stream, (Tq, Hq, d), Q.dtype, Q.device)
-    _dev(Y, "Y", Q.dtype, (Tq, Hq, d))
-    if with_lse and lse is None:
-        lse = _empty(stream, (Tq, Hq), torch.float32, Q.device)
+    else:
+        _dev(Y, "Y", Q.dtype, (Tq, Hq, d))
     if lse is not None:
         _dev(lse, "lse", torch.float32, (Tq, Hq))
+    elif with_lse:
+        lse = _empty(stream, (Tq, Hq), torch.float32, Q.device)
     S = cu_q.shape[0] - 1
-    if workspace is None:
-        n = prompt_attention_workspace(Q.dtype, S, Tq, Tk, Hq, d, causal)
-        if n:
-            workspace = _empty(stream, (n,), torch.uint8, Q.device)
     if workspace is not None:
         _dev(workspace, "workspace", torch.uint8)
-    _same_device(Q, K=K, V=V, cu_q=cu_q, cu_k=cu_k, Y=Y, lse=lse, workspace=workspace)
+    else:
+        n = _prompt_workspace_of(Q.dtype, S, Tq, Tk, Hq, d, bool(causal))
+        if n:
+            workspace = _empty(stream, (n,), torch.uint8, Q.device)
+    at = Q.get_device()
+    if (not K.get_device() == V.get_device() == cu_q.get_device() == cu_k.get_device()
+            == Y.get_device() == at or _elsewhere(lse, at) or _elsewhere(workspace, at)):
+        _same_device(Q, K=K, V=V, cu_q=cu_q, cu_k=cu_k, Y=Y, lse=lse, workspace=workspace)
     _check(lib().avq_prompt_attention_fwd(
         _dtype_code(Q), S, Tq, Tk, Hq, Hkv, d, float(scale), int(bool(causal)),
         Q.data_ptr(), q_stride, K.data_ptr(), k_stride, V.data_ptr(), v_stride, cu_q.data_ptr(),
-        cu_k.data_ptr(), Y.data_ptr(), _ptr(lse), _ptr(workspace), 0 if workspace is None else workspace.numel(), s))
+        cu_k.data_ptr(), Y.data_ptr(), _ptr(lse), _ptr(workspace),
+        0 if workspace is None else workspace.numel(), s))
     return (Y, lse) if with_lse else Y
 
 
@@ -526,15 +538,20 @@ def cache_append(K, V, cache, block_table, start, page_size: int, cu=None, Q=Non
             raise ValueError(f"Q must have {T} tokens, got {Q.shape[0]}")
         if Q_out is None:
             Q_out = _empty(stream, (T, Hq, d), Q.dtype, Q.device)
-        _dev(Q_out, "Q_out", Q.dtype, (T, Hq, d))
+        else:
+            _dev(Q_out, "Q_out", Q.dtype, (T, Hq, d))
     elif Q_out is not None:
         raise ValueError("Q_out without Q")
-    if K_out is None and with_K:
-        K_out = _empty(stream, (T, Hkv, d), K.dtype, K.device)
     if K_out is not None:
         _dev(K_out, "K_out", K.dtype, (T, Hkv, d))
-    _same_device(K, V=V, cache=cache, block_table=block_table, start=start, cu=cu, Q=Q, cos=cos,
-                 sin=sin, Q_out=Q_out, K_out=K_out)
+    elif with_K:
+        K_out = _empty(stream, (T, Hkv, d), K.dtype, K.device)
+    at = K.get_device()
+    if (not V.get_device() == cache.get_device() == block_table.get_device() == start.get_device()
+            == at or _elsewhere(cu, at) or _elsewhere(Q, at) or _elsewhere(Q_out, at)
+            or _elsewhere(cos, at) or _elsewhere(sin, at) or _elsewhere(K_out, at)):
+        _same_device(K, V=V, cache=cache, block_table=block_table, start=start, cu=cu, Q=Q,
+                     cos=cos, sin=sin, Q_out=Q_out, K_out=K_out)
     _check(lib().avq_cache_append(
         _dtype_code(K), int(bool(fp4)), S, T, Hq, Hkv, d, n_pages, page_size, max_pages, rot, n_pos,
         int(bool(interleaved)), _ptr(Q), q_stride, K.data_ptr(), k_stride, V.data_ptr(), v_stride,
@@ -553,11 +570,15 @@ def cache_gather(cache, block_table, start, cu, T: int, page_size: int, dtype, d
     s = _launch_stream(stream, cache.device)
     if K is None:
         K = _empty(stream, (T, Hkv, d), dtype, cache.device)
+    else:
+        _dev(K, "K", dtype, (T, Hkv, d))
     if V is None:
         V = _empty(stream, (T, Hkv, d), dtype, cache.device)
-    _dev(K, "K", dtype, (T, Hkv, d))
-    _dev(V, "V", dtype, (T, Hkv, d))
-    _same_device(cache, block_table=block_table, start=start, cu=cu, K=K, V=V)
+    else:
+        _dev(V, "V", dtype, (T, Hkv, d))
+    if not (block_table.get_device() == start.get_device() == cu.get_device() == K.get_device()
+            == V.get_device() == cache.get_device()):
+        _same_device(cache, block_table=block_table, start=start, cu=cu, K=K, V=V)
     _check(lib().avq_cache_gather(
         _DTYPES[dtype], int(bool(fp4)), S, T, Hkv, d, n_pages, page_size, max_pages,
         cache.data_ptr(), cu.data_ptr(), start.data_ptr(), block_table.data_ptr(), K.data_ptr(),
@@ -603,16 +624,21 @@ def cache_attention_fwd(Q, cache, block_table, lens, page_size: int, scale: floa
     s = _launch_stream(stream, Q.device)
     if Y is None:
         Y = _empty(stream, (S, n_q, Hq, d), Q.dtype, Q.device)
-    _dev(Y, "Y", Q.dtype, (S, n_q, Hq, d))
-    if with_lse and lse is None:
-        lse = _empty(stream, (S, n_q, Hq), torch.float32, Q.device)
+    else:
+        _dev(Y, "Y", Q.dtype, (S, n_q, Hq, d))
     if lse is not None:
         _dev(lse, "lse", torch.float32, (S, n_q, Hq))
+    elif with_lse:
+        lse = _empty(stream, (S, n_q, Hq), torch.float32, Q.device)
     if workspace is None:
         workspace = _empty(stream, (_cache_workspace_of(S, n_q, Hq, Hkv, d),), torch.uint8, Q.device)
-    _dev(workspace, "workspace", torch.uint8)
-    _same_device(Q, cache=cache, block_table=block_table, lens=lens, Y=Y, lse=lse,
-                 workspace=workspace)
+    else:
+        _dev(workspace, "workspace", torch.uint8)
+    at = Q.get_device()
+    if (not cache.get_device() == block_table.get_device() == lens.get_device() == Y.get_device()
+            == workspace.get_device() == at or _elsewhere(lse, at)):
+        _same_device(Q, cache=cache, block_table=block_table, lens=lens, Y=Y, lse=lse,
+                     workspace=workspace)
     _check(lib().avq_cache_attention_fwd(
         _dtype_code(Q), int(bool(fp4)), S, n_q, Hq, Hkv, d, n_pages, page_size, max_pages,
         float(scale), Q.data_ptr(), q_stride, cache.data_ptr(), lens.data_ptr(),
