@@ -503,3 +503,68 @@ def test_the_most_tokens_of_one_call():
     for a, b in ((K, K2), (V, V2)):
         assert torch.equal(a[-n:], b[-n:])
         assert not b[:-n].any()
+
+
+@pytest.mark.parametrize("dtype,fp4", [(BF16, True), (BF16, False), (F32, True)])
+def test_shared_pages(dtype, fp4):
+    """Sequences that read the same pages (a common prompt), and one that names
+    a page twice."""
+    lens, ps = [200, 230, 96], 32
+    t = Setup(lens, [0] * 3, 2, 2, 64, dtype, fp4, ps)
+    cache, _, n = fill(t)
+    t.table[1, :5] = t.table[0, :5]
+    t.table[2, 2] = t.table[2, 0]
+    Q = torch.randn(3, 2, 4, 64, generator=torch.Generator().manual_seed(3)).to(dtype)
+    table = t.table.cuda()
+    Y, lse = avq.cache_attention_fwd(Q.cuda(), cache, table, n, ps, 0.3, fp4=fp4, with_lse=True)
+    check_cached(Y.cpu(), lse.cpu(), Q, t, lens, 0.3)
+    K, V = avq.cache_gather(cache, table, torch.zeros_like(n), cu(lens).cuda(), sum(lens), ps, dtype,
+                            64, fp4=fp4)
+    assert torch.equal(K[:160], K[200:360]) and torch.equal(V[:160], V[200:360])
+    assert torch.equal(K[430:462], K[494:526]) and torch.equal(V[430:462], V[494:526])
+
+
+@pytest.mark.parametrize("Hq,n_q,fp4", [(1024, 16, True), (1024, 1, False), (31, 11, True)])
+def test_many_rows_per_head(Hq, n_q, fp4):
+    lens = [700, 20]
+    t = Setup(lens, [0, 0], 1, 1, 128, BF16, fp4, 64)
+    cache, table, n = fill(t)
+    Q = torch.randn(2, n_q, Hq, 128, generator=torch.Generator().manual_seed(3)).to(BF16)
+    Y, lse = avq.cache_attention_fwd(Q.cuda(), cache, table, n, 64, 0.1, fp4=fp4, with_lse=True)
+    Y, lse = Y.cpu(), lse.cpu()
+    for s in range(2):
+        K, V, _ = read_cache(t.cache, t.table, s, lens[s], BF16, fp4, 64, 128)
+        seen = (torch.arange(n_q) + lens[s] - n_q + 1).clamp(0, lens[s]).repeat_interleave(Hq)
+        check_attention(Y[s].reshape(-1, 128), lse[s].reshape(-1), Q[s].reshape(-1, 128), K[0], V[0],
+                        0.1, seen)
+
+
+def test_two_streams_at_once():
+    """Calls on two streams, each with its own workspace, over one cache."""
+    lens, ps = [3000, 500, 64], 64
+    t = Setup(lens, [0] * 3, 2, 2, 128, BF16, True, ps)
+    cache, table, n = fill(t)
+    g = torch.Generator().manual_seed(3)
+    Q = [torch.randn(3, 4, 8, 128, generator=g).to(BF16).cuda() for _ in range(2)]
+    P = [torch.randn(300, 8, 128, generator=g).to(BF16).cuda() for _ in range(2)]
+    c, ck = cu([100, 150, 50]).cuda(), cu(lens).cuda()
+
+    def work(i):
+        y = avq.cache_attention_fwd(Q[i], cache, table, n, ps, 0.1, fp4=True)
+        k, v = avq.cache_gather(cache, table, torch.zeros_like(n), ck, sum(lens), ps, BF16, 128,
+                                fp4=True)
+        return y, k, v, avq.prompt_attention_fwd(P[i], k, v, c, ck, 0.1)
+
+    assert avq.prompt_attention_workspace(BF16, 3, 300, sum(lens), 8, 128) == 0
+    want = [work(i) for i in range(2)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(10):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i].append(work(i))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for r in got[i]:
+            assert all(torch.equal(a, b) for a, b in zip(r, want[i]))

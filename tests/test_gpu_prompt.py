@@ -300,3 +300,20 @@ def test_one_huge_key_among_ordinary_ones(n, dtype):
     rest = torch.arange(n) != 200
     check_attention(Y[2:, 0], lse[2:, 0], Q[2:, 0], K[rest, 0], V[rest, 0], 0.125,
                     seen_of(32, n - 1, False))
+
+
+def test_equal_runs_on_two_streams_at_once():
+    d, Lk = 128, 6000
+    sets = [[x.cuda() for x in make([200], [Lk], 8, 2, d, BF16, s)] for s in range(2)]
+    c, ck = cu([200]), cu([Lk])
+    assert avq.prompt_attention_workspace(BF16, 1, 200, Lk, 8, d) > 0
+    want = [avq.prompt_attention_fwd(*x, c, ck, 0.1) for x in sets]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(10):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i].append(avq.prompt_attention_fwd(*sets[i], c, ck, 0.1))
+    torch.cuda.synchronize()
+    assert all(torch.equal(y, want[i]) for i in range(2) for y in got[i])
