@@ -509,7 +509,9 @@ avq_status_t avq_cache_gather(avq_dtype_t dtype, avq_cache_t format, int32_t S, 
 
 /* Bytes of the workspace of avq_cache_attention_fwd (-1 for unsupported
  * sizes). Its contents need not be set and mean nothing afterwards; calls that
- * may run at the same time need one each. */
+ * may run at the same time need one each. A cache with room for few positions
+ * per sequence (max_pages * page_size <= AVQ_CACHE_UNDIVIDED) needs none. */
+enum { AVQ_CACHE_UNDIVIDED = 512 };
 int64_t avq_cache_attention_workspace(int32_t S, int32_t n_q, int32_t Hq, int32_t Hkv, int32_t d);
 
 /*
@@ -528,9 +530,10 @@ int64_t avq_cache_attention_workspace(int32_t S, int32_t n_q, int32_t Hq, int32_
  *   Q            [S * n_q] rows of [Hq][d], dtype, q_stride as above
  *   cache, block_table  as above; lens [S] int32
  *   Y            [S][n_q][Hq][d] dtype, out;  lse [S][n_q][Hq] fp32, nullable
- *   workspace    avq_cache_attention_workspace() bytes
- * Two launches (one where no sequence can hold more than 512 positions). What
- * lies in cache slots behind a sequence's length has no effect, whatever it is.
+ *   workspace    avq_cache_attention_workspace() bytes; NULL allowed (it is
+ *                not used) if max_pages * page_size <= AVQ_CACHE_UNDIVIDED
+ * Two launches, one where no workspace is needed. What lies in cache slots
+ * behind a sequence's length has no effect, whatever it is.
  */
 avq_status_t avq_cache_attention_fwd(avq_dtype_t dtype, avq_cache_t format, int32_t S, int32_t n_q,
                                      int32_t Hq, int32_t Hkv, int32_t d, int32_t n_pages,

@@ -31,6 +31,7 @@ SYMBOLS = ("avq_version", "avq_last_error", "avq_packed_bytes", "avq_assign",
            "avq_prompt_attention_workspace",
            "avq_cache_page_bytes", "avq_cache_append", "avq_cache_gather",
            "avq_cache_attention_workspace", "avq_cache_attention_fwd")
+CACHE_UNDIVIDED = 512  # positions of cached sequences whose keys are not divided
 IMPORTANCE_TILE = 64  # parents per codeword tile of attention_fwd(tiled_importance=True)
 
 
@@ -605,8 +606,9 @@ def cache_attention_fwd(Q, cache, block_table, lens, page_size: int, scale: floa
 
     Q [S, n_q, Hq, d]; lens int32 [S]: cached positions, the n_q tokens' own
     among them. workspace: a uint8 tensor of ``cache_attention_workspace(...)``
-    bytes (allocated if not given). Returns Y [S, n_q, Hq, d], or (Y, lse) with
-    ``with_lse`` (lse: fp32 [S, n_q, Hq]).
+    bytes (allocated if needed and not given; a cache with room for at most
+    ``CACHE_UNDIVIDED`` positions per sequence needs none). Returns Y
+    [S, n_q, Hq, d], or (Y, lse) with ``with_lse`` (lse: fp32 [S, n_q, Hq]).
     """
     if not isinstance(Q, torch.Tensor) or not Q.is_cuda:
         raise ValueError("Q must be a tensor on the GPU")
@@ -630,17 +632,20 @@ def cache_attention_fwd(Q, cache, block_table, lens, page_size: int, scale: floa
         _dev(lse, "lse", torch.float32, (S, n_q, Hq))
     elif with_lse:
         lse = _empty(stream, (S, n_q, Hq), torch.float32, Q.device)
-    if workspace is None:
-        workspace = _empty(stream, (_cache_workspace_of(S, n_q, Hq, Hkv, d),), torch.uint8, Q.device)
-    else:
+    if workspace is not None:
         _dev(workspace, "workspace", torch.uint8)
+    else:
+        n = _cache_workspace_of(S, n_q, Hq, Hkv, d)  # refuses unsupported sizes
+        if max_pages * page_size > CACHE_UNDIVIDED:
+            workspace = _empty(stream, (n,), torch.uint8, Q.device)
     at = Q.get_device()
     if (not cache.get_device() == block_table.get_device() == lens.get_device() == Y.get_device()
-            == workspace.get_device() == at or _elsewhere(lse, at)):
+            == at or _elsewhere(workspace, at) or _elsewhere(lse, at)):
         _same_device(Q, cache=cache, block_table=block_table, lens=lens, Y=Y, lse=lse,
                      workspace=workspace)
     _check(lib().avq_cache_attention_fwd(
         _dtype_code(Q), int(bool(fp4)), S, n_q, Hq, Hkv, d, n_pages, page_size, max_pages,
         float(scale), Q.data_ptr(), q_stride, cache.data_ptr(), lens.data_ptr(),
-        block_table.data_ptr(), Y.data_ptr(), _ptr(lse), workspace.data_ptr(), workspace.numel(), s))
+        block_table.data_ptr(), Y.data_ptr(), _ptr(lse), _ptr(workspace),
+        0 if workspace is None else workspace.numel(), s))
     return (Y, lse) if with_lse else Y

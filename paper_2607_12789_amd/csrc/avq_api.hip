@@ -542,11 +542,13 @@ avq_status_t avq_cache_attention_fwd(avq_dtype_t dtype, avq_cache_t format, int3
                 Hq, Hkv);
   if ((int64_t)S * (((int64_t)max_pages * page_size + 127) / 128) > (1LL << 30))
     return fail(AVQ_ERR_UNSUPPORTED, "%s: S * max_pages * page_size: at most 2^37 positions", name);
-  if (!Q || !cache || !lens || !block_table || !Y || !workspace) return null_pointer(name);
+  const bool divided = (int64_t)max_pages * page_size > AVQ_CACHE_UNDIVIDED;
+  if (!Q || !cache || !lens || !block_table || !Y || (divided && !workspace))
+    return null_pointer(name);
   if (!aligned16(Q) || !aligned16(cache) || !aligned16(lens) || !aligned16(block_table) ||
       !aligned16(Y) || !aligned16(lse) || !aligned16(workspace))
     return misaligned(name);
-  const int64_t need = avq_cache_attention_workspace(S, n_q, Hq, Hkv, d);
+  const int64_t need = workspace ? avq_cache_attention_workspace(S, n_q, Hq, Hkv, d) : 0;
   if (workspace_bytes < need)
     return fail(AVQ_ERR_INVALID_ARG, "%s: workspace of %lld bytes, %lld are needed", name,
                 (long long)workspace_bytes, (long long)need);

@@ -25,6 +25,7 @@
 // a part leaves its running max, sum and numerator in the workspace, and a
 // second launch joins the parts. At most a run's first and last segment are
 // parts, so two slots per workgroup hold them.
+#include "../../include/avq.h"
 #include "avq_cache.hpp"
 #include "avq_launch.hpp"
 
@@ -40,7 +41,8 @@ constexpr int kWaves = kThreads / kWave;
 constexpr int kRows = 16;                  // query rows per MFMA tile
 constexpr int kStep = 32;                  // keys per wave and step
 constexpr int kUnit = kStep * kWaves;      // keys per step of a workgroup
-constexpr int kWholeSteps = 4;             // steps of sequences that are not divided
+// steps of sequences that are not divided
+constexpr int kWholeSteps = AVQ_CACHE_UNDIVIDED / kUnit;
 constexpr int kMaxWorkgroups = 1024;       // slots in the workspace
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kLazy = 8.f;         // log2 units the running max may lag behind
@@ -54,7 +56,8 @@ struct CacheAttnArgs {
   void* Y;
   float* lse;           // nullable
   float* parts;         // [workgroups][2] of part_floats(D): see there
-  int32_t* joins;       // [segments][2]: first workgroup and its slot, parts
+  int32_t* joins;       // [segments][2]: first workgroup and its slot, parts;
+                        // null where no segment is divided
   int S, n_q, Hq, G, row_tiles;
   int unit;  // keys per unit, a multiple of kUnit
   float scale_log2;
@@ -475,7 +478,7 @@ void cache_attention_kernel(CacheAttnArgs a) {
     const long long seg = (long long)s * heads + hr;
     const int slot = u == u_first ? 0 : 1;
     const bool whole = x == 0 && x_end == n_units;
-    if (tid == 0 && x == 0) {
+    if (tid == 0 && x == 0 && a.joins) {
       // the workgroup that holds unit v is ((v + 1) W - 1) / U
       const long long w_last = ((u + n_units) * W - 1) / U;
       a.joins[2 * seg] = 2 * w + slot;
@@ -620,6 +623,7 @@ hipError_t launch_tiles(CacheAttnArgs& a, hipStream_t stream) {
       (((long long)a.cache.max_pages << a.cache.ps_log2) + kUnit - 1) / kUnit;
   a.unit = kUnit * (room <= kWholeSteps ? (int)room : 1);
   const long long cap = room <= kWholeSteps ? 1 : room;  // units of a segment, at most
+  if (cap == 1) a.joins = nullptr;
   // as many workgroups as run at once: one more would start when the first
   // ends, after as long again
   DeviceInfo dev;

@@ -568,3 +568,17 @@ def test_two_streams_at_once():
     for i in range(2):
         for r in got[i]:
             assert all(torch.equal(a, b) for a, b in zip(r, want[i]))
+
+
+def test_undivided_needs_no_workspace():
+    """Up to 512 positions of room: no workspace, and the same result with one."""
+    lens, ps = [512, 3, 400], 16
+    t = Setup(lens, [0] * 3, 2, 2, 64, BF16, True, ps)
+    cache, table, n = fill(t)
+    assert table.shape[1] * ps == avq.CACHE_UNDIVIDED
+    Q = torch.randn(3, 2, 4, 64, generator=torch.Generator().manual_seed(3)).to(BF16).cuda()
+    Y = avq.cache_attention_fwd(Q, cache, table, n, ps, 0.3, fp4=True)
+    check_cached(Y.cpu(), None, Q.cpu(), t, lens, 0.3)
+    ws = torch.zeros(avq.cache_attention_workspace(3, 2, 4, 2, 64), dtype=torch.uint8, device="cuda")
+    assert torch.equal(Y, avq.cache_attention_fwd(Q, cache, table, n, ps, 0.3, fp4=True, workspace=ws))
+    assert not ws.any()

@@ -84,7 +84,8 @@ CASES = {
         (dict(n_q=0), INVALID), (dict(n_q=17), UNSUPPORTED), (dict(Hq=3), INVALID),
         (dict(scale=0.0), INVALID), (dict(scale=NAN), INVALID), (dict(qs=100), INVALID),
         (dict(Q=None), INVALID), (dict(cache=None), INVALID), (dict(lens=None), INVALID),
-        (dict(table=None), INVALID), (dict(Y=None), INVALID), (dict(ws=None), INVALID),
+        (dict(table=None), INVALID), (dict(Y=None), INVALID),
+        (dict(ws=None, max_pages=33), INVALID),
         (dict(ws_bytes=64), INVALID), (dict(Y=ODD), INVALID), (dict(ws=ODD), INVALID),
         (dict(S=1024, ps=256, max_pages=1 << 20), UNSUPPORTED),
         (dict(S=1 << 20, Hq=16, Hkv=16, qs=16 * 64), UNSUPPORTED)],
