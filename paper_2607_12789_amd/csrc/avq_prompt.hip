@@ -602,14 +602,20 @@ long long tiles_of(long long Tq, int S, int BM) { return Tq / BM + S; }
 // 8192 tokens and 8 heads 188 / 170, 4096 and 16 98 / 100, 6144 and 16 173 /
 // 190, 2048 and 32 53 / 68, 1024 and 8 25 / 27, chunks of 512 and 300 behind
 // 15872 and 4001 300 / 118 (d = 64: 219 / 76); fp32, d = 64, 2048 and 8 146 / 52.
-// fp32's products alone fill the matrix units: one run per CU, half the parts.
+// fp32's products alone nearly fill the matrix units: one run per CU and half the
+// parts, but two where a run is then still 16 key tiles long (by the mean
+// lengths). Measured, us one / two: 1024 tokens and 16 heads 60 / 65, 2048 and 8
+// 95 / 96, 4096 and 16 587 / 560 (d = 64: 318 / 295), 56 queries of three
+// sequences behind 10848 keys, 42 heads 174 / 120.
 template <typename T, int D>
 int runs_of(int S, int Tq, int Tk, int Hq, int causal) {
   using Cfg = PromptCfg<T, D>;
   const long long tiles = tiles_of(Tq, S, Cfg::BM) * Hq, full = causal ? 1024 : 512;
   const long long excess = (full - tiles) * (Tk / S) / full;
   if (excess < (Cfg::kB ? 2500 : 250)) return 0;
-  return Cfg::kB ? 768 : 256;
+  if (Cfg::kB) return 768;
+  const long long units = tiles * (Tk - (causal ? Tq / 2 : 0)) / S / Cfg::BN;
+  return units < 512 * 16 ? 256 : 512;
 }
 
 }  // namespace
