@@ -74,6 +74,14 @@ __device__ __forceinline__ int units_of(int len, int unit) {
   return max(1, (len + unit - 1) / unit);
 }
 
+// x y, rounded before anything is subtracted from it: fused with the running
+// max it would leave the max's own rounding error in the exponent, which for
+// logits beyond 2^31 no weight can hold.
+__device__ __forceinline__ float product_of(float x, float y) {
+#pragma clang fp contract(off)
+  return x * y;
+}
+
 // A part: numerators [rows][D], then maxima [rows] and sums [rows].
 __host__ __device__ constexpr size_t part_floats(int rows, int D) { return (size_t)rows * (D + 2); }
 
@@ -126,8 +134,8 @@ void cache_attention_kernel(CacheAttnArgs a) {
   constexpr int KQ = kB ? D / 32 : D / 4;  // k-steps of the logit product
   using QFrag = typename std::conditional<kB, bf16x8, float>::type;
 
-  __shared__ int s_units[kThreads];      // units of the sequences before thread i's
   __shared__ int s_wave[kWaves];
+  __shared__ int s_first[3];             // where the run starts
   __shared__ float s_m[kWaves][kRows], s_l[kWaves][kRows];
   __shared__ __attribute__((aligned(16))) float s_o[kWaves][kRows][D + 4];
 
@@ -135,12 +143,15 @@ void cache_attention_kernel(CacheAttnArgs a) {
   const int g = lane / 16, c = lane % 16;
   const int w = blockIdx.x;
 
-  // ---- units before each thread's run of sequences -------------------------
+  // ---- units of each thread's sequences, and before them -------------------
   const int per = (a.S + kThreads - 1) / kThreads;
-  int mine = 0;
+  int mine = 0, mine_len = 0;  // mine_len: length of the first
   for (int i = 0; i < per; ++i) {
     const int s = tid * per + i;
-    if (s < a.S) mine += units_of(length_of(a, s), a.unit);
+    if (s >= a.S) break;
+    const int n = length_of(a, s);
+    if (i == 0) mine_len = n;
+    mine += units_of(n, a.unit);
   }
   const int incl = wave_incl_scan(mine);
   if (lane == kWave - 1) s_wave[wave] = incl;
@@ -150,8 +161,6 @@ void cache_attention_kernel(CacheAttnArgs a) {
     if (i < wave) before += s_wave[i];
     total += s_wave[i];
   }
-  s_units[tid] = before + incl - mine;
-  __syncthreads();
 
   const int heads = a.cache.Hkv * a.row_tiles;
   const long long U = (long long)total * heads;
@@ -161,15 +170,14 @@ void cache_attention_kernel(CacheAttnArgs a) {
   const long long u_end = U * (w + 1) / W;
   const long long u_first = u;
 
-  // head and sequence of the run's first unit
+  // head and sequence of the run's first unit, from the thread whose sequences
+  // hold it (every sequence has a unit)
   int hr = (int)(u / total);
-  int x = (int)(u % total);
-  int t = 0;  // the last thread whose sequences start at or before x
-  for (int step = kThreads / 2; step > 0; step /= 2)
-    if (t + step < kThreads && s_units[t + step] <= x) t += step;
-  int s = t * per;
-  x -= s_units[t];
-  int len = length_of(a, s), n_units = units_of(len, a.unit);
+  int x = (int)(u % total) - (before + incl - mine);
+  if (x >= 0 && x < mine) s_first[0] = tid * per, s_first[1] = x, s_first[2] = mine_len;
+  __syncthreads();
+  int s = s_first[0], len = s_first[2], n_units = units_of(len, a.unit);
+  x = s_first[1];
   while (x >= n_units && s + 1 < a.S) {
     x -= n_units;
     ++s;
@@ -340,7 +348,7 @@ void cache_attention_kernel(CacheAttnArgs a) {
       for (int n = 0; n < NT; ++n) {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-          p[n][i] = scaled_less(sc[n][i / 4][i % 4], a.scale_log2, 0.f);
+          p[n][i] = product_of(sc[n][i / 4][i % 4], a.scale_log2);
         if (masked) {
 #pragma unroll
           for (int i = 0; i < 8; ++i)

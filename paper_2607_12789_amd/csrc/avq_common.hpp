@@ -145,13 +145,6 @@ __device__ __forceinline__ float exp_neg(float x) {
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float log2_hw(float x) { return __builtin_amdgcn_logf(x); }
 
-// x y - z with the product rounded, not fused.
-__device__ __forceinline__ float scaled_less(float x, float y, float z) {
-#pragma clang fp contract(off)
-  const float p = x * y;
-  return p - z;
-}
-
 template <typename T>
 __device__ __forceinline__ float to_f32(T v) { return (float)v; }
 
