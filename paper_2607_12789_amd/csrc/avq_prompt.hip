@@ -594,14 +594,23 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a) {
 long long tiles_of(long long Tq, int S, int BM) { return Tq / BM + S; }
 
 // Equal runs (workgroups), or 0 for whole tiles. With whole tiles the longest
-// tile's chain of keys bounds the time; with runs it is the mean work, which is
-// tiles / 1024 of it under the causal mask (tiles / 512 without one, two tiles
-// per CU), and the parts: 15 to 20 us for writing and joining them. So runs are
-// taken where the chain exceeds the mean by enough keys, the sequences' mean
-// length standing for all. Measured, us whole / runs (d = 128): one sequence of
-// 8192 tokens and 8 heads 188 / 170, 4096 and 16 98 / 100, 6144 and 16 173 /
-// 190, 2048 and 32 53 / 68, 1024 and 8 25 / 27, chunks of 512 and 300 behind
-// 15872 and 4001 300 / 118 (d = 64: 219 / 76); fp32, d = 64, 2048 and 8 146 / 52.
+// tile's chain of keys bounds the time; with runs it is the mean work, and the
+// parts, which are written and joined. So runs are taken where the chain exceeds
+// the mean by enough keys, the sequences' mean lengths standing for all.
+// * More tiles than CUs share these, so the chain is slower: the mean is tiles /
+//   1024 of it under the causal mask (tiles / 512 without one), the parts cost 15
+//   to 20 us. Measured, us whole / runs (d = 128): one sequence of 8192 tokens and
+//   8 heads 188 / 170, 4096 and 16 98 / 100, 6144 and 16 173 / 190, 2048 and 32
+//   53 / 68; fp32, d = 64, 2048 and 8 146 / 52, 256 and 16 22 / 19, and without a
+//   mask 1024 and 32 79 / 86.
+// * bf16 tiles with a CU each (0.6 us per 32 keys of a chain, 0.5 per unit of a
+//   CU): a run has 256 keys at least, and the parts cost by their rows: 7 us up to
+//   4096 rows, 20 up to 32768, 28 for all 768 runs. Measured, us whole / runs:
+//   32 queries behind 992 keys, 4, 16, 32 heads 23 / 15, 22 / 17, 22 / 20; 128
+//   behind 896 25 / 17, 25 / 25, 25 / 30; 128 behind 1920 44 / 18, 44 / 29, 44 /
+//   31; a prompt of 2048, 4 and 16 heads 44 / 37, 45 / 50, of 1024, 8 heads 25 /
+//   27; chunks of 512 and 300 behind 15872 and 4001, 16 heads 300 / 118 (d = 64:
+//   219 / 76).
 // fp32's products alone nearly fill the matrix units: one run per CU and half the
 // parts, but two where a run is then still 16 key tiles long (by the mean
 // lengths). Measured, us one / two: 1024 tokens and 16 heads 60 / 65, 2048 and 8
@@ -612,8 +621,17 @@ int runs_of(int S, int Tq, int Tk, int Hq, int causal) {
   using Cfg = PromptCfg<T, D>;
   const long long tiles = tiles_of(Tq, S, Cfg::BM) * Hq, full = causal ? 1024 : 512;
   const long long excess = (full - tiles) * (Tk / S) / full;
-  if (excess < (Cfg::kB ? 2500 : 250)) return 0;
-  if (Cfg::kB) return 768;
+  if (Cfg::kB) {
+    constexpr int kRuns = 768;
+    const long long Lq = std::max(1, Tq / S), Lk = Tk / S;  // mean lengths
+    const long long own = (Lq + Cfg::BM - 1) / Cfg::BM * S * Hq;
+    if (own > 256) return excess < 2500 ? 0 : kRuns;
+    const long long keys = own * (Lk - (causal ? std::min(Lq, Lk) / 2 : 0));
+    const long long mean = std::max(256LL, keys * 5 / 6 / 256);
+    const long long rows = std::min(keys / 256, (long long)kRuns) * std::min<long long>(Lq, Cfg::BM);
+    return Lk - mean < (rows <= 4096 ? 450 : rows <= 32768 ? 1100 : 1600) ? 0 : kRuns;
+  }
+  if (excess < (causal ? 200 : 600)) return 0;
   const long long units = tiles * (Tk - (causal ? Tq / 2 : 0)) / S / Cfg::BN;
   return units < 512 * 16 ? 256 : 512;
 }

@@ -317,3 +317,16 @@ def test_equal_runs_on_two_streams_at_once():
                 got[i].append(avq.prompt_attention_fwd(*sets[i], c, ck, 0.1))
     torch.cuda.synchronize()
     assert all(torch.equal(y, want[i]) for i in range(2) for y in got[i])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("lens_q,lens_k,Hq", [([32], [1024], 4), ([31, 75, 9], [357, 2209, 125], 4),
+                                              ([130, 1, 0], [2000, 1500, 1700], 6)])
+def test_parts_of_few_tiles(lens_q, lens_k, Hq, d, dtype):
+    """Tiles of few rows, in a few runs of one tile each or less."""
+    Q, K, V = make(lens_q, lens_k, Hq, 2, d, dtype, 21)
+    n = avq.prompt_attention_workspace(dtype, len(lens_q), sum(lens_q), sum(lens_k), Hq, d)
+    assert n > 0
+    Y, lse = run(Q, K, V, lens_q, lens_k, 1 / math.sqrt(d), True)
+    check_prompt(Y, lse, Q, K, V, lens_q, lens_k, 1 / math.sqrt(d), True)
