@@ -95,8 +95,10 @@ struct PromptCfg {
 // part leaves its numerators, maxima and sums, and a second launch joins the
 // parts. At most a run's first and last tile are parts.
 
-// A part: numerators [BM][D], maxima [BM], sums [BM]; run i has parts 2 i and
-// 2 i + 1.
+// A part: numerators, maxima [BM], sums [BM]; run i has parts 2 i and 2 i + 1.
+// The numerators lie as the lanes hold them, so that every store and load of a
+// wave covers 1 KB: piece q = 4 i + j of wave w, [w][q][64 lanes][4], are the
+// columns 32 i + 8 j + 4 (lane / 32) + 0 .. 3 of row 32 w + lane % 32.
 __host__ __device__ constexpr size_t part_floats(int BM, int D) { return (size_t)BM * (D + 2); }
 
 struct Tile {
@@ -412,7 +414,7 @@ __device__ __forceinline__ void attend(const PromptArgs& a, const Tile& tile, in
       for (int i = 0; i < DT; ++i)
 #pragma unroll
         for (int r = 0; r < 16; r += 4)
-          *reinterpret_cast<f32x4*>(part + r0 * D + 32 * i + 2 * r + 4 * h) =
+          *reinterpret_cast<f32x4*>(part + ((wave * (D / 8) + 4 * i + r / 4) * kWave + lane) * 4) =
               f32x4{o[i][r], o[i][r + 1], o[i][r + 2], o[i][r + 3]};
     }
     return;
@@ -545,13 +547,12 @@ void prompt_runs_kernel(PromptArgs a) {
   }
 }
 
-// Joins the parts of a tile's rows (D / 4 threads per row, 4 columns each): the
+// Joins the parts of a tile's rows (one piece of 4 columns per thread): the
 // first part is the one that joins names, the others are the first ones of the
 // runs that follow.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a) {
   constexpr int BM = PromptCfg<T, D>::BM;
-  constexpr int TPR = D / 4, RPW = 256 / TPR;  // threads per row, rows per workgroup
   const int tile = blockIdx.x / a.Hq, hq = blockIdx.x % a.Hq;
   Tile t;  // tile qa / BM + s + lt; ids that belong to none have no entry in joins
   t.s = find_sequence(a.S, tile, threadIdx.x % kWave, [&](int k) {
@@ -563,7 +564,9 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a) {
   if (a.joins[-1] == 0) return;
   const int first = a.joins[2 * (size_t)blockIdx.x], n = a.joins[2 * (size_t)blockIdx.x + 1];
   if (n == 1) return;
-  const int r = blockIdx.y * RPW + threadIdx.x / TPR, d0 = threadIdx.x % TPR * 4;
+  const int piece = blockIdx.y * 256 + threadIdx.x, q = piece / kWave % (D / 8);
+  const int r = 32 * (piece / kWave / (D / 8)) + piece % 32;
+  const int d0 = 8 * q + 4 * (piece % kWave / 32);
   const int row = t.lt * BM + r;
   if (row >= t.Lq) return;
   auto part = [&](int i) {
@@ -578,7 +581,7 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a) {
     const float* p = part(i);
     const float f = exp2_hw(p[BM * D + r] - m);
     l = fmaf(f, p[BM * D + BM + r], l);
-    acc += f * *reinterpret_cast<const f32x4*>(p + r * D + d0);
+    acc += f * *reinterpret_cast<const f32x4*>(p + 4 * piece);
   }
   const float inv = l > 0.f ? 1.f / l : 0.f;
   const size_t at = (size_t)(t.qa + row) * a.Hq + hq;
@@ -605,10 +608,10 @@ long long tiles_of(long long Tq, int S, int BM) { return Tq / BM + S; }
 //   mask 1024 and 32 79 / 86.
 // * bf16 tiles with a CU each (0.6 us per 32 keys of a chain, 0.5 per unit of a
 //   CU): a run has 256 keys at least, and the parts cost by their rows: 7 us up to
-//   4096 rows, 20 up to 32768, 28 for all 768 runs. Measured, us whole / runs:
-//   32 queries behind 992 keys, 4, 16, 32 heads 23 / 15, 22 / 17, 22 / 20; 128
-//   behind 896 25 / 17, 25 / 25, 25 / 30; 128 behind 1920 44 / 18, 44 / 29, 44 /
-//   31; a prompt of 2048, 4 and 16 heads 44 / 37, 45 / 50, of 1024, 8 heads 25 /
+//   4096 rows, 12 to 18 up to 32768, 25 for all 768 runs. Measured, us whole /
+//   runs: 32 queries behind 992 keys, 4, 16, 32 heads 23 / 15, 22 / 16, 22 / 19;
+//   128 behind 896 25 / 16, 25 / 23, 25 / 27; 128 behind 1920 44 / 17, 44 / 25, 44
+//   / 29; a prompt of 2048, 4 and 16 heads 44 / 33, 45 / 47, of 1024, 8 heads 25 /
 //   27; chunks of 512 and 300 behind 15872 and 4001, 16 heads 300 / 118 (d = 64:
 //   219 / 76).
 // fp32's products alone nearly fill the matrix units: one run per CU and half the
