@@ -486,11 +486,13 @@ void prompt_runs_kernel(PromptArgs a) {
   const int incl = wave_incl_scan(mine);
   const int per_head = last_lane(incl);
   const long long U = (long long)per_head * a.Hq;
-  // each run has kLeast units at least; consecutive runs on one XCD, so that it
-  // takes consecutive heads, which share keys
+  // each run has kLeast units at least; consecutive runs on one XCD (workgroup i
+  // runs on XCD i % 8), so that it takes consecutive heads, which share keys, and
+  // every XCD has its share of the runs there are
   const int W = (int)min((long long)gridDim.x, (U + Cfg::kLeast - 1) / Cfg::kLeast);
-  const int w = xcd_remap(blockIdx.x, gridDim.x);
-  if (w >= W) return;
+  if ((int)blockIdx.x >= W) return;
+  const int xcd = blockIdx.x % 8;
+  const int w = xcd * (W / 8) + min(xcd, W % 8) + blockIdx.x / 8;
   long long u = U * w / W;
   const long long u_first = u, u_end = U * (w + 1) / W;
 
@@ -607,13 +609,13 @@ long long tiles_of(long long Tq, int S, int BM) { return Tq / BM + S; }
 //   53 / 68; fp32, d = 64, 2048 and 8 146 / 52, 256 and 16 22 / 19, and without a
 //   mask 1024 and 32 79 / 86.
 // * bf16 tiles with a CU each (0.6 us per 32 keys of a chain, 0.5 per unit of a
-//   CU): a run has 256 keys at least, and the parts cost by their rows: 7 us up to
-//   4096 rows, 12 to 18 up to 32768, 25 for all 768 runs. Measured, us whole /
-//   runs: 32 queries behind 992 keys, 4, 16, 32 heads 23 / 15, 22 / 16, 22 / 19;
-//   128 behind 896 25 / 16, 25 / 23, 25 / 27; 128 behind 1920 44 / 17, 44 / 25, 44
-//   / 29; a prompt of 2048, 4 and 16 heads 44 / 33, 45 / 47, of 1024, 8 heads 25 /
-//   27; chunks of 512 and 300 behind 15872 and 4001, 16 heads 300 / 118 (d = 64:
-//   219 / 76).
+//   CU): a run has 256 keys at least, and a second launch and the parts cost by
+//   their rows: as much as 500 keys up to 16384 rows, 900 up to 32768, 1250 for
+//   all 768 runs. Measured, us whole / runs (d = 128): 32 queries behind 992 keys,
+//   4, 16, 32 heads 23 / 15, 22 / 15, 22 / 15; behind 480 13 / 13 each; 128 behind
+//   896 25 / 16, 25 / 18, 25 / 20; 128 behind 1920 43 / 16, 44 / 19, 44 / 25; a
+//   prompt of 2048, 4 and 16 heads 44 / 29, 45 / 45, of 1024 25 / 21, 25 / 31;
+//   chunks of 512 and 300 behind 15872 and 4001, 16 heads 300 / 116.
 // fp32's products alone nearly fill the matrix units: one run per CU and half the
 // parts, but two where a run is then still 16 key tiles long (by the mean
 // lengths). Measured, us one / two: 1024 tokens and 16 heads 60 / 65, 2048 and 8
@@ -632,7 +634,10 @@ int runs_of(int S, int Tq, int Tk, int Hq, int causal) {
     const long long keys = own * (Lk - (causal ? std::min(Lq, Lk) / 2 : 0));
     const long long mean = std::max(256LL, keys * 5 / 6 / 256);
     const long long rows = std::min(keys / 256, (long long)kRuns) * std::min<long long>(Lq, Cfg::BM);
-    return Lk - mean < (rows <= 4096 ? 450 : rows <= 32768 ? 1100 : 1600) ? 0 : kRuns;
+    if (Lk - mean < (rows <= 16384 ? 500 : rows <= 32768 ? 900 : 1250)) return 0;
+    // room for twice the runs that the mean lengths give (ragged tiles): 64 runs'
+    // parts are 8 MB, those of 768 100 MB
+    return (int)std::min<long long>(kRuns, (keys / 128 + 63) / 64 * 64);
   }
   if (excess < (causal ? 200 : 600)) return 0;
   const long long units = tiles * (Tk - (causal ? Tq / 2 : 0)) / S / Cfg::BN;

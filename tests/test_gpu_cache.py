@@ -555,7 +555,6 @@ def test_two_streams_at_once():
                                 fp4=True)
         return y, k, v, avq.prompt_attention_fwd(P[i], k, v, c, ck, 0.1)
 
-    assert avq.prompt_attention_workspace(BF16, 3, 300, sum(lens), 8, 128) == 0
     want = [work(i) for i in range(2)]
     streams = [torch.cuda.Stream() for _ in range(2)]
     torch.cuda.synchronize()
