@@ -495,7 +495,7 @@ avq_status_t avq_cache_append(avq_dtype_t dtype, avq_cache_t format, int32_t S, 
 /*
  * avq_cache_gather - cached positions read back as packed rows: row cu[s] + i
  * is position start[s] + i of sequence s, in dtype (4-bit values are exact in
- * either type). With start = 0 and cu the cached lengths these are the K and V
+ * either type). Positions below 0 read as 0, as those without a page. With start = 0 and cu the cached lengths these are the K and V
  * that avq_prompt_attention_fwd takes for a chunk behind a cached prefix.
  *
  *   cu           [S + 1], start [S], block_table [S][max_pages]: int32

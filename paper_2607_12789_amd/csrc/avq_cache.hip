@@ -56,8 +56,21 @@ struct AppendArgs {
   int row_blocks;        // workgroups for queries and keys; the others take values
 };
 
+// A position that no table reaches and no angles cover (both hold fewer than
+// 2^31): it stands for all beyond it.
+constexpr int kNoPlace = 0x7fffffff;
+
+// Tokens that the cache holds before the call's (start[s]). A negative number:
+// -1, the sequence takes no part, or with kAll its positions have no page.
+template <bool kAll>
+__device__ __forceinline__ int start_of(const TokenArgs& a, int s) {
+  const int p = a.start[s];
+  return p >= 0 ? p : kAll ? kNoPlace : -1;
+}
+
 // Sequence and position of packed token t, the same for the whole wave (-1: of
 // no sequence).
+template <bool kAll>
 __device__ __forceinline__ int place(const TokenArgs& a, int t, int lane, int& pos) {
   int s = t, i = 0;
   if (a.cu) {
@@ -67,9 +80,9 @@ __device__ __forceinline__ int place(const TokenArgs& a, int t, int lane, int& p
     if (t < b || t >= e) return -1;
     i = t - b;
   }
-  const int p0 = a.start[s];
-  if (p0 < 0 || p0 > 0x7fffffff - i) return -1;
-  pos = p0 + i;
+  const int p0 = start_of<kAll>(a, s);
+  if (p0 < 0) return -1;
+  pos = p0 + min(i, kNoPlace - p0);
   return s;
 }
 
@@ -141,7 +154,7 @@ __device__ __forceinline__ void append_rows(const AppendArgs& a) {
   if (t >= a.tok.T) return;
   const int first = wave % a.groups * a.steps;
   int pos = 0;
-  const int s = place(a.tok, t, lane, pos);
+  const int s = place<false>(a.tok, t, lane, pos);
   if (s < 0 || (a.rot && pos >= a.n_pos)) return;
   const int u = lane % LPR, hl = lane / LPR;
   const int half = a.rot / 2;
@@ -224,13 +237,14 @@ __device__ __forceinline__ void append_rows(const AppendArgs& a) {
 // An octet of positions of one sequence, and which of its positions are among
 // the call's tokens.
 struct Octet {
-  int s, pos0, t0;  // sequence, first position, packed row of that position
+  int s, pos0, t0;  // sequence, first position (at most kNoPlace), its packed row
   unsigned mask;    // bit j: position pos0 + j is a token of this call
 };
+template <bool kAll>
 __device__ __forceinline__ Octet find_octet(const TokenArgs& a, long long slot, int lane) {
   Octet o;
   o.mask = 0;
-  int b, e, p0;
+  int b, e;
   long long first = 0;
   if (a.cu) {
     o.s = find_sequence(a.S, slot, lane, [&](int s) {
@@ -244,12 +258,12 @@ __device__ __forceinline__ Octet find_octet(const TokenArgs& a, long long slot, 
     e = b + 1;
     first = slot;
   }
-  p0 = a.start[o.s];
-  if (p0 < 0 || p0 > 0x7fffffff - (e - b) - 8) return o;
-  const long long k = p0 / 8 + (slot - first);
-  if (k * 8 >= (long long)p0 + (e - b)) return o;
-  o.pos0 = (int)(k * 8);
-  o.t0 = b + (o.pos0 - p0);
+  const int p0 = start_of<kAll>(a, o.s);
+  if (p0 < 0) return o;
+  const long long pos0 = (p0 / 8 + (slot - first)) * 8;
+  if (pos0 >= (long long)p0 + (e - b)) return o;
+  o.pos0 = (int)min(pos0, (long long)kNoPlace);
+  o.t0 = (int)(b + (pos0 - p0));
 #pragma unroll
   for (int j = 0; j < 8; ++j)
     if (o.t0 + j >= b && o.t0 + j < e) o.mask |= 1u << j;
@@ -271,12 +285,12 @@ __device__ __forceinline__ void append_values(const AppendArgs& a) {
   const long long slot = wave / HG;
   if (slot >= slots_of(a.tok)) return;
   const int u = lane % LPR, h = (int)(wave % HG) * HPS + lane / LPR;
-  const Octet o = find_octet(a.tok, slot, lane);
+  const Octet o = find_octet<false>(a.tok, slot, lane);
   unsigned mask = o.mask;
   if (a.rot && mask) {  // positions past the table are not written
 #pragma unroll
     for (int j = 0; j < 8; ++j)
-      if (o.pos0 + j >= a.n_pos) mask &= ~(1u << j);
+      if (o.pos0 >= a.n_pos - j) mask &= ~(1u << j);
   }
   if (mask == 0 || h >= Hkv) return;
   const PageLayout L = page_layout(FP4, sizeof(T), 1 << a.cache.ps_log2, D);
@@ -400,7 +414,7 @@ __device__ __forceinline__ void gather_keys(const GatherArgs& a) {
     out[k] = Chunk<T>{};
     dst[k] = nullptr;
     int pos = 0, s = -1;
-    if (k < a.steps * a.tokens && t < a.tok.T) s = place(a.tok, t, lane, pos);
+    if (k < a.steps * a.tokens && t < a.tok.T) s = place<true>(a.tok, t, lane, pos);
     if (s >= 0 && h < Hkv) {
       dst[k] = static_cast<T*>(a.K) + ((size_t)t * Hkv + h) * D + 8 * u;
       const unsigned char* src = page_of(a.cache, L.bytes, s, pos, h);
@@ -440,7 +454,7 @@ __device__ __forceinline__ void gather_values(const GatherArgs& a) {
   const long long slot = wave / HG;
   if (slot >= slots_of(a.tok)) return;
   const int u = lane % LPR, h = (int)(wave % HG) * HPS + lane / LPR;
-  const Octet o = find_octet(a.tok, slot, lane);
+  const Octet o = find_octet<true>(a.tok, slot, lane);
   if (o.mask == 0 || h >= Hkv) return;
   const PageLayout L = page_layout(FP4, sizeof(T), 1 << a.cache.ps_log2, D);
   const unsigned char* page = page_of(a.cache, L.bytes, o.s, o.pos0, h);

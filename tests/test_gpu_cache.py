@@ -581,3 +581,38 @@ def test_undivided_needs_no_workspace():
     ws = torch.zeros(avq.cache_attention_workspace(3, 2, 4, 2, 64), dtype=torch.uint8, device="cuda")
     assert torch.equal(Y, avq.cache_attention_fwd(Q, cache, table, n, ps, 0.3, fp4=True, workspace=ws))
     assert not ws.any()
+
+
+@pytest.mark.parametrize("fp4", [False, True])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_gathered_starts_without_a_place(dtype, fp4):
+    """Keys and values of positions that no page can hold (before 0, past the
+    table, past 2^31) both read as 0; positions with a page beside them are read."""
+    ps, d, lens = 16, 64, [40, 24, 9, 30, 17]
+    t = Setup(lens, [0] * 5, 2, 2, d, dtype, fp4, ps)
+    t.append()
+    top = (1 << 31) - 1
+    start = torch.tensor([0, -1, top - 3, -(1 << 31), top - 24], dtype=torch.int32)
+    K = torch.full((sum(lens) + 3, 2, d), 5.0, dtype=dtype, device="cuda")
+    V = K.clone()
+    avq.cache_gather(t.cache.cuda(), t.table.cuda(), start.cuda(), cu(lens).cuda(), len(K), ps, dtype,
+                     d, fp4=fp4, K=K, V=V)
+    k, v, _ = read_cache(t.cache, t.table, 0, lens[0], dtype, fp4, ps, d)
+    for got, x in ((K, k), (V, v)):
+        assert torch.equal(got[:40].cpu().double(), x.transpose(0, 1))
+        assert (got[40:-3] == 0).all() and (got[-3:] == 5).all()
+
+
+def test_appended_starts_without_a_place():
+    """Tokens past 2^31 have no page, but their queries and keys are given out
+    like those of any position without one; a negative start takes no part."""
+    top, d = (1 << 31) - 1, 64
+    t = Setup([20, 20, 5], [0, 0, 0], 2, 2, d, BF16, True, 16)
+    t.start = torch.tensor([top - 7, -1, 0], dtype=torch.int32)
+    Qo, Ko = (torch.full((45, 2, d), 3.0, dtype=BF16, device="cuda") for _ in range(2))
+    t.append(Q_out=Qo, K_out=Ko)
+    for got, x in ((Qo.cpu(), t.Q), (Ko.cpu(), t.K)):
+        assert torch.equal(got[:20], x[:20]) and torch.equal(got[40:], x[40:])
+        assert (got[20:40] == 3).all()
+    changed = (t.cache != t.before).flatten(1).any(1).nonzero().flatten().tolist()
+    assert set(changed) <= {int(t.table[2, 0])}
