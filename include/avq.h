@@ -388,6 +388,9 @@ avq_status_t avq_codebook_update(avq_dtype_t dtype, int32_t B, int32_t H, int32_
  * packed tokens, 0 included (nothing is then written). Element counts may pass
  * 2^31. An infinity or NaN in a sequence's inputs leaves the outputs of other
  * sequences as they are; the sequence's own are unspecified.
+ * The attentions need |q_i . k_j| and |S_ij| log2(e) below 3e38, and values below
+ * 2^120 / n in magnitude for n keys: numerators are fp32 sums of values times
+ * weights of at most 2^8.
  */
 
 /* Bytes of the workspace of avq_prompt_attention_fwd for these sizes: 0 where
@@ -441,7 +444,8 @@ enum { AVQ_CACHE_NATIVE = 0, AVQ_CACHE_FP4 = 1 };
  *           A code byte holds dimensions 2i (low 4 bits) and 2i+1 of one
  *           position as e2m1: sign, then 0, 0.5, 1, 1.5, 2, 3, 4, 6 for codes
  *           0 .. 7. A scale byte e in 1 .. 254 is 2^(e - 127), shared by 32
- *           dimensions of one position: 4.25 bits per element.
+ *           dimensions of one position: 4.25 bits per element. Magnitudes above
+ *           3.5 2^126 (2.97e38) become code 4 at 2^126, which is 2^128.
  * block_table [S][max_pages] (int32, device) names the page of positions
  * i*page_size .. (i+1)*page_size - 1 of each sequence in column i; columns past
  * a sequence's length are not read. A position without a page (past max_pages,
@@ -495,8 +499,10 @@ avq_status_t avq_cache_append(avq_dtype_t dtype, avq_cache_t format, int32_t S, 
 /*
  * avq_cache_gather - cached positions read back as packed rows: row cu[s] + i
  * is position start[s] + i of sequence s, in dtype (4-bit values are exact in
- * either type). Positions below 0 read as 0, as those without a page. With start = 0 and cu the cached lengths these are the K and V
- * that avq_prompt_attention_fwd takes for a chunk behind a cached prefix.
+ * either type, but 2^128 is read as the type's largest finite value). Positions
+ * below 0 read as 0, like those without a page. With start = 0 and cu the cached
+ * lengths these are the K and V that avq_prompt_attention_fwd takes for a chunk
+ * behind a cached prefix.
  *
  *   cu           [S + 1], start [S], block_table [S][max_pages]: int32
  *   K, V         [T][Hkv][d] dtype, contiguous, out

@@ -616,3 +616,21 @@ def test_appended_starts_without_a_place():
         assert (got[20:40] == 3).all()
     changed = (t.cache != t.before).flatten(1).any(1).nonzero().flatten().tolist()
     assert set(changed) <= {int(t.table[2, 0])}
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_the_largest_values_in_4_bits_are_read_as_finite(dtype):
+    """Magnitudes above 3.5 2^126 take code 4 at a scale of 2^126, which is
+    2^128: read as the largest finite value."""
+    d, top = 64, torch.finfo(dtype).max
+    x = torch.zeros(16, 1, d, dtype=dtype)
+    x[0], x[1], x[2, 0, 5], x[2, 0, 6] = 3.0e38, -3.0e38, top, -2.0e38
+    x[3], x[4, 0, 33] = 2.9e38, 2.0 ** 127
+    cache = torch.zeros(1, 1, avq.cache_page_bytes(dtype, 16, d, True), dtype=torch.uint8).cuda()
+    table, start = torch.zeros(1, 1, dtype=torch.int32).cuda(), torch.zeros(1, dtype=torch.int32).cuda()
+    avq.cache_append(x.cuda(), x.cuda(), cache, table, start, 16, cu=cu([16]).cuda(), fp4=True)
+    k64 = read_cache(cache.cpu(), table.cpu(), 0, 16, dtype, True, 16, d)[0].transpose(0, 1)
+    assert (k64.abs() == 2.0 ** 128).sum() == 2 * d + 1  # rows 0 and 1, and one of row 2
+    for y in avq.cache_gather(cache, table, start, cu([16]).cuda(), 16, 16, dtype, d, fp4=True):
+        assert torch.isfinite(y).all()
+        assert torch.equal(y.cpu().double(), k64.clamp(-top, top))
