@@ -411,7 +411,7 @@ int64_t avq_prompt_attention_workspace(avq_dtype_t dtype, int32_t S, int32_t Tq,
  * earlier keys when Lq < Lk). A query that sees no key (Lk = 0, or causal with
  * Lq > Lk + i) gets Y_i = 0 and lse_i = -inf.
  *
- *   scale  > 0, finite;  causal  0 or 1
+ *   scale  > 0, scale log2(e) finite in fp32 (2.35e38);  causal  0 or 1
  *   Q      [Tq] rows of [Hq][d], K, V [Tk] rows of [Hkv][d], dtype
  *   cu_q, cu_k  [S + 1] int32 (they may be one array)
  *   Y      [Tq][Hq][d] dtype, contiguous, out
@@ -532,7 +532,7 @@ int64_t avq_cache_attention_workspace(int32_t S, int32_t n_q, int32_t Hq, int32_
  * max_pages * page_size; S * max_pages * page_size <= 2^37 and
  * S * Hkv * ceil(n_q * Hq / Hkv / 16) < 2^24.
  *
- *   n_q          1 .. 16
+ *   n_q          1 .. 16;  scale  as in avq_prompt_attention_fwd
  *   Q            [S * n_q] rows of [Hq][d], dtype, q_stride as above
  *   cache, block_table  as above; lens [S] int32
  *   Y            [S][n_q][Hq][d] dtype, out;  lse [S][n_q][Hq] fp32, nullable

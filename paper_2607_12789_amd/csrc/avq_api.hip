@@ -1,6 +1,7 @@
 // C ABI of the AVQ-Attention forward pass: argument validation on the host,
 // then dispatch to the gfx950 kernels. Nothing here allocates device memory or
 // synchronises; no exception crosses the boundary.
+#include <float.h>
 #include <stdarg.h>
 #include <stdio.h>
 
@@ -356,8 +357,10 @@ avq_status_t check_stride(const char* name, const char* what, avq_dtype_t dtype,
 }
 
 avq_status_t check_scale(const char* name, float scale) {
-  if (!(scale > 0.f && scale <= 3.0e38f))
-    return fail(AVQ_ERR_INVALID_ARG, "%s: scale=%g must be positive and finite", name, (double)scale);
+  // the kernels multiply by scale log2(e): infinite, it would make 0 logits NaN
+  if (!(scale > 0.f && scale * avq::kLog2e <= FLT_MAX))
+    return fail(AVQ_ERR_INVALID_ARG, "%s: scale=%g must be positive, and finite times log2(e)", name,
+                (double)scale);
   return AVQ_OK;
 }
 

@@ -161,3 +161,11 @@ def test_binding_refuses_another_device(monkeypatch):
     a, b = SimpleNamespace(device=dev), SimpleNamespace(device=torch.device("cuda", 0))
     with pytest.raises(ValueError):
         avq._same_device(a, other=b)
+
+
+@pytest.mark.parametrize("fn", [prompt, cached])
+@pytest.mark.parametrize("scale", [2.4e38, 2.9e38])
+def test_scales_that_overflow_are_refused(L, fn, scale):
+    """scale log2(e), by which the kernels multiply, has to be finite."""
+    assert fn(L, scale=scale) == INVALID
+    assert "scale" in L.avq_last_error().decode()
