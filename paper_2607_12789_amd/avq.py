@@ -351,8 +351,14 @@ def _launch_stream(stream, device: torch.device) -> int:
     if device.index != current or (stream is not None and stream.device != device):
         raise ValueError(f"tensors on {device}: the current device is cuda:{current}"
                          + (f", the stream's {stream.device}" if stream is not None else ""))
-    # the current stream's handle without a Stream object: 0.1 us instead of 2.6
-    return torch._C._cuda_getCurrentRawStream(current) if stream is None else stream.cuda_stream
+    if stream is None:
+        # the current stream's handle without a Stream object (0.1 us instead of
+        # 2.6) where this torch gives it out
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        if raw is not None:
+            return raw(current)
+        stream = torch.cuda.current_stream()
+    return stream.cuda_stream
 
 
 def _elsewhere(t: Optional[torch.Tensor], at: int) -> bool:

@@ -169,3 +169,11 @@ def test_scales_that_overflow_are_refused(L, fn, scale):
     """scale log2(e), by which the kernels multiply, has to be finite."""
     assert fn(L, scale=scale) == INVALID
     assert "scale" in L.avq_last_error().decode()
+
+
+def test_binding_without_the_raw_stream(monkeypatch):
+    """A torch that does not give out the raw handle: the public Stream's."""
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.delattr(torch._C, "_cuda_getCurrentRawStream", raising=False)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda: SimpleNamespace(cuda_stream=55))
+    assert avq._launch_stream(None, torch.device("cuda", 0)) == 55
