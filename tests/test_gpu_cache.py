@@ -634,3 +634,76 @@ def test_the_largest_values_in_4_bits_are_read_as_finite(dtype):
     for y in avq.cache_gather(cache, table, start, cu([16]).cuda(), 16, 16, dtype, d, fp4=True):
         assert torch.isfinite(y).all()
         assert torch.equal(y.cpu().double(), k64.clamp(-top, top))
+
+
+@pytest.mark.parametrize("bad", [math.inf, math.nan])
+@pytest.mark.parametrize("dtype,fp4", [(BF16, False), (BF16, True), (F32, False), (F32, True)])
+def test_bad_values_stay_in_their_sequence(bad, dtype, fp4):
+    """Infinities and NaN in one sequence's queries, keys and values, where
+    workgroups go from one sequence to the next and leave parts (1248
+    units of 128 keys): the others' results keep their bits."""
+    lens, ps, Hkv, d = [2900, 300, 1500, 3], 64, 32, 64
+    t = Setup(lens, [0] * 4, Hkv, Hkv, d, dtype, fp4, ps)
+    assert t.table.shape[1] * ps > avq.CACHE_UNDIVIDED
+    cache, table, n = fill(t)
+    Q = torch.randn(4, 4, 2 * Hkv, d, generator=torch.Generator().manual_seed(3)).to(dtype).cuda()
+    want = avq.cache_attention_fwd(Q, cache, table, n, ps, 0.1, fp4=fp4, with_lse=True)
+    t.K[2900:3200] = t.V[2900:3200] = bad
+    t.cache = t.before
+    cache, table, n = fill(t)
+    if fp4:  # in 4 bits the codes hold neither: scales of 2^128, infinite in both types
+        for p in t.table[1, :4].tolist():
+            cache[p, :, ps * d:] = 0xff
+    Q[1] = bad
+    got = avq.cache_attention_fwd(Q, cache, table, n, ps, 0.1, fp4=fp4, with_lse=True)
+    for a, b in zip(got, want):
+        for s in (0, 2, 3):
+            assert torch.equal(a[s], b[s]), f"sequence {s}"
+
+
+@pytest.mark.parametrize("fp4", [False, True])
+def test_many_sequences_in_parts(fp4):
+    """More sequences than threads of a workgroup (several per thread), among
+    them long ones whose keys are divided."""
+    S, ps, far = 600, 64, {0: 1500, 255: 700, 256: 2000, 511: 3, 599: 1100}
+    lens = [far.get(s, s % 90) for s in range(S)]
+    t = Setup(lens, [0] * S, 2, 2, 64, BF16, fp4, ps)
+    assert t.table.shape[1] * ps > avq.CACHE_UNDIVIDED
+    cache, table, n = fill(t)
+    Q = torch.randn(S, 2, 6, 64, generator=torch.Generator().manual_seed(3)).to(BF16)
+    Y, lse = avq.cache_attention_fwd(Q.cuda(), cache, table, n, ps, 0.3, fp4=fp4, with_lse=True)
+    check_cached(Y.cpu(), lse.cpu(), Q, t, lens, 0.3, rows=set(far) | {1, 2, 90, 254, 257, 598})
+
+
+@pytest.mark.parametrize("dtype,fp4", [(BF16, False), (BF16, True), (F32, True)])
+def test_drafted_tokens_after_a_prompt(dtype, fp4):
+    """Drafted tokens as a server tries them: a prompt is appended, then rounds
+    of n_q tokens per sequence (append with cu, attention of the rotated
+    queries), of which some are kept: the next round's start overwrites the
+    rest."""
+    S, Hq, Hkv, d, ps, scale, n_q = 3, 4, 2, 64, 16, 0.25, 4
+    g = torch.Generator().manual_seed(17)
+    done, kept = [600, 14, 0], [[1, 4, 2], [3, 2, 4], [4, 1, 1]]
+    table, n_pages = tables([n + 4 * n_q for n in done], ps)
+    cache = garbage(n_pages, Hkv, avq.cache_page_bytes(dtype, ps, d, fp4)).cuda()
+    cos, sin = (x.cuda() for x in angles(700, d))
+    table_d = table.cuda()
+    K, V = (torch.randn(sum(done), Hkv, d, generator=g).to(dtype).cuda() for _ in range(2))
+    avq.cache_append(K, V, cache, table_d, torch.zeros(S, dtype=torch.int32).cuda(), ps,
+                     cu=cu(done).cuda(), cos=cos, sin=sin, fp4=fp4)
+    for keep in kept:
+        Q, K, V = (torch.randn(S * n_q, h, d, generator=g).to(dtype).cuda() for h in (Hq, Hkv, Hkv))
+        start = torch.tensor(done, dtype=torch.int32).cuda()
+        Qr, _ = avq.cache_append(K, V, cache, table_d, start, ps, cu=cu([n_q] * S).cuda(), Q=Q,
+                                 cos=cos, sin=sin, fp4=fp4)
+        pos = torch.cat([torch.arange(o, o + n_q) for o in done])
+        want, err = rotate64(Q.cpu(), pos, cos.cpu(), sin.cpu(), False)
+        assert ((Qr.cpu().double() - want).abs() <= HALF_STEP[dtype] * want.abs() + 1.01 * err).all()
+        lens = [n + n_q for n in done]
+        Y, lse = avq.cache_attention_fwd(Qr.view(S, n_q, Hq, d), cache, table_d, start + n_q, ps, scale,
+                                         fp4=fp4, with_lse=True)
+        rows = [read_cache(cache.cpu(), table, s, lens[s], dtype, fp4, ps, d) for s in range(S)]
+        check_prompt(Y.flatten(0, 1).cpu(), lse.flatten(0, 1).cpu(), Qr.cpu(),
+                     torch.cat([r[0].transpose(0, 1) for r in rows]),
+                     torch.cat([r[1].transpose(0, 1) for r in rows]), [n_q] * S, lens, scale, True)
+        done = [a + b for a, b in zip(done, keep)]

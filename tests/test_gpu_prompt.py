@@ -330,3 +330,19 @@ def test_parts_of_few_tiles(lens_q, lens_k, Hq, d, dtype):
     assert n > 0
     Y, lse = run(Q, K, V, lens_q, lens_k, 1 / math.sqrt(d), True)
     check_prompt(Y, lse, Q, K, V, lens_q, lens_k, 1 / math.sqrt(d), True)
+
+
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("d,Hq", [(64, 4), (128, 16)])
+def test_bad_values_stay_in_their_sequence_in_parts(d, Hq, dtype, bad):
+    """The same where workgroups go from one sequence's tiles to the next and
+    leave parts that a second launch joins."""
+    lens_q, lens_k = [130, 5, 40], [3100, 2700, 4000]
+    assert avq.prompt_attention_workspace(dtype, 3, sum(lens_q), sum(lens_k), Hq, d, True) > 0
+    Q, K, V = make(lens_q, lens_k, Hq, 2, d, dtype, 9)
+    want = run(Q, K, V, lens_q, lens_k, 0.3, True)
+    Q[130:135], K[3100:5800], V[3100:5800] = bad, bad, bad
+    Y, lse = run(Q, K, V, lens_q, lens_k, 0.3, True)
+    for a, b in ((0, 130), (135, 175)):
+        assert torch.equal(Y[a:b], want[0][a:b]) and torch.equal(lse[a:b], want[1][a:b])
