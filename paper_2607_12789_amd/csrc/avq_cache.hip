@@ -382,14 +382,23 @@ struct GatherArgs {
   int tokens;                     // per wave
 };
 
-// Two decoded values of byte B of w. The one code that neither type holds, 4 at
-// a scale of 2^126 (2^128), becomes the type's largest finite value.
-template <typename T, int B>
+// two decoded values of byte B of w
+template <int B>
 __device__ __forceinline__ void decode2(uint32_t w, float scale, float& a, float& b) {
-  constexpr float kTop = Elem<T>::kBf16 ? 0x1.fep127f : 0x1.fffffep127f;
   const auto v = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, B);
-  a = __builtin_amdgcn_fmed3f(v[0], -kTop, kTop);
-  b = __builtin_amdgcn_fmed3f(v[1], -kTop, kTop);
+  a = v[0];
+  b = v[1];
+}
+// The one decoded value that neither type holds, 4 at a scale of 2^126 (2^128),
+// becomes the type's largest finite one. In a branch: 4945 tokens of 6 heads of
+// 64 take 6.5 us, 7.3 with every value clamped.
+template <typename T>
+__device__ __forceinline__ void saturate(float scale, float (&x)[8]) {
+  constexpr float kTop = Elem<T>::kBf16 ? 0x1.fep127f : 0x1.fffffep127f;
+  if (__any(scale >= 0x1p126f)) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = __builtin_amdgcn_fmed3f(x[i], -kTop, kTop);
+  }
 }
 __device__ __forceinline__ float scale_of(uint32_t w, int byte) {
   return __uint_as_float((w >> (8 * byte) & 0xffu) << 23);
@@ -436,10 +445,11 @@ __device__ __forceinline__ void gather_keys(const GatherArgs& a) {
     if constexpr (FP4) {
       float x[8];
       const float sc = scale_of(scale[k], 0);
-      decode2<T, 0>(code[k], sc, x[0], x[1]);
-      decode2<T, 1>(code[k], sc, x[2], x[3]);
-      decode2<T, 2>(code[k], sc, x[4], x[5]);
-      decode2<T, 3>(code[k], sc, x[6], x[7]);
+      decode2<0>(code[k], sc, x[0], x[1]);
+      decode2<1>(code[k], sc, x[2], x[3]);
+      decode2<2>(code[k], sc, x[4], x[5]);
+      decode2<3>(code[k], sc, x[6], x[7]);
+      saturate<T>(sc, x);
       out[k].set(x);
     }
     if (dst[k]) out[k].store(dst[k]);
@@ -479,11 +489,12 @@ __device__ __forceinline__ void gather_values(const GatherArgs& a) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const uint32_t c = code[i][j / 4];
-        if (j % 4 == 0) decode2<T, 0>(c, scale, x[2 * i], x[2 * i + 1]);
-        if (j % 4 == 1) decode2<T, 1>(c, scale, x[2 * i], x[2 * i + 1]);
-        if (j % 4 == 2) decode2<T, 2>(c, scale, x[2 * i], x[2 * i + 1]);
-        if (j % 4 == 3) decode2<T, 3>(c, scale, x[2 * i], x[2 * i + 1]);
+        if (j % 4 == 0) decode2<0>(c, scale, x[2 * i], x[2 * i + 1]);
+        if (j % 4 == 1) decode2<1>(c, scale, x[2 * i], x[2 * i + 1]);
+        if (j % 4 == 2) decode2<2>(c, scale, x[2 * i], x[2 * i + 1]);
+        if (j % 4 == 3) decode2<3>(c, scale, x[2 * i], x[2 * i + 1]);
       }
+      saturate<T>(scale, x);
       Chunk<T> out;
       out.set(x);
       if (o.mask >> j & 1) out.store(dst + (o.t0 + j) * stride);
