@@ -394,9 +394,10 @@ avq_status_t avq_codebook_update(avq_dtype_t dtype, int32_t B, int32_t H, int32_
  */
 
 /* Bytes of the workspace of avq_prompt_attention_fwd for these sizes: 0 where
- * it needs none (enough query tiles to fill the device), -1 for unsupported
- * sizes. Its contents need not be set and mean nothing afterwards; calls that
- * may run at the same time need one each. */
+ * it needs none (no query tile's keys are divided: enough tiles to fill the
+ * device, or too few keys), -1 for unsupported sizes. Its contents need not be
+ * set and mean nothing afterwards; calls that may run at the same time need one
+ * each. */
 int64_t avq_prompt_attention_workspace(avq_dtype_t dtype, int32_t S, int32_t Tq, int32_t Tk,
                                        int32_t Hq, int32_t d, int32_t causal);
 

@@ -404,6 +404,8 @@ void cache_attention_kernel(CacheAttnArgs a) {
           }
         }
       }
+      // bf16: the matrix product takes the weights rounded to bf16 (by at most
+      // half a step, 2^-8; their sum l is of the unrounded ones)
       if constexpr (kB) {
         bf16x8 pb[NT];
 #pragma unroll
