@@ -445,8 +445,9 @@ enum { AVQ_CACHE_NATIVE = 0, AVQ_CACHE_FP4 = 1 };
  *           A code byte holds dimensions 2i (low 4 bits) and 2i+1 of one
  *           position as e2m1: sign, then 0, 0.5, 1, 1.5, 2, 3, 4, 6 for codes
  *           0 .. 7. A scale byte e in 1 .. 254 is 2^(e - 127), shared by 32
- *           dimensions of one position: 4.25 bits per element. Magnitudes above
- *           3.5 2^126 (2.97e38) become code 4 at 2^126, which is 2^128.
+ *           dimensions of one position: 4.25 bits per element. Magnitudes of
+ *           3.5 2^126 (2.97e38) and more become code 4 at 2^126, which is 2^128:
+ *           infinite in avq_cache_attention_fwd.
  * block_table [S][max_pages] (int32, device) names the page of positions
  * i*page_size .. (i+1)*page_size - 1 of each sequence in column i; columns past
  * a sequence's length are not read. A position without a page (past max_pages,
