@@ -32,6 +32,9 @@
  *   avq_cache_append   keys and values into a paged cache, with the rotation
  *   avq_cache_gather   cached positions read back
  *   avq_cache_attention_fwd  exact attention of the newest tokens over the cache
+ *   avq_rotate_axes    rotary positions with several axes, and back
+ *   avq_cross_attention_fwd, avq_cross_attention_bwd  exact attention over an
+ *                      encoder's states, and its gradients
  *
  * Conventions shared by every call:
  *   - Every array argument is a DEVICE pointer owned by the caller, contiguous,
@@ -550,6 +553,110 @@ avq_status_t avq_cache_attention_fwd(avq_dtype_t dtype, avq_cache_t format, int3
                                      const int32_t* lens, const int32_t* block_table, void* Y,
                                      float* lse, void* workspace, int64_t workspace_bytes,
                                      void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Rotary positions with several axes, and cross attention (serving and training).
+ * Packed rows, strides and sizes as for avq_prompt_attention_fwd.
+ */
+
+/*
+ * avq_rotate_axes - rotates the queries, and keys, of packed tokens by their
+ * positions on several axes (time, height and width of a video's patches, say),
+ * or back.
+ *
+ * Token t has n_axes positions pos[t][0 .. n_axes-1]. Pair i of every head, i <
+ * rot/2, is dimensions (i, i + rot/2), or with interleaved = 1 (2i, 2i + 1), as
+ * in avq_cache_append; it turns by the angle of column i of the tables at the
+ * token's position on axis[i]: with p = pos[t][axis[i]],
+ *   a' = a cos[p][i] - b sin[p][i],  b' = b cos[p][i] + a sin[p][i]   (fp32)
+ * and with inverse = 1 by the opposite angle, -sin in place of sin: that takes
+ * gradients of the rotated rows to gradients of the rows. Results are rounded once
+ * to dtype; dimensions from rot on are copied. Nothing is written for a token that
+ * has a position outside [0, n_pos).
+ *
+ *   rot          a multiple of 16 in [16, d]
+ *   n_axes       1 .. AVQ_MAX_AXES
+ *   axis         [rot/2] bytes, HOST, each below n_axes: any order of the axes
+ *   Q            [T] rows of [Hq][d], dtype
+ *   K            [T] rows of [Hkv][d], nullable with K_out (Hkv and k_stride are
+ *                then not used)
+ *   pos          [T][n_axes] int32
+ *   cos, sin     [n_pos][rot/2] fp32
+ *   Q_out, K_out [T][Hq][d], [T][Hkv][d] dtype, contiguous, out (may be Q and K
+ *                themselves if these are contiguous; otherwise they overlap no input)
+ * T <= 2^24, 0 included. One launch. axis has been read when the call returns.
+ */
+enum { AVQ_MAX_AXES = 4 };
+avq_status_t avq_rotate_axes(avq_dtype_t dtype, int32_t T, int32_t Hq, int32_t Hkv, int32_t d,
+                             int32_t rot, int32_t n_axes, const uint8_t* axis, int32_t n_pos,
+                             int32_t interleaved, int32_t inverse, const void* Q, int64_t q_stride,
+                             const void* K, int64_t k_stride, const int32_t* pos, const float* cos,
+                             const float* sin, void* Q_out, void* K_out, void* stream);
+
+/*
+ * avq_cross_attention_fwd - exact softmax attention of packed queries over the
+ * states of an encoder (or any others) of another length.
+ *
+ * Source s has queries cu_q[s] .. cu_q[s+1]-1 and states cu_k[s] .. cu_k[s+1]-1;
+ * the queries of all sequences that read a source are simply packed together. With
+ * S_ij = scale q_i . k_j over the states j of i's source that take part:
+ *   lse_i = ln sum_j exp(S_ij),  Y_i = sum_j exp(S_ij - lse_i) v_j
+ * A query that sees no state gets Y_i = 0 and lse_i = -inf. Query head h reads
+ * key-value head h / (Hq / Hkv).
+ *
+ *   Q            [Tq] rows of [Hq][d], K, V [Tk] rows of [Hkv][d], dtype
+ *   cu_q, cu_k   [S + 1] int32, as in avq_prompt_attention_fwd
+ *   mask         [Tk] bytes, nullable, of any alignment: states with a 0 take no
+ *                part, whatever their rows of K and V hold (infinities and NaN too)
+ *   Y            [Tq][Hq][d] dtype, contiguous, out
+ *   lse          [Tq][Hq] fp32, out, nullable (avq_cross_attention_bwd takes it)
+ *   workspace    avq_cross_attention_workspace() bytes, NULL allowed for 0
+ * Sizes: (Tq Hq / Hkv / 128 + S) Hkv and (Tk / 128 + S) Hkv below 2^24. One launch,
+ * two with a workspace. Arithmetic and limits as avq_prompt_attention_fwd.
+ */
+avq_status_t avq_cross_attention_fwd(avq_dtype_t dtype, int32_t S, int32_t Tq, int32_t Tk,
+                                     int32_t Hq, int32_t Hkv, int32_t d, float scale, const void* Q,
+                                     int64_t q_stride, const void* K, int64_t k_stride,
+                                     const void* V, int64_t v_stride, const int32_t* cu_q,
+                                     const int32_t* cu_k, const uint8_t* mask, void* Y, float* lse,
+                                     void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Bytes of the workspaces of the cross attention calls (0: none needed, -1:
+ * unsupported sizes). Their contents need not be set and mean nothing afterwards;
+ * calls that may run at the same time need one each. */
+int64_t avq_cross_attention_workspace(int32_t S, int32_t Tq, int32_t Tk, int32_t Hq, int32_t Hkv,
+                                      int32_t d);
+int64_t avq_cross_attention_bwd_workspace(int32_t S, int32_t Tq, int32_t Tk, int32_t Hq,
+                                          int32_t Hkv, int32_t d);
+
+/*
+ * avq_cross_attention_bwd - gradients of avq_cross_attention_fwd's Y with respect
+ * to Q, K and V, from dY, that of the result with respect to Y. With P_ij =
+ * exp(S_ij - lse_i) and dS_ij = P_ij (dY_i . v_j - dY_i . Y_i):
+ *   dQ_i = scale sum_j dS_ij k_j,  dK_j = scale sum_i dS_ij q_i,  dV_j = sum_i P_ij dY_i
+ * The sums over i take all queries of the source and all heads that share the
+ * key-value head. Queries that see no state get dQ = 0, states that take no part or
+ * are read by no query dK = dV = 0; rows that belong to no source are left as they
+ * were. The same inputs give the same bits at every call.
+ *
+ *   dY           [Tq] rows of [Hq][d], dtype; dy_stride as the others
+ *   Q, K, V, cu_q, cu_k, mask, scale  those of the forward call
+ *   Y, lse       its results ([Tq][Hq][d], [Tq][Hq], contiguous)
+ *   dQ           [Tq][Hq][d], dK, dV [Tk][Hkv][d], dtype, contiguous, out
+ *   workspace    avq_cross_attention_bwd_workspace() bytes
+ * Sizes as the forward call. Two to four launches. bf16: products with fp32
+ * accumulation; P and dS, fp32, are rounded to bf16 for the products they enter.
+ * fp32: fp32 throughout. P is taken from lse, whose rounding leaves a relative error
+ * of |lse| 2^-23 in it.
+ */
+avq_status_t avq_cross_attention_bwd(avq_dtype_t dtype, int32_t S, int32_t Tq, int32_t Tk,
+                                     int32_t Hq, int32_t Hkv, int32_t d, float scale,
+                                     const void* dY, int64_t dy_stride, const void* Q,
+                                     int64_t q_stride, const void* K, int64_t k_stride,
+                                     const void* V, int64_t v_stride, const void* Y,
+                                     const float* lse, const int32_t* cu_q, const int32_t* cu_k,
+                                     const uint8_t* mask, void* dQ, void* dK, void* dV,
+                                     void* workspace, int64_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -30,7 +30,9 @@ SYMBOLS = ("avq_version", "avq_last_error", "avq_packed_bytes", "avq_assign",
            "avq_pack_aggregates", "avq_assign_aggregate", "avq_prompt_attention_fwd",
            "avq_prompt_attention_workspace",
            "avq_cache_page_bytes", "avq_cache_append", "avq_cache_gather",
-           "avq_cache_attention_workspace", "avq_cache_attention_fwd")
+           "avq_cache_attention_workspace", "avq_cache_attention_fwd",
+           "avq_rotate_axes", "avq_cross_attention_workspace", "avq_cross_attention_fwd",
+           "avq_cross_attention_bwd_workspace", "avq_cross_attention_bwd")
 CACHE_UNDIVIDED = 512  # positions of cached sequences whose keys are not divided
 IMPORTANCE_TILE = 64  # parents per codeword tile of attention_fwd(tiled_importance=True)
 
@@ -85,8 +87,18 @@ def lib():
         L.avq_cache_attention_workspace.restype = i64
         L.avq_cache_attention_fwd.argtypes = [ci, ci] + [i32] * 8 + [cf, vp, i64, vp, vp, vp, vp,
                                                                      vp, vp, i64, vp]
+        L.avq_rotate_axes.argtypes = ([ci] + [i32] * 6 + [ctypes.c_char_p] + [i32] * 3
+                                      + [vp, i64, vp, i64] + [vp] * 6)
+        L.avq_cross_attention_fwd.argtypes = ([ci] + [i32] * 6 + [cf] + [vp, i64] * 3 + [vp] * 6
+                                              + [i64, vp])
+        L.avq_cross_attention_bwd.argtypes = ([ci] + [i32] * 6 + [cf] + [vp, i64] * 4 + [vp] * 9
+                                              + [i64, vp])
+        for name in ("avq_cross_attention_workspace", "avq_cross_attention_bwd_workspace"):
+            getattr(L, name).argtypes = [i32] * 6
+            getattr(L, name).restype = i64
         for name in ("avq_prompt_attention_fwd", "avq_cache_append", "avq_cache_gather",
-                     "avq_cache_attention_fwd"):
+                     "avq_cache_attention_fwd", "avq_rotate_axes", "avq_cross_attention_fwd",
+                     "avq_cross_attention_bwd"):
             getattr(L, name).restype = ci
         for name in ("avq_assign", "avq_aggregate", "avq_attention_fwd", "avq_pack_aggregates",
                      "avq_assign_aggregate",
@@ -655,3 +667,194 @@ def cache_attention_fwd(Q, cache, block_table, lens, page_size: int, scale: floa
         block_table.data_ptr(), Y.data_ptr(), _ptr(lse), _ptr(workspace),
         0 if workspace is None else workspace.numel(), s))
     return (Y, lse) if with_lse else Y
+
+
+# ---- rotary positions with several axes, cross attention ----------------------
+
+
+@functools.lru_cache(maxsize=256)
+def _axis_bytes(axis: tuple) -> bytes:
+    if not all(isinstance(a, int) and 0 <= a < 256 for a in axis):
+        raise ValueError(f"axis must hold axis numbers, got {axis}")
+    return bytes(axis)
+
+
+def rotate_axes(Q, K, pos, cos, sin, axis, interleaved: bool = False, inverse: bool = False,
+                Q_out=None, K_out=None, stream=None):
+    """Rotates packed queries and keys by positions on several axes
+    (``avq_rotate_axes``), or with ``inverse`` back: the gradients' way.
+
+    Q [T, Hq, d], K [T, Hkv, d] or None: packed token rows as for
+    ``prompt_attention_fwd``; pos int32 [T, n_axes] on the GPU; cos, sin fp32
+    [n_pos, rot / 2]; axis: a tuple of rot / 2 axis numbers, one per pair. A token
+    with a position outside the tables is not written. Returns (Q_out, K_out),
+    which may be given and may be Q and K themselves; K_out is None without K.
+    """
+    q_stride = _rows(Q, "Q")
+    T, Hq, d = Q.shape
+    _dev(pos, "pos", torch.int32)
+    if pos.dim() != 2 or pos.shape[0] != T:
+        raise ValueError(f"pos must be [{T} tokens, axes], got {tuple(pos.shape)}")
+    _dev(cos, "cos", torch.float32)
+    _dev(sin, "sin", torch.float32, cos.shape)
+    if cos.dim() != 2:
+        raise ValueError(f"cos must be [positions, rot / 2], got {tuple(cos.shape)}")
+    n_pos, half = cos.shape
+    axes = _axis_bytes(axis if type(axis) is tuple else tuple(axis))
+    if len(axes) != half:
+        raise ValueError(f"axis must name the axes of {half} pairs, got {len(axes)}")
+    Hkv, k_stride = Hq, 0
+    if K is not None:
+        k_stride = _rows(K, "K", d=d, dtype=Q.dtype)
+        Hkv = K.shape[1]
+        if K.shape[0] != T:
+            raise ValueError(f"K must have {T} tokens, got {K.shape[0]}")
+    elif K_out is not None:
+        raise ValueError("K_out without K")
+    s = _launch_stream(stream, Q.device)
+    if Q_out is None:
+        Q_out = _empty(stream, (T, Hq, d), Q.dtype, Q.device)
+    else:
+        _dev(Q_out, "Q_out", Q.dtype, (T, Hq, d))
+    if K_out is not None:
+        _dev(K_out, "K_out", Q.dtype, (T, Hkv, d))
+    elif K is not None:
+        K_out = _empty(stream, (T, Hkv, d), Q.dtype, Q.device)
+    at = Q.get_device()
+    if (not pos.get_device() == cos.get_device() == sin.get_device() == Q_out.get_device() == at
+            or _elsewhere(K, at) or _elsewhere(K_out, at)):
+        _same_device(Q, K=K, pos=pos, cos=cos, sin=sin, Q_out=Q_out, K_out=K_out)
+    _check(lib().avq_rotate_axes(
+        _dtype_code(Q), T, Hq, Hkv, d, 2 * half, pos.shape[1], axes, n_pos, int(bool(interleaved)),
+        int(bool(inverse)), Q.data_ptr(), q_stride, _ptr(K), k_stride, pos.data_ptr(),
+        cos.data_ptr(), sin.data_ptr(), Q_out.data_ptr(), _ptr(K_out), s))
+    return Q_out, K_out
+
+
+def cross_attention_workspace(S: int, Tq: int, Tk: int, Hq: int, Hkv: int, d: int,
+                              backward: bool = False) -> int:
+    """Bytes of the workspace of ``cross_attention_fwd`` (0: none needed) or
+    ``cross_attention_bwd``."""
+    L = lib()
+    n = (L.avq_cross_attention_bwd_workspace if backward else L.avq_cross_attention_workspace)(
+        S, Tq, Tk, Hq, Hkv, d)
+    if n < 0:
+        raise ValueError(f"unsupported sizes S={S} Tq={Tq} Tk={Tk} Hq={Hq} Hkv={Hkv} d={d}")
+    return n
+
+
+_cross_workspace_of = functools.lru_cache(maxsize=256)(cross_attention_workspace)
+
+
+def _cross(Q, K, V, cu_q, cu_k, mask):
+    """Checks what the cross attention calls share; returns the strides."""
+    q_stride = _rows(Q, "Q")
+    d = Q.shape[2]
+    k_stride = _rows(K, "K", d=d, dtype=Q.dtype)
+    Tk = K.shape[0]
+    v_stride = _rows(V, "V", K.shape[1], d, Q.dtype)
+    if V.shape[0] != Tk:
+        raise ValueError(f"V must have {Tk} tokens, got {V.shape[0]}")
+    _dev(cu_q, "cu_q", torch.int32)
+    _dev(cu_k, "cu_k", torch.int32, cu_q.shape)
+    if cu_q.dim() != 1 or cu_q.shape[0] < 2:
+        raise ValueError(f"cu_q must be [sources + 1], got {tuple(cu_q.shape)}")
+    if mask is not None:
+        if isinstance(mask, torch.Tensor) and mask.dtype not in (torch.bool, torch.uint8):
+            raise ValueError(f"mask must be bool or uint8, got {mask.dtype}")
+        _dev(mask, "mask", None, (Tk,))
+    return q_stride, k_stride, v_stride
+
+
+def cross_attention_fwd(Q, K, V, cu_q, cu_k, scale: float, mask=None, Y=None,
+                        with_lse: bool = False, lse=None, workspace=None, stream=None):
+    """Exact attention of packed queries over the states of their source
+    (``avq_cross_attention_fwd``).
+
+    Q [Tq, Hq, d], K and V [Tk, Hkv, d]: packed token rows as for
+    ``prompt_attention_fwd``; cu_q, cu_k int32 [S + 1] on the GPU: the queries and
+    the states of each source. mask: bool or uint8 [Tk], False for states that take
+    no part. Rows behind the last source are left as they were. Returns Y
+    [Tq, Hq, d], or (Y, lse) with ``with_lse`` (lse: fp32 [Tq, Hq], which
+    ``cross_attention_bwd`` takes).
+    """
+    q_stride, k_stride, v_stride = _cross(Q, K, V, cu_q, cu_k, mask)
+    Tq, Hq, d = Q.shape
+    Tk, Hkv = K.shape[0], K.shape[1]
+    s = _launch_stream(stream, Q.device)
+    if Y is None:
+        Y = _empty(stream, (Tq, Hq, d), Q.dtype, Q.device)
+    else:
+        _dev(Y, "Y", Q.dtype, (Tq, Hq, d))
+    if lse is not None:
+        _dev(lse, "lse", torch.float32, (Tq, Hq))
+    elif with_lse:
+        lse = _empty(stream, (Tq, Hq), torch.float32, Q.device)
+    S = cu_q.shape[0] - 1
+    if workspace is not None:
+        _dev(workspace, "workspace", torch.uint8)
+    else:
+        n = _cross_workspace_of(S, Tq, Tk, Hq, Hkv, d)
+        if n:
+            workspace = _empty(stream, (n,), torch.uint8, Q.device)
+    at = Q.get_device()
+    if (not K.get_device() == V.get_device() == cu_q.get_device() == cu_k.get_device()
+            == Y.get_device() == at or _elsewhere(mask, at) or _elsewhere(lse, at)
+            or _elsewhere(workspace, at)):
+        _same_device(Q, K=K, V=V, cu_q=cu_q, cu_k=cu_k, mask=mask, Y=Y, lse=lse,
+                     workspace=workspace)
+    _check(lib().avq_cross_attention_fwd(
+        _dtype_code(Q), S, Tq, Tk, Hq, Hkv, d, float(scale), Q.data_ptr(), q_stride, K.data_ptr(),
+        k_stride, V.data_ptr(), v_stride, cu_q.data_ptr(), cu_k.data_ptr(), _ptr(mask),
+        Y.data_ptr(), _ptr(lse), _ptr(workspace), 0 if workspace is None else workspace.numel(), s))
+    return (Y, lse) if with_lse else Y
+
+
+def cross_attention_bwd(dY, Q, K, V, Y, lse, cu_q, cu_k, scale: float, mask=None, dQ=None, dK=None,
+                        dV=None, workspace=None, stream=None):
+    """Gradients of ``cross_attention_fwd`` (``avq_cross_attention_bwd``): dY
+    [Tq, Hq, d] (packed rows; an expanded or otherwise overlapping gradient is
+    refused), the forward call's inputs and its Y and lse. Rows that belong to no
+    source are left as they were (pass dQ, dK, dV to set them). workspace: a uint8
+    tensor of ``cross_attention_workspace(..., backward=True)`` bytes. Returns
+    (dQ, dK, dV)."""
+    q_stride, k_stride, v_stride = _cross(Q, K, V, cu_q, cu_k, mask)
+    Tq, Hq, d = Q.shape
+    Tk, Hkv = K.shape[0], K.shape[1]
+    dy_stride = _rows(dY, "dY", Hq, d, Q.dtype)
+    if dY.shape[0] != Tq:
+        raise ValueError(f"dY must have {Tq} tokens, got {dY.shape[0]}")
+    _dev(Y, "Y", Q.dtype, (Tq, Hq, d))
+    _dev(lse, "lse", torch.float32, (Tq, Hq))
+    s = _launch_stream(stream, Q.device)
+    if dQ is None:
+        dQ = _empty(stream, (Tq, Hq, d), Q.dtype, Q.device)
+    else:
+        _dev(dQ, "dQ", Q.dtype, (Tq, Hq, d))
+    if dK is None:
+        dK = _empty(stream, (Tk, Hkv, d), Q.dtype, Q.device)
+    else:
+        _dev(dK, "dK", Q.dtype, (Tk, Hkv, d))
+    if dV is None:
+        dV = _empty(stream, (Tk, Hkv, d), Q.dtype, Q.device)
+    else:
+        _dev(dV, "dV", Q.dtype, (Tk, Hkv, d))
+    S = cu_q.shape[0] - 1
+    if workspace is not None:
+        _dev(workspace, "workspace", torch.uint8)
+    else:
+        n = _cross_workspace_of(S, Tq, Tk, Hq, Hkv, d, True)
+        workspace = _empty(stream, (n,), torch.uint8, Q.device)
+    at = Q.get_device()
+    if (not dY.get_device() == K.get_device() == V.get_device() == Y.get_device()
+            == lse.get_device() == cu_q.get_device() == cu_k.get_device() == dQ.get_device()
+            == dK.get_device() == dV.get_device() == workspace.get_device() == at
+            or _elsewhere(mask, at)):
+        _same_device(Q, dY=dY, K=K, V=V, Y=Y, lse=lse, cu_q=cu_q, cu_k=cu_k, mask=mask, dQ=dQ,
+                     dK=dK, dV=dV, workspace=workspace)
+    _check(lib().avq_cross_attention_bwd(
+        _dtype_code(Q), S, Tq, Tk, Hq, Hkv, d, float(scale), dY.data_ptr(), dy_stride,
+        Q.data_ptr(), q_stride, K.data_ptr(), k_stride, V.data_ptr(), v_stride, Y.data_ptr(),
+        lse.data_ptr(), cu_q.data_ptr(), cu_k.data_ptr(), _ptr(mask), dQ.data_ptr(), dK.data_ptr(),
+        dV.data_ptr(), workspace.data_ptr(), workspace.numel(), s))
+    return dQ, dK, dV

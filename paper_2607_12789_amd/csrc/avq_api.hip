@@ -386,6 +386,46 @@ avq_status_t null_pointer(const char* name) {
   return fail(AVQ_ERR_INVALID_ARG, "%s: null pointer argument", name);
 }
 
+avq_status_t check_workspace(const char* name, int64_t need, const void* workspace,
+                             int64_t workspace_bytes) {
+  if (need > 0 && (!workspace || workspace_bytes < need))
+    return fail(AVQ_ERR_INVALID_ARG, "%s: workspace of %lld bytes, %lld are needed", name,
+                workspace ? (long long)workspace_bytes : 0LL, (long long)need);
+  return AVQ_OK;
+}
+
+// Sizes of the cross attention calls: rows (a query and a head of its group) and
+// states in tiles of 128 per key-value head.
+bool cross_tiles_fit(int32_t S, int32_t Tq, int32_t Tk, int32_t Hq, int32_t Hkv) {
+  const int64_t rows = (int64_t)Tq * (Hq / Hkv);
+  return (rows / 128 + S) * Hkv < kMaxBlocks && ((int64_t)Tk / 128 + S) * Hkv < kMaxBlocks;
+}
+bool cross_sizes(int32_t S, int32_t Tq, int32_t Tk, int32_t Hq, int32_t Hkv, int32_t d) {
+  return S >= 1 && S <= (1 << 20) && Hq >= 1 && Hkv >= 1 && Hq <= kMaxHeads && Hq % Hkv == 0 &&
+         (d == 64 || d == 128) && Tq >= 0 && Tk >= 0 && Tq <= (1 << 24) && Tk <= (1 << 24) &&
+         cross_tiles_fit(S, Tq, Tk, Hq, Hkv);
+}
+
+avq_status_t check_cross(const char* name, avq_dtype_t dtype, int32_t S, int32_t Tq, int32_t Tk,
+                         int32_t Hq, int32_t Hkv, int32_t d, float scale, int64_t q_stride,
+                         int64_t k_stride, int64_t v_stride) {
+  avq_status_t st = check_heads(name, dtype, S, Hq, Hkv, d);
+  if (st == AVQ_OK) st = check_stride(name, "q_stride", dtype, q_stride, Hq, d);
+  if (st == AVQ_OK) st = check_stride(name, "k_stride", dtype, k_stride, Hkv, d);
+  if (st == AVQ_OK) st = check_stride(name, "v_stride", dtype, v_stride, Hkv, d);
+  if (st == AVQ_OK) st = check_scale(name, scale);
+  if (st != AVQ_OK) return st;
+  if (Tq < 0 || Tk < 0)
+    return fail(AVQ_ERR_INVALID_ARG, "%s: Tq=%d and Tk=%d must not be negative", name, Tq, Tk);
+  if (Tq > (1 << 24) || Tk > (1 << 24))
+    return fail(AVQ_ERR_UNSUPPORTED, "%s: Tq=%d, Tk=%d: at most 2^24 tokens", name, Tq, Tk);
+  if (!cross_tiles_fit(S, Tq, Tk, Hq, Hkv))
+    return fail(AVQ_ERR_UNSUPPORTED,
+                "%s: Tq=%d queries and Tk=%d states of S=%d sources, Hq=%d, Hkv=%d heads: too many",
+                name, Tq, Tk, S, Hq, Hkv);
+  return AVQ_OK;
+}
+
 // calls launch<T, D> for the dtype and head width
 #define AVQ_BY_TYPE(launch, ...)                                                        \
   (dtype == AVQ_BF16 ? (d == 64 ? avq::launch<avq::bf16, 64>(__VA_ARGS__)               \
@@ -560,6 +600,113 @@ avq_status_t avq_cache_attention_fwd(avq_dtype_t dtype, avq_cache_t format, int3
   return from_hip(AVQ_BY_TYPE(launch_cache_attention, c, S, n_q, Hq, scale, Q, q_stride, cache, lens,
                               block_table, Y, lse, workspace, s),
                   "avq_cache_attention_fwd launch");
+}
+
+avq_status_t avq_rotate_axes(avq_dtype_t dtype, int32_t T, int32_t Hq, int32_t Hkv, int32_t d,
+                             int32_t rot, int32_t n_axes, const uint8_t* axis, int32_t n_pos,
+                             int32_t interleaved, int32_t inverse, const void* Q, int64_t q_stride,
+                             const void* K, int64_t k_stride, const int32_t* pos, const float* cos,
+                             const float* sin, void* Q_out, void* K_out, void* stream) {
+  const char* name = "avq_rotate_axes";
+  // without keys only the queries' heads count
+  avq_status_t st = check_heads(name, dtype, 1, Hq, K ? Hkv : Hq, d);
+  if (st == AVQ_OK) st = check_stride(name, "q_stride", dtype, q_stride, Hq, d);
+  if (st == AVQ_OK && K) st = check_stride(name, "k_stride", dtype, k_stride, Hkv, d);
+  if (st != AVQ_OK) return st;
+  if (T < 0) return fail(AVQ_ERR_INVALID_ARG, "%s: T=%d must not be negative", name, T);
+  if (T > (1 << 24)) return fail(AVQ_ERR_UNSUPPORTED, "%s: T=%d: at most 2^24 tokens", name, T);
+  if (rot < 16 || rot > d || rot % 16 != 0)
+    return fail(AVQ_ERR_INVALID_ARG, "%s: rot=%d must be a multiple of 16 in [16, d=%d]", name, rot,
+                d);
+  if (n_axes < 1 || n_axes > AVQ_MAX_AXES)
+    return fail(AVQ_ERR_INVALID_ARG, "%s: n_axes=%d must be in [1, %d]", name, n_axes, AVQ_MAX_AXES);
+  if (n_pos < 1) return fail(AVQ_ERR_INVALID_ARG, "%s: n_pos=%d must be positive", name, n_pos);
+  if ((interleaved != 0 && interleaved != 1) || (inverse != 0 && inverse != 1))
+    return fail(AVQ_ERR_INVALID_ARG, "%s: interleaved=%d, inverse=%d: must be 0 or 1", name,
+                interleaved, inverse);
+  if (!axis || !cos || !sin || (!K != !K_out) || (T > 0 && (!Q || !Q_out || !pos)))
+    return null_pointer(name);
+  for (int i = 0; i < rot / 2; ++i)
+    if (axis[i] >= n_axes)
+      return fail(AVQ_ERR_INVALID_ARG, "%s: axis[%d]=%d must be below n_axes=%d", name, i, axis[i],
+                  n_axes);
+  if (!aligned16(Q) || !aligned16(K) || !aligned16(pos) || !aligned16(cos) || !aligned16(sin) ||
+      !aligned16(Q_out) || !aligned16(K_out))
+    return misaligned(name);
+  if (T == 0) return ok();
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  return from_hip(AVQ_BY_TYPE(launch_rotate_axes, T, Hq, Hkv, rot, n_axes, axis, n_pos, interleaved,
+                              inverse, Q, q_stride, K, k_stride, pos, cos, sin, Q_out, K_out, s),
+                  "avq_rotate_axes launch");
+}
+
+int64_t avq_cross_attention_workspace(int32_t S, int32_t Tq, int32_t Tk, int32_t Hq, int32_t Hkv,
+                                      int32_t d) {
+  return cross_sizes(S, Tq, Tk, Hq, Hkv, d)
+             ? (int64_t)avq::cross_attention_workspace(S, Tq, Tk, Hq, Hkv, d)
+             : -1;
+}
+
+avq_status_t avq_cross_attention_fwd(avq_dtype_t dtype, int32_t S, int32_t Tq, int32_t Tk,
+                                     int32_t Hq, int32_t Hkv, int32_t d, float scale, const void* Q,
+                                     int64_t q_stride, const void* K, int64_t k_stride,
+                                     const void* V, int64_t v_stride, const int32_t* cu_q,
+                                     const int32_t* cu_k, const uint8_t* mask, void* Y, float* lse,
+                                     void* workspace, int64_t workspace_bytes, void* stream) {
+  const char* name = "avq_cross_attention_fwd";
+  avq_status_t st =
+      check_cross(name, dtype, S, Tq, Tk, Hq, Hkv, d, scale, q_stride, k_stride, v_stride);
+  if (st != AVQ_OK) return st;
+  if (!cu_q || !cu_k || (Tq > 0 && (!Q || !Y)) || (Tk > 0 && (!K || !V))) return null_pointer(name);
+  if (!aligned16(Q) || !aligned16(K) || !aligned16(V) || !aligned16(cu_q) || !aligned16(cu_k) ||
+      !aligned16(Y) || !aligned16(lse) || !aligned16(workspace))
+    return misaligned(name);
+  st = check_workspace(name, avq_cross_attention_workspace(S, Tq, Tk, Hq, Hkv, d), workspace,
+                       workspace_bytes);
+  if (st != AVQ_OK) return st;
+  if (Tq == 0) return ok();
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  return from_hip(AVQ_BY_TYPE(launch_cross_attention, S, Tq, Tk, Hq, Hkv, scale, Q, q_stride, K,
+                              k_stride, V, v_stride, cu_q, cu_k, mask, Y, lse, workspace, s),
+                  "avq_cross_attention_fwd launch");
+}
+
+int64_t avq_cross_attention_bwd_workspace(int32_t S, int32_t Tq, int32_t Tk, int32_t Hq,
+                                          int32_t Hkv, int32_t d) {
+  return cross_sizes(S, Tq, Tk, Hq, Hkv, d)
+             ? (int64_t)avq::cross_attention_bwd_workspace(S, Tq, Tk, Hq, Hkv, d)
+             : -1;
+}
+
+avq_status_t avq_cross_attention_bwd(avq_dtype_t dtype, int32_t S, int32_t Tq, int32_t Tk,
+                                     int32_t Hq, int32_t Hkv, int32_t d, float scale,
+                                     const void* dY, int64_t dy_stride, const void* Q,
+                                     int64_t q_stride, const void* K, int64_t k_stride,
+                                     const void* V, int64_t v_stride, const void* Y,
+                                     const float* lse, const int32_t* cu_q, const int32_t* cu_k,
+                                     const uint8_t* mask, void* dQ, void* dK, void* dV,
+                                     void* workspace, int64_t workspace_bytes, void* stream) {
+  const char* name = "avq_cross_attention_bwd";
+  avq_status_t st =
+      check_cross(name, dtype, S, Tq, Tk, Hq, Hkv, d, scale, q_stride, k_stride, v_stride);
+  if (st == AVQ_OK) st = check_stride(name, "dy_stride", dtype, dy_stride, Hq, d);
+  if (st != AVQ_OK) return st;
+  if (!cu_q || !cu_k || (Tq > 0 && (!dY || !Q || !Y || !lse || !dQ)) ||
+      (Tk > 0 && (!K || !V || !dK || !dV)))
+    return null_pointer(name);
+  if (!aligned16(dY) || !aligned16(Q) || !aligned16(K) || !aligned16(V) || !aligned16(Y) ||
+      !aligned16(lse) || !aligned16(cu_q) || !aligned16(cu_k) || !aligned16(dQ) ||
+      !aligned16(dK) || !aligned16(dV) || !aligned16(workspace))
+    return misaligned(name);
+  st = check_workspace(name, avq_cross_attention_bwd_workspace(S, Tq, Tk, Hq, Hkv, d), workspace,
+                       workspace_bytes);
+  if (st != AVQ_OK) return st;
+  if (Tq == 0 && Tk == 0) return ok();
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  return from_hip(AVQ_BY_TYPE(launch_cross_attention_bwd, S, Tq, Tk, Hq, Hkv, scale, Q, q_stride, K,
+                              k_stride, V, v_stride, cu_q, cu_k, mask, Y, lse, dY, dy_stride, dQ, dK,
+                              dV, workspace, s),
+                  "avq_cross_attention_bwd launch");
 }
 
 }  // extern "C"
