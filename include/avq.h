@@ -35,6 +35,8 @@
  *   avq_rotate_axes    rotary positions with several axes, and back
  *   avq_cross_attention_fwd, avq_cross_attention_bwd  exact attention over an
  *                      encoder's states, and its gradients
+ *   avq_cache_prefix_attention_fwd  attention over the cache for groups of
+ *                      sequences that share their first positions
  *
  * Conventions shared by every call:
  *   - Every array argument is a DEVICE pointer owned by the caller, contiguous,
@@ -657,6 +659,45 @@ avq_status_t avq_cross_attention_bwd(avq_dtype_t dtype, int32_t S, int32_t Tq, i
                                      const float* lse, const int32_t* cu_q, const int32_t* cu_k,
                                      const uint8_t* mask, void* dQ, void* dK, void* dV,
                                      void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Bytes of the workspace of avq_cache_prefix_attention_fwd (-1: unsupported
+ * sizes). Its contents need not be set and mean nothing afterwards; calls that may
+ * run at the same time need one each. */
+int64_t avq_cache_prefix_attention_workspace(int32_t S, int32_t n_groups, int32_t n_q, int32_t Hq,
+                                             int32_t Hkv, int32_t d);
+
+/*
+ * avq_cache_prefix_attention_fwd - avq_cache_attention_fwd for groups of sequences
+ * that share their first positions (several answers to one long prompt): those are
+ * attended to once for the whole group, and read once.
+ *
+ * Group g is the sequences cu_groups[g] .. cu_groups[g+1]-1 of the batch, whose
+ * first shared[g] positions are the same ones: their block tables may name the same
+ * pages for them, or copies (of the page in which the shared positions end, say).
+ * Positions below P_g = min(shared[g], lens[cu_groups[g]]) are read through the
+ * table of the group's first sequence only, for all of its sequences; a sequence
+ * whose own positions there differ is answered as if they did not. A group of one
+ * sequence, and sequences of no group, share nothing. If the first sequence of a
+ * group is idle (lens 0), so is the sharing: P_g = 0, and every sequence reads its
+ * own pages. Y and lse are those of avq_cache_attention_fwd on the same arguments,
+ * but for the rounding of the sums.
+ *
+ *   cu_groups    [n_groups + 1] int32; it must not decrease (if it does, outputs are
+ *                unspecified); values outside [0, S] are taken as the nearest
+ *   shared       [n_groups] int32, below 0: none
+ *   others       as avq_cache_attention_fwd
+ *   workspace    avq_cache_prefix_attention_workspace() bytes
+ * n_groups >= 1; (S n_q Hq / Hkv / 128 + n_groups) Hkv < 2^24. Two launches.
+ */
+avq_status_t avq_cache_prefix_attention_fwd(avq_dtype_t dtype, avq_cache_t format, int32_t S,
+                                            int32_t n_groups, int32_t n_q, int32_t Hq, int32_t Hkv,
+                                            int32_t d, int32_t n_pages, int32_t page_size,
+                                            int32_t max_pages, float scale, const void* Q,
+                                            int64_t q_stride, const void* cache,
+                                            const int32_t* lens, const int32_t* block_table,
+                                            const int32_t* cu_groups, const int32_t* shared,
+                                            void* Y, float* lse, void* workspace,
+                                            int64_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -32,7 +32,8 @@ SYMBOLS = ("avq_version", "avq_last_error", "avq_packed_bytes", "avq_assign",
            "avq_cache_page_bytes", "avq_cache_append", "avq_cache_gather",
            "avq_cache_attention_workspace", "avq_cache_attention_fwd",
            "avq_rotate_axes", "avq_cross_attention_workspace", "avq_cross_attention_fwd",
-           "avq_cross_attention_bwd_workspace", "avq_cross_attention_bwd")
+           "avq_cross_attention_bwd_workspace", "avq_cross_attention_bwd",
+           "avq_cache_prefix_attention_workspace", "avq_cache_prefix_attention_fwd")
 CACHE_UNDIVIDED = 512  # positions of cached sequences whose keys are not divided
 IMPORTANCE_TILE = 64  # parents per codeword tile of attention_fwd(tiled_importance=True)
 
@@ -93,12 +94,15 @@ def lib():
                                               + [i64, vp])
         L.avq_cross_attention_bwd.argtypes = ([ci] + [i32] * 6 + [cf] + [vp, i64] * 4 + [vp] * 9
                                               + [i64, vp])
-        for name in ("avq_cross_attention_workspace", "avq_cross_attention_bwd_workspace"):
+        L.avq_cache_prefix_attention_fwd.argtypes = [ci, ci] + [i32] * 9 + [cf, vp, i64] + [vp] * 8 + [
+            i64, vp]
+        for name in ("avq_cross_attention_workspace", "avq_cross_attention_bwd_workspace",
+                     "avq_cache_prefix_attention_workspace"):
             getattr(L, name).argtypes = [i32] * 6
             getattr(L, name).restype = i64
         for name in ("avq_prompt_attention_fwd", "avq_cache_append", "avq_cache_gather",
                      "avq_cache_attention_fwd", "avq_rotate_axes", "avq_cross_attention_fwd",
-                     "avq_cross_attention_bwd"):
+                     "avq_cross_attention_bwd", "avq_cache_prefix_attention_fwd"):
             getattr(L, name).restype = ci
         for name in ("avq_assign", "avq_aggregate", "avq_attention_fwd", "avq_pack_aggregates",
                      "avq_assign_aggregate",
@@ -616,6 +620,21 @@ def cache_attention_workspace(S: int, n_q: int, Hq: int, Hkv: int, d: int) -> in
 _cache_workspace_of = functools.lru_cache(maxsize=256)(cache_attention_workspace)
 
 
+def _newest(Q):
+    """Checks the newest tokens' queries; returns their sizes and the elements from
+    one token to the next."""
+    if not isinstance(Q, torch.Tensor) or not Q.is_cuda:
+        raise ValueError("Q must be a tensor on the GPU")
+    if Q.dim() != 4:
+        raise ValueError(f"Q must be [sequences, tokens, heads, d], got {tuple(Q.shape)}")
+    S, n_q, Hq, d = Q.shape
+    if Q.is_contiguous():
+        return S, n_q, Hq, d, Hq * d
+    if S > 1 and n_q > 1 and Q.stride(0) != n_q * Q.stride(1):
+        raise ValueError("Q: the tokens must be evenly spaced")
+    return S, n_q, Hq, d, _rows(Q.view(S * n_q, Hq, d), "Q")
+
+
 def cache_attention_fwd(Q, cache, block_table, lens, page_size: int, scale: float,
                         fp4: bool = False, Y=None, with_lse: bool = False, lse=None,
                         workspace=None, stream=None):
@@ -628,17 +647,7 @@ def cache_attention_fwd(Q, cache, block_table, lens, page_size: int, scale: floa
     ``CACHE_UNDIVIDED`` positions per sequence needs none). Returns Y
     [S, n_q, Hq, d], or (Y, lse) with ``with_lse`` (lse: fp32 [S, n_q, Hq]).
     """
-    if not isinstance(Q, torch.Tensor) or not Q.is_cuda:
-        raise ValueError("Q must be a tensor on the GPU")
-    if Q.dim() != 4:
-        raise ValueError(f"Q must be [sequences, tokens, heads, d], got {tuple(Q.shape)}")
-    S, n_q, Hq, d = Q.shape
-    if Q.is_contiguous():
-        q_stride = Hq * d
-    elif S > 1 and n_q > 1 and Q.stride(0) != n_q * Q.stride(1):
-        raise ValueError("Q: the tokens must be evenly spaced")
-    else:
-        q_stride = _rows(Q.view(S * n_q, Hq, d), "Q")
+    S, n_q, Hq, d, q_stride = _newest(Q)
     n_pages, Hkv, _, max_pages = _cache(cache, block_table, Q.dtype, page_size, d, fp4, S)
     _dev(lens, "lens", torch.int32, (S,))
     s = _launch_stream(stream, Q.device)
@@ -858,3 +867,68 @@ def cross_attention_bwd(dY, Q, K, V, Y, lse, cu_q, cu_k, scale: float, mask=None
         lse.data_ptr(), cu_q.data_ptr(), cu_k.data_ptr(), _ptr(mask), dQ.data_ptr(), dK.data_ptr(),
         dV.data_ptr(), workspace.data_ptr(), workspace.numel(), s))
     return dQ, dK, dV
+
+
+# ---- groups of sequences that share their first positions ----------------------
+
+
+def cache_prefix_attention_workspace(S: int, n_groups: int, n_q: int, Hq: int, Hkv: int,
+                                     d: int) -> int:
+    """Bytes of the workspace of ``cache_prefix_attention_fwd``."""
+    n = lib().avq_cache_prefix_attention_workspace(S, n_groups, n_q, Hq, Hkv, d)
+    if n < 0:
+        raise ValueError(f"unsupported sizes S={S} n_groups={n_groups} n_q={n_q} Hq={Hq} Hkv={Hkv} "
+                         f"d={d}")
+    return n
+
+
+_prefix_workspace_of = functools.lru_cache(maxsize=256)(cache_prefix_attention_workspace)
+
+
+def cache_prefix_attention_fwd(Q, cache, block_table, lens, cu_groups, shared, page_size: int,
+                               scale: float, fp4: bool = False, Y=None, with_lse: bool = False,
+                               lse=None, workspace=None, stream=None):
+    """``cache_attention_fwd`` for groups of sequences that share their first
+    positions, which are attended to once per group
+    (``avq_cache_prefix_attention_fwd``).
+
+    cu_groups int32 [groups + 1]: group g is the sequences cu_groups[g] ..
+    cu_groups[g + 1] - 1; shared int32 [groups]: how many first positions they have in
+    common. The other arguments, and what is returned, are those of
+    ``cache_attention_fwd``; workspace: a uint8 tensor of
+    ``cache_prefix_attention_workspace(...)`` bytes (allocated if not given).
+    """
+    S, n_q, Hq, d, q_stride = _newest(Q)
+    n_pages, Hkv, _, max_pages = _cache(cache, block_table, Q.dtype, page_size, d, fp4, S)
+    _dev(lens, "lens", torch.int32, (S,))
+    _dev(shared, "shared", torch.int32)
+    if shared.dim() != 1:
+        raise ValueError(f"shared must be [groups], got {tuple(shared.shape)}")
+    n_groups = shared.shape[0]
+    _dev(cu_groups, "cu_groups", torch.int32, (n_groups + 1,))
+    s = _launch_stream(stream, Q.device)
+    if Y is None:
+        Y = _empty(stream, (S, n_q, Hq, d), Q.dtype, Q.device)
+    else:
+        _dev(Y, "Y", Q.dtype, (S, n_q, Hq, d))
+    if lse is not None:
+        _dev(lse, "lse", torch.float32, (S, n_q, Hq))
+    elif with_lse:
+        lse = _empty(stream, (S, n_q, Hq), torch.float32, Q.device)
+    if workspace is not None:
+        _dev(workspace, "workspace", torch.uint8)
+    else:
+        n = _prefix_workspace_of(S, n_groups, n_q, Hq, Hkv, d)
+        workspace = _empty(stream, (n,), torch.uint8, Q.device)
+    at = Q.get_device()
+    if (not cache.get_device() == block_table.get_device() == lens.get_device()
+            == cu_groups.get_device() == shared.get_device() == Y.get_device()
+            == workspace.get_device() == at or _elsewhere(lse, at)):
+        _same_device(Q, cache=cache, block_table=block_table, lens=lens, cu_groups=cu_groups,
+                     shared=shared, Y=Y, lse=lse, workspace=workspace)
+    _check(lib().avq_cache_prefix_attention_fwd(
+        _dtype_code(Q), int(bool(fp4)), S, n_groups, n_q, Hq, Hkv, d, n_pages, page_size, max_pages,
+        float(scale), Q.data_ptr(), q_stride, cache.data_ptr(), lens.data_ptr(),
+        block_table.data_ptr(), cu_groups.data_ptr(), shared.data_ptr(), Y.data_ptr(), _ptr(lse),
+        workspace.data_ptr(), workspace.numel(), s))
+    return (Y, lse) if with_lse else Y

@@ -25,7 +25,8 @@ CSRC = PKG / "csrc"
 LIB = PKG / "libavq.so"
 SOURCES = ["avq_api.hip", "avq_assign.hip", "avq_aggregate.hip", "avq_attention.hip",
            "avq_codebook.hip", "avq_order.hip", "avq_pack.hip", "avq_prompt.hip", "avq_cache.hip",
-           "avq_cache_attention.hip", "avq_rotate.hip", "avq_cross.hip", "avq_cross_bwd.hip"]
+           "avq_cache_attention.hip", "avq_rotate.hip", "avq_cross.hip", "avq_cross_bwd.hip",
+           "avq_prefix.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 COMPILE_FLAGS = [

@@ -426,6 +426,32 @@ avq_status_t check_cross(const char* name, avq_dtype_t dtype, int32_t S, int32_t
   return AVQ_OK;
 }
 
+// What the attentions over the cache share.
+avq_status_t check_cached(const char* name, avq_dtype_t dtype, avq_cache_t format, int32_t S,
+                          int32_t n_q, int32_t Hq, int32_t Hkv, int32_t d, int32_t n_pages,
+                          int32_t page_size, int32_t max_pages, float scale, int64_t q_stride) {
+  avq_status_t st = check_heads(name, dtype, S, Hq, Hkv, d);
+  if (st == AVQ_OK) st = check_cache(name, format, n_pages, page_size, max_pages);
+  if (st == AVQ_OK) st = check_stride(name, "q_stride", dtype, q_stride, Hq, d);
+  if (st == AVQ_OK) st = check_scale(name, scale);
+  if (st != AVQ_OK) return st;
+  if (n_q < 1) return fail(AVQ_ERR_INVALID_ARG, "%s: n_q=%d must be positive", name, n_q);
+  if (n_q > kMaxDrafts)
+    return fail(AVQ_ERR_UNSUPPORTED, "%s: n_q=%d: at most %d tokens per sequence", name, n_q,
+                kMaxDrafts);
+  if (cache_segments(S, n_q, Hq, Hkv) >= kMaxBlocks)
+    return fail(AVQ_ERR_UNSUPPORTED, "%s: S=%d sequences of Hq=%d, Hkv=%d heads: too many", name, S,
+                Hq, Hkv);
+  if ((int64_t)S * (((int64_t)max_pages * page_size + 127) / 128) > (1LL << 30))
+    return fail(AVQ_ERR_UNSUPPORTED, "%s: S * max_pages * page_size: at most 2^37 positions", name);
+  return AVQ_OK;
+}
+
+bool groups_fit(int32_t S, int32_t n_groups, int32_t n_q, int32_t Hq, int32_t Hkv) {
+  return n_groups >= 1 && n_groups <= (1 << 20) &&
+         ((int64_t)S * n_q * (Hq / Hkv) / 128 + n_groups) * Hkv < kMaxBlocks;
+}
+
 // calls launch<T, D> for the dtype and head width
 #define AVQ_BY_TYPE(launch, ...)                                                        \
   (dtype == AVQ_BF16 ? (d == 64 ? avq::launch<avq::bf16, 64>(__VA_ARGS__)               \
@@ -571,20 +597,9 @@ avq_status_t avq_cache_attention_fwd(avq_dtype_t dtype, avq_cache_t format, int3
                                      float* lse, void* workspace, int64_t workspace_bytes,
                                      void* stream) {
   const char* name = "avq_cache_attention_fwd";
-  avq_status_t st = check_heads(name, dtype, S, Hq, Hkv, d);
-  if (st == AVQ_OK) st = check_cache(name, format, n_pages, page_size, max_pages);
-  if (st == AVQ_OK) st = check_stride(name, "q_stride", dtype, q_stride, Hq, d);
-  if (st == AVQ_OK) st = check_scale(name, scale);
+  const avq_status_t st = check_cached(name, dtype, format, S, n_q, Hq, Hkv, d, n_pages, page_size,
+                                       max_pages, scale, q_stride);
   if (st != AVQ_OK) return st;
-  if (n_q < 1) return fail(AVQ_ERR_INVALID_ARG, "%s: n_q=%d must be positive", name, n_q);
-  if (n_q > kMaxDrafts)
-    return fail(AVQ_ERR_UNSUPPORTED, "%s: n_q=%d: at most %d tokens per sequence", name, n_q,
-                kMaxDrafts);
-  if (cache_segments(S, n_q, Hq, Hkv) >= kMaxBlocks)
-    return fail(AVQ_ERR_UNSUPPORTED, "%s: S=%d sequences of Hq=%d, Hkv=%d heads: too many", name, S,
-                Hq, Hkv);
-  if ((int64_t)S * (((int64_t)max_pages * page_size + 127) / 128) > (1LL << 30))
-    return fail(AVQ_ERR_UNSUPPORTED, "%s: S * max_pages * page_size: at most 2^37 positions", name);
   const bool divided = (int64_t)max_pages * page_size > AVQ_CACHE_UNDIVIDED;
   if (!Q || !cache || !lens || !block_table || !Y || (divided && !workspace))
     return null_pointer(name);
@@ -707,6 +722,48 @@ avq_status_t avq_cross_attention_bwd(avq_dtype_t dtype, int32_t S, int32_t Tq, i
                               k_stride, V, v_stride, cu_q, cu_k, mask, Y, lse, dY, dy_stride, dQ, dK,
                               dV, workspace, s),
                   "avq_cross_attention_bwd launch");
+}
+
+int64_t avq_cache_prefix_attention_workspace(int32_t S, int32_t n_groups, int32_t n_q, int32_t Hq,
+                                             int32_t Hkv, int32_t d) {
+  if (avq_cache_attention_workspace(S, n_q, Hq, Hkv, d) < 0 ||
+      !groups_fit(S, n_groups, n_q, Hq, Hkv))
+    return -1;
+  return (int64_t)avq::prefix_attention_workspace(S, n_groups, n_q, Hq, Hkv, d);
+}
+
+avq_status_t avq_cache_prefix_attention_fwd(avq_dtype_t dtype, avq_cache_t format, int32_t S,
+                                            int32_t n_groups, int32_t n_q, int32_t Hq, int32_t Hkv,
+                                            int32_t d, int32_t n_pages, int32_t page_size,
+                                            int32_t max_pages, float scale, const void* Q,
+                                            int64_t q_stride, const void* cache,
+                                            const int32_t* lens, const int32_t* block_table,
+                                            const int32_t* cu_groups, const int32_t* shared,
+                                            void* Y, float* lse, void* workspace,
+                                            int64_t workspace_bytes, void* stream) {
+  const char* name = "avq_cache_prefix_attention_fwd";
+  avq_status_t st = check_cached(name, dtype, format, S, n_q, Hq, Hkv, d, n_pages, page_size,
+                                 max_pages, scale, q_stride);
+  if (st != AVQ_OK) return st;
+  if (n_groups < 1)
+    return fail(AVQ_ERR_INVALID_ARG, "%s: n_groups=%d must be positive", name, n_groups);
+  if (!groups_fit(S, n_groups, n_q, Hq, Hkv))
+    return fail(AVQ_ERR_UNSUPPORTED, "%s: n_groups=%d groups of S=%d sequences, Hkv=%d heads: too many",
+                name, n_groups, S, Hkv);
+  if (!Q || !cache || !lens || !block_table || !cu_groups || !shared || !Y)
+    return null_pointer(name);
+  if (!aligned16(Q) || !aligned16(cache) || !aligned16(lens) || !aligned16(block_table) ||
+      !aligned16(cu_groups) || !aligned16(shared) || !aligned16(Y) || !aligned16(lse) ||
+      !aligned16(workspace))
+    return misaligned(name);
+  st = check_workspace(name, avq_cache_prefix_attention_workspace(S, n_groups, n_q, Hq, Hkv, d),
+                       workspace, workspace_bytes);
+  if (st != AVQ_OK) return st;
+  const avq::CacheShape c{format == AVQ_CACHE_FP4, n_pages, page_size, max_pages, Hkv};
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  return from_hip(AVQ_BY_TYPE(launch_prefix_attention, c, S, n_groups, n_q, Hq, scale, Q, q_stride,
+                              cache, lens, block_table, cu_groups, shared, Y, lse, workspace, s),
+                  "avq_cache_prefix_attention_fwd launch");
 }
 
 }  // extern "C"

@@ -80,6 +80,13 @@ hipError_t launch_cross_attention_bwd(int S, int Tq, int Tk, int Hq, int Hkv, fl
                                       const uint8_t* mask, const void* Y, const float* lse,
                                       const void* dY, int64_t dy_stride, void* dQ, void* dK,
                                       void* dV, void* workspace, hipStream_t stream);
+size_t prefix_attention_workspace(int S, int n_groups, int n_q, int Hq, int Hkv, int d);
+template <typename T, int D>
+hipError_t launch_prefix_attention(const CacheShape& c, int S, int n_groups, int n_q, int Hq,
+                                   float scale, const void* Q, int64_t q_stride, const void* cache,
+                                   const int32_t* lens, const int32_t* table,
+                                   const int32_t* cu_groups, const int32_t* shared, void* Y,
+                                   float* lse, void* workspace, hipStream_t stream);
 size_t cache_attention_workspace(int S, int n_q, int Hq, int Hkv, int d);
 template <typename T, int D>
 hipError_t launch_cache_attention(const CacheShape& c, int S, int n_q, int Hq, float scale,

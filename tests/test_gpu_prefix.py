@@ -1,0 +1,287 @@
+"""cache_prefix_attention_fwd against the 64-bit reference, every sequence over its own
+pages (MI355X)."""
+import math
+
+import pytest
+import torch
+
+from paper_2607_12789_amd import avq
+from tests.serving_reference import check_attention, read_cache, views
+
+pytestmark = pytest.mark.gpu
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+class Setup:
+    """groups: (shared positions, lengths of the group's sequences); a sequence's
+    shared positions are those it has of them. Slots behind the lengths hold anything."""
+
+    def __init__(self, groups, Hq, Hkv, d, dtype, fp4=False, ps=16, n_q=1, seed=0):
+        self.__dict__.update(Hq=Hq, Hkv=Hkv, d=d, dtype=dtype, fp4=fp4, ps=ps, n_q=n_q)
+        g = torch.Generator().manual_seed(seed)
+        self.lens = [n for _, lens in groups for n in lens]
+        self.S = len(self.lens)
+        rows, copies, next_page = [], [], 0
+        for shared, lens in groups:
+            whole = []
+            holder, held = None, 0
+            for n in lens:
+                common = min(n, shared)
+                row = []
+                for j in range(-(-n // ps)):
+                    if (j + 1) * ps <= common:
+                        if j == len(whole):
+                            whole.append(next_page)
+                            next_page += 1
+                        row.append(whole[j])
+                    else:
+                        row.append(next_page)
+                        next_page += 1
+                rows.append(row)
+                # positions of a page that the sequences share only in part
+                for j, page in enumerate(row):
+                    part = min(min(common, held) - j * ps, ps)
+                    if part > 0 and holder is not None and j < len(holder) and page != holder[j]:
+                        copies.append((holder[j], page, part))
+                if holder is None or len(row) > len(holder):
+                    holder, held = row, n
+        self.n_pages = next_page + 2
+        order = torch.randperm(self.n_pages, generator=g).tolist()
+        self.table = torch.full((self.S, max(1, max(map(len, rows)))), -7, dtype=torch.int32)
+        for i, row in enumerate(rows):
+            self.table[i, :len(row)] = torch.tensor([order[p] for p in row], dtype=torch.int32)
+        E = avq.cache_page_bytes(dtype, ps, d, fp4)
+        self.cache = torch.randint(0, 256, (self.n_pages, Hkv, E), generator=g, dtype=torch.uint8)
+        self.cache.view(-1)[::3] = 0xff  # as bf16 or fp32 also infinities and NaN
+        self.names = [("Kc", "Ks"), ("Vc", "Vs")] if fp4 else [("K",), ("V",)]
+        w = self.views()
+        for row, n in zip(rows, self.lens):
+            for j, page in enumerate(row):
+                slots = torch.arange(min(n - j * ps, ps))
+                for name, x in w.items():
+                    at = self.at(x, order[page], slots, name)
+                    if name in ("Ks", "Vs"):
+                        v = torch.randint(124, 128, at.shape, generator=g, dtype=torch.uint8)
+                    elif fp4:
+                        v = torch.randint(0, 256, at.shape, generator=g, dtype=torch.uint8)
+                    else:
+                        v = torch.randn(at.shape, generator=g).to(dtype)
+                    self.put(x, order[page], slots, name, v)
+        for a, b, n in copies:
+            slots = torch.arange(n)
+            for name, x in w.items():
+                self.put(x, order[b], slots, name, self.at(x, order[a], slots, name))
+        self.Q = torch.randn(self.S, n_q, Hq, d, generator=g).to(dtype)
+        self.cu = torch.tensor([0] + [len(x) for _, x in groups]).cumsum(0).int()
+        self.shared = torch.tensor([n for n, _ in groups], dtype=torch.int32)
+
+    def views(self):
+        return views(self.cache, self.dtype, self.fp4, self.ps, self.d)
+
+    @staticmethod
+    def at(x, page, slots, name):
+        return x[page, :, slots] if name[0] == "K" else x[page, :, slots // 8, :, slots % 8]
+
+    @staticmethod
+    def put(x, page, slots, name, v):
+        if name[0] == "K":
+            x[page, :, slots] = v
+        else:
+            x[page, :, slots // 8, :, slots % 8] = v
+
+    def run(self, scale=0.2, **kw):
+        dev = [x.cuda() for x in (self.Q, self.cache, self.table,
+                                  torch.tensor(self.lens, dtype=torch.int32), self.cu, self.shared)]
+        Y, lse = avq.cache_prefix_attention_fwd(*dev, self.ps, scale, fp4=self.fp4, with_lse=True,
+                                                **kw)
+        torch.cuda.synchronize()
+        return Y.cpu(), lse.cpu()
+
+    def check(self, Y, lse, scale=0.2, lens=None):
+        for s, n in enumerate(lens or self.lens):
+            n = min(max(n, 0), self.table.shape[1] * self.ps)
+            K, V, ok = read_cache(self.cache, self.table, s, n, self.dtype, self.fp4, self.ps,
+                                  self.d)
+            for i in range(self.n_q):
+                seen = max(0, n - (self.n_q - 1 - i))
+                keep = ok.clone()
+                keep[seen:] = False
+                for h in range(self.Hq):
+                    k = h // (self.Hq // self.Hkv)
+                    check_attention(Y[s, i, h][None], lse[s, i, h][None], self.Q[s, i, h][None],
+                                    K[k, keep], V[k, keep], scale, torch.tensor([int(keep.sum())]),
+                                    f"sequence {s} token {i} head {h}")
+
+
+GROUPS = [
+    [(40, [41, 45, 70])],                               # ends inside a page, and an octet
+    [(64, [65, 200, 64, 80])],                          # one sequence has nothing else
+    [(33, [40, 90]), (0, [7, 30]), (128, [129, 300, 150])],
+    [(100, [101]), (50, [60, 61])],                     # one sequence alone shares nothing
+    [(3, [4, 5, 9]), (8, [9, 8])],
+    [(300, [301, 20, 0, 310])],                         # shorter than the shared positions, idle
+    [(300, [0, 310, 320])],                             # the first one is idle
+    [(500, [200, 510, 700])],                           # the first one holds only some of them
+    [(1000, [1001, 1100, 1300])],                       # divided
+]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("fp4", [False, True])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("groups", GROUPS)
+def test_groups(groups, d, fp4, dtype):
+    s = Setup(groups, 4, 2, d, dtype, fp4, 16)
+    s.check(*s.run())
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("fp4", [False, True])
+@pytest.mark.parametrize("ps", [16, 32, 64, 256])
+def test_pages(ps, fp4, dtype):
+    s = Setup([(130, [131, 200, 300]), (257, [260, 259])], 2, 1, 64, dtype, fp4, ps, seed=1)
+    s.check(*s.run())
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("fp4", [False, True])
+@pytest.mark.parametrize("Hq,Hkv,n_q", [(1, 1, 1), (7, 1, 3), (6, 6, 2), (8, 1, 5), (12, 4, 16),
+                                        (32, 1, 4), (16, 2, 3)])
+def test_heads_and_drafts(Hq, Hkv, n_q, fp4, dtype):
+    """Up to 128 rows a sequence, several row tiles; tokens see up to their own place,
+    also where that lies in the shared positions."""
+    s = Setup([(90, [91, 95, 140]), (40, [40, 41, 60])], Hq, Hkv, 64, dtype, fp4, 16, n_q, seed=2)
+    s.check(*s.run())
+
+
+@pytest.mark.parametrize("fp4", [False, True])
+def test_many_sequences(fp4):
+    """More rows than a tile holds, in one group; groups that begin inside a tile."""
+    groups = [(70, [71 + i % 5 for i in range(50)]), (33, [34 + i for i in range(9)]),
+              (16, [17] * 40)]
+    s = Setup(groups, 4, 1, 64, BF16, fp4, 16, seed=3)
+    s.check(*s.run())
+
+
+def test_more_groups_than_fit_in_lds():
+    groups = [(20 + i % 3, [24 + i % 7, 25]) for i in range(300)]
+    s = Setup(groups, 1, 1, 64, BF16, False, 16, seed=4)
+    s.check(*s.run())
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_sequences_of_no_group(dtype):
+    """Before the first group, behind the last, and empty groups between them."""
+    s = Setup([(40, [41, 50]), (64, [70, 80, 90]), (30, [33, 35])], 2, 1, 64, dtype, False, 16,
+              seed=5)
+    s.cu = torch.tensor([2, 2, 5, 5, 5], dtype=torch.int32)
+    s.shared = torch.tensor([10 ** 9, 64, 77, -4], dtype=torch.int32)
+    s.check(*s.run())
+
+
+def test_bounds_outside_the_batch():
+    s = Setup([(40, [41, 50]), (64, [70, 80, 90])], 2, 1, 64, BF16, False, 16, seed=6)
+    s.cu = torch.tensor([-3, 2, 1000], dtype=torch.int32)
+    s.shared = torch.tensor([40, 64], dtype=torch.int32)
+    s.check(*s.run())
+    s.shared = torch.tensor([-5, -1], dtype=torch.int32)
+    s.check(*s.run())
+
+
+@pytest.mark.parametrize("fp4", [False, True])
+def test_positions_without_a_page(fp4):
+    """A shared page that is none takes no part, for any sequence; lengths beyond the
+    table are taken as its end, and negative ones as 0."""
+    s = Setup([(96, [100, 120, 110])], 4, 2, 64, BF16, fp4, 16, seed=7)
+    s.table[:, 1], s.table[:, 4] = 10 ** 6, -1
+    s.check(*s.run())
+    s = Setup([(96, [128, 120, 110])], 4, 2, 64, BF16, fp4, 16, seed=8)
+    lens = list(s.lens)
+    s.lens = [10 ** 9, 120, -5]
+    Y, lse = s.run()
+    s.check(Y, lse, lens=[128, 120, 0])
+    s.lens = lens
+
+
+@pytest.mark.parametrize("fp4", [False, True])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_large_logits(dtype, fp4):
+    """Logits of hundreds: one part outweighs the other."""
+    s = Setup([(200, [230, 260, 201])], 4, 2, 128, dtype, fp4, 64, seed=9)
+    s.check(*s.run(scale=8.0), scale=8.0)
+
+
+def test_same_as_without_groups():
+    """Against cache_attention_fwd on the same arguments: each within the bounds, and
+    for groups of one sequence the same bits."""
+    s = Setup([(0, [50, 300, 0, 700])], 4, 2, 64, BF16, False, 16, seed=10)
+    lens = torch.tensor(s.lens, dtype=torch.int32).cuda()
+    args = [x.cuda() for x in (s.Q, s.cache, s.table)]
+    s.cu, s.shared = torch.arange(5).int(), torch.full((4,), 30, dtype=torch.int32)
+    Y, lse = s.run()
+    y, l = avq.cache_attention_fwd(*args, lens, 16, 0.2, with_lse=True)
+    s.check(y.cpu(), l.cpu())
+    s.check(Y, lse)
+
+
+def test_strided_queries_and_untouched_cache():
+    s = Setup([(90, [91, 95, 140])], 4, 2, 64, BF16, False, 16, 2, seed=11)
+    wide = torch.randn(3, 2, 6, 64).to(BF16).cuda()
+    wide[:, :, :4] = s.Q.cuda()
+    cache = s.cache.cuda()
+    lens = torch.tensor(s.lens, dtype=torch.int32).cuda()
+    Y, lse = avq.cache_prefix_attention_fwd(wide[:, :, :4], cache, s.table.cuda(), lens, s.cu.cuda(),
+                                            s.shared.cuda(), 16, 0.2, with_lse=True)
+    s.check(Y.cpu(), lse.cpu())
+    assert torch.equal(cache.cpu(), s.cache)
+
+
+def test_refusals_on_the_gpu():
+    s = Setup([(40, [41, 50])], 2, 1, 64, BF16)
+    lens = torch.tensor(s.lens, dtype=torch.int32)
+    names = ("Q", "cache", "block_table", "lens", "cu_groups", "shared")
+    good = dict(zip(names, (x.cuda() for x in (s.Q, s.cache, s.table, lens, s.cu, s.shared))))
+    for change in (dict(Q=s.Q.cuda()[0]), dict(lens=lens), dict(shared=s.shared.cuda().long()),
+                   dict(cu_groups=s.cu.cuda()[:1]), dict(shared=s.shared.cuda()[None]),
+                   dict(Y=torch.empty(1, device="cuda")), dict(lens=lens.cuda()[:1])):
+        with pytest.raises(ValueError):
+            avq.cache_prefix_attention_fwd(**{**good, **change}, page_size=16, scale=0.2)
+    for kw in (dict(workspace=torch.empty(64, dtype=torch.uint8, device="cuda")),
+               dict(scale=-1.0)):
+        with pytest.raises(avq.AvqError):
+            avq.cache_prefix_attention_fwd(**good, page_size=16, **{"scale": 0.2, **kw})
+
+
+def test_graph():
+    """Captured once, replayed while the sequences grow."""
+    s = Setup([(300, [340, 600, 350]), (64, [90, 100])], 4, 2, 64, BF16, False, 16, seed=12)
+    dev = [x.cuda() for x in (s.Q, s.cache, s.table)]
+    lens = torch.tensor([301, 305, 302, 65, 70], dtype=torch.int32, device="cuda")
+    groups = [s.cu.cuda(), s.shared.cuda()]
+    call = lambda: avq.cache_prefix_attention_fwd(*dev, lens, *groups, 16, 0.2, with_lse=True)
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = call()
+    for n in range(4):
+        lens += 5
+        graph.replay()
+        torch.cuda.synchronize()
+        s.check(out[0].cpu(), out[1].cpu(), lens=lens.tolist())
+        eager = call()
+        assert torch.equal(out[0], eager[0]) and torch.equal(out[1], eager[1])
+
+
+def test_two_streams():
+    sets = [Setup([(300, [340, 600, 350])], 4, 2, 64, BF16, fp4, 16, seed=13) for fp4 in (0, 1)]
+    want = [s.run() for s in sets]
+    streams = [torch.cuda.Stream() for _ in sets]
+    dev = [[x.cuda() for x in (s.Q, s.cache, s.table, torch.tensor(s.lens, dtype=torch.int32), s.cu,
+                               s.shared)] for s in sets]
+    torch.cuda.synchronize()
+    got = [avq.cache_prefix_attention_fwd(*x, 16, 0.2, fp4=s.fp4, with_lse=True, stream=st)
+           for s, x, st in zip(sets, dev, streams)]
+    torch.cuda.synchronize()
+    for a, b in zip(want, got):
+        assert torch.equal(a[0], b[0].cpu()) and torch.equal(a[1], b[1].cpu())
