@@ -626,10 +626,10 @@ avq_status_t avq_cross_attention_fwd(avq_dtype_t dtype, int32_t S, int32_t Tq, i
 /* Bytes of the workspaces of the cross attention calls (0: none needed, -1:
  * unsupported sizes). Their contents need not be set and mean nothing afterwards;
  * calls that may run at the same time need one each. */
-int64_t avq_cross_attention_workspace(int32_t S, int32_t Tq, int32_t Tk, int32_t Hq, int32_t Hkv,
-                                      int32_t d);
-int64_t avq_cross_attention_bwd_workspace(int32_t S, int32_t Tq, int32_t Tk, int32_t Hq,
-                                          int32_t Hkv, int32_t d);
+int64_t avq_cross_attention_workspace(avq_dtype_t dtype, int32_t S, int32_t Tq, int32_t Tk,
+                                      int32_t Hq, int32_t Hkv, int32_t d);
+int64_t avq_cross_attention_bwd_workspace(avq_dtype_t dtype, int32_t S, int32_t Tq, int32_t Tk,
+                                          int32_t Hq, int32_t Hkv, int32_t d);
 
 /*
  * avq_cross_attention_bwd - gradients of avq_cross_attention_fwd's Y with respect

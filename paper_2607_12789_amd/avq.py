@@ -96,10 +96,11 @@ def lib():
                                               + [i64, vp])
         L.avq_cache_prefix_attention_fwd.argtypes = [ci, ci] + [i32] * 9 + [cf, vp, i64] + [vp] * 8 + [
             i64, vp]
-        for name in ("avq_cross_attention_workspace", "avq_cross_attention_bwd_workspace",
-                     "avq_cache_prefix_attention_workspace"):
-            getattr(L, name).argtypes = [i32] * 6
+        for name in ("avq_cross_attention_workspace", "avq_cross_attention_bwd_workspace"):
+            getattr(L, name).argtypes = [ci] + [i32] * 6
             getattr(L, name).restype = i64
+        L.avq_cache_prefix_attention_workspace.argtypes = [i32] * 6
+        L.avq_cache_prefix_attention_workspace.restype = i64
         for name in ("avq_prompt_attention_fwd", "avq_cache_append", "avq_cache_gather",
                      "avq_cache_attention_fwd", "avq_rotate_axes", "avq_cross_attention_fwd",
                      "avq_cross_attention_bwd", "avq_cache_prefix_attention_fwd"):
@@ -740,13 +741,15 @@ def rotate_axes(Q, K, pos, cos, sin, axis, interleaved: bool = False, inverse: b
     return Q_out, K_out
 
 
-def cross_attention_workspace(S: int, Tq: int, Tk: int, Hq: int, Hkv: int, d: int,
+def cross_attention_workspace(dtype, S: int, Tq: int, Tk: int, Hq: int, Hkv: int, d: int,
                               backward: bool = False) -> int:
     """Bytes of the workspace of ``cross_attention_fwd`` (0: none needed) or
     ``cross_attention_bwd``."""
+    if dtype not in _DTYPES:
+        raise ValueError(f"unsupported dtype {dtype}: use float32 or bfloat16")
     L = lib()
     n = (L.avq_cross_attention_bwd_workspace if backward else L.avq_cross_attention_workspace)(
-        S, Tq, Tk, Hq, Hkv, d)
+        _DTYPES[dtype], S, Tq, Tk, Hq, Hkv, d)
     if n < 0:
         raise ValueError(f"unsupported sizes S={S} Tq={Tq} Tk={Tk} Hq={Hq} Hkv={Hkv} d={d}")
     return n
@@ -803,7 +806,7 @@ def cross_attention_fwd(Q, K, V, cu_q, cu_k, scale: float, mask=None, Y=None,
     if workspace is not None:
         _dev(workspace, "workspace", torch.uint8)
     else:
-        n = _cross_workspace_of(S, Tq, Tk, Hq, Hkv, d)
+        n = _cross_workspace_of(Q.dtype, S, Tq, Tk, Hq, Hkv, d)
         if n:
             workspace = _empty(stream, (n,), torch.uint8, Q.device)
     at = Q.get_device()
@@ -852,7 +855,7 @@ def cross_attention_bwd(dY, Q, K, V, Y, lse, cu_q, cu_k, scale: float, mask=None
     if workspace is not None:
         _dev(workspace, "workspace", torch.uint8)
     else:
-        n = _cross_workspace_of(S, Tq, Tk, Hq, Hkv, d, True)
+        n = _cross_workspace_of(Q.dtype, S, Tq, Tk, Hq, Hkv, d, True)
         workspace = _empty(stream, (n,), torch.uint8, Q.device)
     at = Q.get_device()
     if (not dY.get_device() == K.get_device() == V.get_device() == Y.get_device()

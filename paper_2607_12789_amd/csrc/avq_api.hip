@@ -400,8 +400,8 @@ bool cross_tiles_fit(int32_t S, int32_t Tq, int32_t Tk, int32_t Hq, int32_t Hkv)
   const int64_t rows = (int64_t)Tq * (Hq / Hkv);
   return (rows / 128 + S) * Hkv < kMaxBlocks && ((int64_t)Tk / 128 + S) * Hkv < kMaxBlocks;
 }
-bool cross_sizes(int32_t S, int32_t Tq, int32_t Tk, int32_t Hq, int32_t Hkv, int32_t d) {
-  return S >= 1 && S <= (1 << 20) && Hq >= 1 && Hkv >= 1 && Hq <= kMaxHeads && Hq % Hkv == 0 &&
+bool cross_sizes(avq_dtype_t dtype, int32_t S, int32_t Tq, int32_t Tk, int32_t Hq, int32_t Hkv, int32_t d) {
+  return (dtype == AVQ_F32 || dtype == AVQ_BF16) && S >= 1 && S <= (1 << 20) && Hq >= 1 && Hkv >= 1 && Hq <= kMaxHeads && Hq % Hkv == 0 &&
          (d == 64 || d == 128) && Tq >= 0 && Tk >= 0 && Tq <= (1 << 24) && Tk <= (1 << 24) &&
          cross_tiles_fit(S, Tq, Tk, Hq, Hkv);
 }
@@ -655,11 +655,10 @@ avq_status_t avq_rotate_axes(avq_dtype_t dtype, int32_t T, int32_t Hq, int32_t H
                   "avq_rotate_axes launch");
 }
 
-int64_t avq_cross_attention_workspace(int32_t S, int32_t Tq, int32_t Tk, int32_t Hq, int32_t Hkv,
-                                      int32_t d) {
-  return cross_sizes(S, Tq, Tk, Hq, Hkv, d)
-             ? (int64_t)avq::cross_attention_workspace(S, Tq, Tk, Hq, Hkv, d)
-             : -1;
+int64_t avq_cross_attention_workspace(avq_dtype_t dtype, int32_t S, int32_t Tq, int32_t Tk,
+                                      int32_t Hq, int32_t Hkv, int32_t d) {
+  if (!cross_sizes(dtype, S, Tq, Tk, Hq, Hkv, d)) return -1;
+  return (int64_t)AVQ_BY_TYPE(cross_attention_workspace, S, Tq, Tk, Hq, Hkv);
 }
 
 avq_status_t avq_cross_attention_fwd(avq_dtype_t dtype, int32_t S, int32_t Tq, int32_t Tk,
@@ -676,7 +675,7 @@ avq_status_t avq_cross_attention_fwd(avq_dtype_t dtype, int32_t S, int32_t Tq, i
   if (!aligned16(Q) || !aligned16(K) || !aligned16(V) || !aligned16(cu_q) || !aligned16(cu_k) ||
       !aligned16(Y) || !aligned16(lse) || !aligned16(workspace))
     return misaligned(name);
-  st = check_workspace(name, avq_cross_attention_workspace(S, Tq, Tk, Hq, Hkv, d), workspace,
+  st = check_workspace(name, avq_cross_attention_workspace(dtype, S, Tq, Tk, Hq, Hkv, d), workspace,
                        workspace_bytes);
   if (st != AVQ_OK) return st;
   if (Tq == 0) return ok();
@@ -686,11 +685,10 @@ avq_status_t avq_cross_attention_fwd(avq_dtype_t dtype, int32_t S, int32_t Tq, i
                   "avq_cross_attention_fwd launch");
 }
 
-int64_t avq_cross_attention_bwd_workspace(int32_t S, int32_t Tq, int32_t Tk, int32_t Hq,
-                                          int32_t Hkv, int32_t d) {
-  return cross_sizes(S, Tq, Tk, Hq, Hkv, d)
-             ? (int64_t)avq::cross_attention_bwd_workspace(S, Tq, Tk, Hq, Hkv, d)
-             : -1;
+int64_t avq_cross_attention_bwd_workspace(avq_dtype_t dtype, int32_t S, int32_t Tq, int32_t Tk,
+                                          int32_t Hq, int32_t Hkv, int32_t d) {
+  if (!cross_sizes(dtype, S, Tq, Tk, Hq, Hkv, d)) return -1;
+  return (int64_t)AVQ_BY_TYPE(cross_attention_bwd_workspace, S, Tq, Tk, Hq, Hkv);
 }
 
 avq_status_t avq_cross_attention_bwd(avq_dtype_t dtype, int32_t S, int32_t Tq, int32_t Tk,
@@ -713,7 +711,7 @@ avq_status_t avq_cross_attention_bwd(avq_dtype_t dtype, int32_t S, int32_t Tq, i
       !aligned16(lse) || !aligned16(cu_q) || !aligned16(cu_k) || !aligned16(dQ) ||
       !aligned16(dK) || !aligned16(dV) || !aligned16(workspace))
     return misaligned(name);
-  st = check_workspace(name, avq_cross_attention_bwd_workspace(S, Tq, Tk, Hq, Hkv, d), workspace,
+  st = check_workspace(name, avq_cross_attention_bwd_workspace(dtype, S, Tq, Tk, Hq, Hkv, d), workspace,
                        workspace_bytes);
   if (st != AVQ_OK) return st;
   if (Tq == 0 && Tk == 0) return ok();

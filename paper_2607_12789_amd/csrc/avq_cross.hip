@@ -26,8 +26,6 @@ namespace avq {
 
 namespace {
 
-constexpr int kLeastTiles = 4;  // tiles of 32 states that a workgroup takes, at least
-
 template <typename T, int D>
 constexpr int kPerCu = Elem<T>::kBf16 && D == 128 ? 3 : 2;  // waves per SIMD, at least
 
@@ -43,7 +41,7 @@ void cross_kernel(CrossArgs a) {
   const int hkv = blockIdx.x % a.Hkv, tile = blockIdx.x / a.Hkv;
   CrossTile t;
   if (!find_cross_tile<false>(a, tile, lane, t)) return;
-  const int n_tiles = (t.Lk + 31) / 32, splits = splits_of<kLeastTiles>(a, n_tiles);
+  const int n_tiles = (t.Lk + 31) / 32, splits = splits_of(a, n_tiles);
   const int split = blockIdx.y;
   if (split >= splits) return;
   const int t_begin = (int)((long long)n_tiles * split / splits);
@@ -140,76 +138,34 @@ void cross_kernel(CrossArgs a) {
 
   l = add_xor<32>(l);
   if (!fused) ms = m * a.scale_log2;
-  if (splits > 1) {
-    float* part = cross_part(a, tile, hkv, split, cross_part_floats(D));
-    if (h == 0) {
-      part[kCrossTile * D + 32 * wave + c] = ms;
-      part[kCrossTile * (D + 1) + 32 * wave + c] = l;
-    }
-    if (has_row) store_lanes<D>(part, wave, lane, o);
-    return;
-  }
   if (!has_row) return;
   const size_t at = (size_t)qi * a.Hq + hq;
+  if (splits > 1) {
+    const size_t rows_all = (size_t)a.Tq * a.Hq, part = split * rows_all + at;
+    store_part<D>(a.parts + part * D, h, o);
+    if (h == 0) {
+      a.parts[a.splits * rows_all * D + part] = ms;
+      a.parts[a.splits * rows_all * (D + 1) + part] = l;
+    }
+    return;
+  }
   store_row<T, D>(static_cast<T*>(a.Y) + at * D, h, l > 0.f ? 1.f / l : 0.f, o);
   if (a.lse && h == 0) a.lse[at] = l > 0.f ? (ms + log2_hw(l)) * kLn2 : -INFINITY;
 }
 
-// Joins the parts of a tile's rows (one piece of 4 columns per thread).
-template <typename T, int D>
-__global__ __launch_bounds__(256) void cross_join_kernel(CrossArgs a) {
-  const int hkv = blockIdx.x % a.Hkv, tile = blockIdx.x / a.Hkv;
-  CrossTile t;
-  if (!find_cross_tile<false>(a, tile, threadIdx.x % kWave, t)) return;
-  const int n = splits_of<kLeastTiles>(a, (t.Lk + 31) / 32);
-  if (n == 1) return;
-  const int piece = blockIdx.y * 256 + threadIdx.x, q = piece / kWave % (D / 8);
-  const int r = 32 * (piece / kWave / (D / 8)) + piece % 32;
-  const int d0 = 8 * q + 4 * (piece % kWave / 32);
-  const int row = t.lt * kCrossTile + r;
-  if (row >= t.Lq * a.G) return;
-  const float* part = cross_part(a, tile, hkv, 0, cross_part_floats(D));
-  float m = kMaxFloor, l = 0.f;
-#pragma unroll 8
-  for (int i = 0; i < n; ++i)
-    m = fmaxf(m, part[i * cross_part_floats(D) + kCrossTile * D + r]);
-  f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll 8
-  for (int i = 0; i < n; ++i) {
-    const float* p = part + i * cross_part_floats(D);
-    const float f = exp2_hw(p[kCrossTile * D + r] - m);
-    l = fmaf(f, p[kCrossTile * (D + 1) + r], l);
-    acc += f * *reinterpret_cast<const f32x4*>(p + 4 * piece);
-  }
-  const float inv = l > 0.f ? 1.f / l : 0.f;
-  const size_t at = (size_t)(t.qa + row / a.G) * a.Hq + hkv * a.G + row % a.G;
-  T* y = static_cast<T*>(a.Y) + at * D + d0;
-  if constexpr (Elem<T>::kBf16)
-    *reinterpret_cast<bf16x4*>(y) = bf16x4{(bf16)(acc[0] * inv), (bf16)(acc[1] * inv),
-                                           (bf16)(acc[2] * inv), (bf16)(acc[3] * inv)};
-  else
-    *reinterpret_cast<f32x4*>(y) = acc * inv;
-  if (a.lse && d0 == 0) a.lse[at] = l > 0.f ? (m + log2_hw(l)) * kLn2 : -INFINITY;
-}
-
 long long tiles_of(long long rows, int S) { return rows / kCrossTile + S; }
 
-// Workgroups that share a tile's states: as many as fill the device, the sources'
-// mean lengths standing for all.
-int splits_for(int S, int Tq, int Tk, int Hq, int Hkv) {
-  const long long rows = std::max(1LL, (long long)Tq * (Hq / Hkv) / S);
-  const long long own = (rows + kCrossTile - 1) / kCrossTile * S * Hkv;
-  const long long most = std::max(1LL, (long long)Tk / S / (32 * kLeastTiles));
-  return (int)std::min({std::max(1LL, 768 / own), most, 64LL});
+template <typename T>
+CrossSplit split_for(int S, int Tq, int Tk, int Hq, int Hkv) {
+  return cross_split((long long)Tq * (Hq / Hkv), Tk, S, Hkv, 768, sizeof(T) == 4);
 }
 
 }  // namespace
 
-size_t cross_attention_workspace(int S, int Tq, int Tk, int Hq, int Hkv, int d) {
-  const int splits = splits_for(S, Tq, Tk, Hq, Hkv);
-  if (splits == 1) return 0;
-  return (size_t)tiles_of((long long)Tq * (Hq / Hkv), S) * Hkv * splits * cross_part_floats(d) *
-         sizeof(float);
+template <typename T, int D>
+size_t cross_attention_workspace(int S, int Tq, int Tk, int Hq, int Hkv) {
+  const int splits = split_for<T>(S, Tq, Tk, Hq, Hkv).splits;
+  return splits == 1 ? 0 : (size_t)Tq * Hq * splits * (D + 2) * sizeof(float);
 }
 
 template <typename T, int D>
@@ -223,7 +179,8 @@ hipError_t launch_cross_attention(int S, int Tq, int Tk, int Hq, int Hkv, float 
   a.cu_q = cu_q, a.cu_k = cu_k, a.mask = mask, a.Y = Y, a.lse = lse;
   a.S = S, a.Tq = Tq, a.Tk = Tk, a.Hq = Hq, a.Hkv = Hkv, a.G = Hq / Hkv;
   a.tiles = (int)tiles_of((long long)Tq * a.G, S);
-  a.splits = splits_for(S, Tq, Tk, Hq, Hkv);
+  const CrossSplit split = split_for<T>(S, Tq, Tk, Hq, Hkv);
+  a.per = split.per, a.splits = split.splits;
   a.scale = scale, a.scale_log2 = scale * kLog2e, a.lazy = kLazy / a.scale_log2;
   a.parts = static_cast<float*>(workspace);
   const dim3 grid((unsigned)(a.tiles * Hkv), (unsigned)a.splits);
@@ -233,16 +190,14 @@ hipError_t launch_cross_attention(int S, int Tq, int Tk, int Hq, int Hkv, float 
     hipLaunchKernelGGL((cross_kernel<T, D, false>), grid, dim3(256), 0, stream, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.splits == 1) return e;
-  hipLaunchKernelGGL((cross_join_kernel<T, D>),
-                     dim3((unsigned)(a.tiles * Hkv), kCrossTile * D / 4 / 256), dim3(256), 0, stream,
-                     a);
-  return hipGetLastError();
+  return launch_cross_join<T, D, kJoinSoftmax>(a, stream);
 }
 
 #define AVQ_INSTANCE(T, D)                                                                        \
   template hipError_t launch_cross_attention<T, D>(                                               \
       int, int, int, int, int, float, const void*, int64_t, const void*, int64_t, const void*,    \
-      int64_t, const int32_t*, const int32_t*, const uint8_t*, void*, float*, void*, hipStream_t);
+      int64_t, const int32_t*, const int32_t*, const uint8_t*, void*, float*, void*, hipStream_t);    \
+  template size_t cross_attention_workspace<T, D>(int, int, int, int, int);
 AVQ_INSTANCE(bf16, 64)
 AVQ_INSTANCE(bf16, 128)
 AVQ_INSTANCE(float, 64)

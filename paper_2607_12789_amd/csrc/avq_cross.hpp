@@ -13,6 +13,9 @@
 #include "avq_cache.hpp"
 #include "avq_tiles.hpp"
 
+#include <algorithm>
+#include <type_traits>
+
 namespace avq {
 
 struct CrossArgs {
@@ -28,7 +31,8 @@ struct CrossArgs {
   void *dQ, *dK, *dV;
   int S, Tq, Tk, Hq, Hkv, G;
   uint32_t g_reciprocal;
-  int tiles, splits;  // per key-value head; workgroups that share a tile's work
+  int tiles;          // per key-value head, at most
+  int per, splits;    // steps of 32 that a workgroup takes; workgroups of a tile, at most
   float scale, scale_log2;
   float lazy;  // kLazy / scale_log2
   float* parts;
@@ -61,35 +65,142 @@ __device__ __forceinline__ bool find_cross_tile(const CrossArgs& a, int tile, in
   return t.lt >= 0 && (long long)t.lt * kCrossTile < n;
 }
 
-// Workgroups of a tile that have work: each as many of the n steps as the others,
-// but kLeast at least. The same on the joining side.
-template <int kLeast>
+// Workgroups that share a tile's n steps, each about a.per of them. The same on the
+// joining side.
 __device__ __forceinline__ int splits_of(const CrossArgs& a, int n) {
-  return max(1, min(a.splits, n / kLeast));
+  return max(1, min(a.splits, (n + a.per - 1) / a.per));
 }
 
-// A part of rows: numerators [128][D], then maxima and sums [128]. The numerators
-// lie as the lanes hold them, so that every store and load of a wave covers 1 KB:
-// piece q = 4 i + j of wave w, [w][q][64 lanes][4], are the columns
-// 32 i + 8 j + 4 (lane / 32) + 0 .. 3 of row 32 w + lane % 32.
-__host__ __device__ constexpr size_t cross_part_floats(int D) {
-  return (size_t)kCrossTile * (D + 2);
-}
-// Place of (tile, head)'s first part.
-__device__ __forceinline__ float* cross_part(const CrossArgs& a, int tile, int head, int split,
-                                             size_t floats) {
-  return a.parts + (((size_t)tile * a.Hkv + head) * a.splits + split) * floats;
+// How the work of a kernel's tiles is shared out. The host knows the sources' mean
+// lengths only: with `own` rows (or states) and `others` it runs over per source, W
+// workgroups take equal parts of the whole, but 4 or 8 steps at least. A source of
+// four times the mean length is still divided like that, a longer one in as many
+// parts.
+struct CrossSplit {
+  int per, splits;
+};
+inline CrossSplit cross_split(long long own, long long others, int S, int Hkv, int W, bool wide) {
+  // parts of many rows cost as much as some more steps
+  const int least = !wide && own / S > kCrossTile ? 8 : 4;
+  const long long tiles = ((own + S - 1) / S + kCrossTile - 1) / kCrossTile * S * Hkv;
+  // parts of few rows cost little: twice as many, shorter ones, which lengths of all
+  // kinds leave less uneven
+  if (own / S <= 32) W *= 2;
+  if (tiles >= W) return {least, 1};
+  const long long mean = (others / S + 31) / 32, all = (others + 31) / 32;
+  const long long per = std::max<long long>(least, (tiles * mean + W - 1) / W);
+  const long long most = std::min((all + per - 1) / per, 4 * ((mean + per - 1) / per));
+  return {(int)per, (int)std::max(1LL, std::min(most, 64LL))};
 }
 
+// Parts: rows [splits][rows][D], then, of the forward pass, maxima and sums
+// [splits][rows] each, where row = query * Hq + head (states: state * Hkv + head).
 template <int D>
-__device__ __forceinline__ void store_lanes(float* part, int wave, int lane,
-                                            const f32x16 (&o)[D / 32]) {
+__device__ __forceinline__ void store_part(float* row, int h, const f32x16 (&o)[D / 32]) {
 #pragma unroll
   for (int i = 0; i < D / 32; ++i)
 #pragma unroll
     for (int r = 0; r < 16; r += 4)
-      *reinterpret_cast<f32x4*>(part + ((wave * (D / 8) + 4 * i + r / 4) * kWave + lane) * 4) =
+      *reinterpret_cast<f32x4*>(row + 32 * i + 2 * r + 4 * h) =
           f32x4{o[i][r], o[i][r + 1], o[i][r + 2], o[i][r + 3]};
+}
+
+enum CrossJoin { kJoinSoftmax, kJoinQueries, kJoinStates };
+
+// Joins the parts of one row, in their order: kWaves waves a row, whose lanes take 4
+// columns of 256 / D parts each at a time.
+template <typename T, int D, CrossJoin kWhat, int kWaves>
+__global__ __launch_bounds__(256) void cross_join_kernel(CrossArgs a) {
+  constexpr int TPP = D / 4, PG = kWaves * kWave / TPP, kRows = 4 / kWaves;
+  constexpr bool kStates = kWhat == kJoinStates;
+  __shared__ __attribute__((aligned(16))) float s_acc[kWaves == 1 ? 1 : PG][D];
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  const int heads = kStates ? a.Hkv : a.Hq, T_ = kStates ? a.Tk : a.Tq;
+  const size_t rows = (size_t)T_ * heads;
+  const size_t row = (size_t)blockIdx.x * kRows + (kWaves == 1 ? wave : 0);
+  if (row >= rows) return;
+  const int token = __builtin_amdgcn_readfirstlane((int)(row / heads));
+  const int32_t* cu = kStates ? a.cu_k : a.cu_q;
+  const int s = find_sequence(a.S, token, lane,
+                              [&](int k) { return (long long)min(max(cu[k], 0), T_); });
+  int qa, qb, ka, kb;
+  packed_range(a.cu_q, s, a.Tq, qa, qb);
+  packed_range(a.cu_k, s, a.Tk, ka, kb);
+  if (token < (kStates ? ka : qa) || token >= (kStates ? kb : qb)) return;
+  const int n = splits_of(a, (((kStates ? (qb - qa) * a.G : kb - ka)) + 31) / 32);
+  if (n == 1) return;  // stored already
+  const int pg = (wave % kWaves * kWave + lane) / TPP, d0 = lane % TPP * 4;
+  const float* const ms = a.parts + (size_t)a.splits * rows * D;
+  const float* const ls = ms + (size_t)a.splits * rows;
+  float m = kMaxFloor, l = 0.f;
+  if (kWhat == kJoinSoftmax) {
+    // lane i: the parts i (at most 64), all waves the same
+    const float mine = lane < n ? ms[lane * rows + row] : kMaxFloor;
+    const float sum = lane < n ? ls[lane * rows + row] : 0.f;
+    m = mine;
+#pragma unroll
+    for (int k = 1; k < kWave; k *= 2) m = fmaxf(m, __shfl_xor(m, k, kWave));
+    l = exp2_hw(mine - m) * sum;
+#pragma unroll
+    for (int k = 1; k < kWave; k *= 2) l += __shfl_xor(l, k, kWave);
+  }
+  f32x4 x = f32x4{0.f, 0.f, 0.f, 0.f}, y = x;
+#pragma unroll 4
+  for (int i = pg; i < n; i += PG) {
+    const float* part = a.parts + ((size_t)i * rows + row) * D + d0;
+    const f32x4 v = *reinterpret_cast<const f32x4*>(part);
+    if (kWhat == kJoinSoftmax)
+      x += exp2_hw(ms[i * rows + row] - m) * v;
+    else
+      x += v;
+    if (kStates) y += *reinterpret_cast<const f32x4*>(part + (size_t)a.splits * rows * D);
+  }
+  // the groups of lanes, then the waves
+  auto gather = [&](f32x4& v) {
+#pragma unroll
+    for (int k = TPP; k < kWave; k *= 2)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] += __shfl_xor(v[e], k, kWave);
+    if constexpr (kWaves > 1) {
+      if (lane < TPP) *reinterpret_cast<f32x4*>(&s_acc[wave][d0]) = v;
+      __syncthreads();
+      v = *reinterpret_cast<const f32x4*>(&s_acc[0][d0]);
+#pragma unroll
+      for (int w = 1; w < kWaves; ++w) v += *reinterpret_cast<const f32x4*>(&s_acc[w][d0]);
+      __syncthreads();
+    }
+  };
+  gather(x);
+  if (kStates) gather(y);
+  if (wave % kWaves != 0 || lane >= TPP) return;
+  auto store = [&](void* out, const f32x4& v) {
+    T* o = static_cast<T*>(out) + row * D + d0;
+    if constexpr (Elem<T>::kBf16)
+      *reinterpret_cast<bf16x4*>(o) = bf16x4{(bf16)v[0], (bf16)v[1], (bf16)v[2], (bf16)v[3]};
+    else
+      *reinterpret_cast<f32x4*>(o) = v;
+  };
+  if (kWhat == kJoinSoftmax) {
+    store(a.Y, (l > 0.f ? 1.f / l : 0.f) * x);
+    if (a.lse && lane == 0) a.lse[row] = l > 0.f ? (m + log2_hw(l)) * kLn2 : -INFINITY;
+  } else if (kWhat == kJoinQueries) {
+    store(a.dQ, a.scale * x);
+  } else {
+    store(a.dK, a.scale * x);
+    store(a.dV, y);
+  }
+}
+
+template <typename T, int D, CrossJoin kWhat>
+hipError_t launch_cross_join(const CrossArgs& a, hipStream_t stream) {
+  const size_t rows = kWhat == kJoinStates ? (size_t)a.Tk * a.Hkv : (size_t)a.Tq * a.Hq;
+  if (a.splits > 8)
+    hipLaunchKernelGGL((cross_join_kernel<T, D, kWhat, 4>), dim3((unsigned)rows), dim3(256), 0,
+                       stream, a);
+  else
+    hipLaunchKernelGGL((cross_join_kernel<T, D, kWhat, 1>), dim3((unsigned)((rows + 3) / 4)),
+                       dim3(256), 0, stream, a);
+  return hipGetLastError();
 }
 
 // The lane's columns of one row, times f: 32 i + 2 r + 4 h + 0 .. 3.
@@ -132,17 +243,26 @@ __device__ __forceinline__ void load_row(const T* p, int h,
   }
 }
 
+// A lane's place in a staged tile, computed where it is used: held over the loop, the
+// places of all reads (8 to 32 of them) would take the registers of the products.
+// Others follow from it by exchanging bits, as the swizzles are linear over them:
+// swizzle(r ^ x) = swizzle(r) ^ swizzle(x).
+__device__ __forceinline__ uint32_t place(uint32_t at) {
+  asm volatile("" : "+v"(at));
+  return at;
+}
+
 // acc[row][lane's column] += sum_d tile[row][d] x[d]: 32 staged rows, read row by
 // row (lane c the row c), against the lanes' own ones.
 template <typename T, int D, typename Swizzle>
 __device__ __forceinline__ void row_product(const unsigned char* tile, int lane,
                                             const CrossFrag<T> (&x)[kCrossSteps<T, D>],
                                             Swizzle swizzle, f32x16& acc) {
-  const int h = lane / 32, r = lane % 32;
-  const unsigned char* rowp = tile + r * (D * (int)sizeof(T));
+  constexpr uint32_t kRow = D * sizeof(T);
+  const uint32_t h = lane / 32, r = lane % 32, at = place(r * kRow + 16 * (h ^ swizzle(r)));
 #pragma unroll
-  for (int k = 0; k < D * (int)sizeof(T) / 32; ++k) {
-    const unsigned char* p = rowp + 16 * ((2 * k + h) ^ swizzle(r));
+  for (int k = 0; k < (int)kRow / 32; ++k) {
+    const unsigned char* p = tile + (at ^ (32u * k));
     if constexpr (Elem<T>::kBf16) {
       acc = mfma32(*reinterpret_cast<const bf16x8*>(p), x[k], acc);
     } else {
@@ -160,25 +280,26 @@ __device__ __forceinline__ void row_product(const unsigned char* tile, int lane,
 template <typename T, int D, typename Swizzle>
 __device__ __forceinline__ void column_product(const unsigned char* tile, int lane, const f32x16& w,
                                                Swizzle swizzle, f32x16 (&acc)[D / 32]) {
-  const int h = lane / 32, c = lane % 32;
-  constexpr int kRow = D * (int)sizeof(T);
+  constexpr uint32_t kRow = D * sizeof(T);
+  const uint32_t h = lane / 32, c = lane % 32;
   if constexpr (Elem<T>::kBf16) {
+    // 16 rows a step, 4 h + 0..3 and 8 + 4 h + 0..3 per lane; 32 bytes of 32 columns
+    const uint32_t row = 4 * h + c % 16 / 4;
+    const uint32_t at =
+        place(row * kRow + 16 * ((c / 16 * 2 + c % 4 / 2) ^ swizzle(row)) + 8 * (c % 2));
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {  // 16 rows: 4 h + 0..3 and 8 + 4 h + 0..3 per lane
+    for (int k = 0; k < 2; ++k) {
       bf16x8 p;
 #pragma unroll
       for (int e = 0; e < 8; ++e) p[e] = (bf16)w[8 * k + e];
-      const int row = 16 * k + 4 * h + lane % 16 / 4;
 #pragma unroll
       for (int i = 0; i < D / 32; ++i) {
-        const int unit = 4 * i + lane / 16 % 2 * 2 + lane % 4 / 2;
         bf16x8 v;
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          const int r = row + 8 * e;
           const bf16x4 part = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(
-              (__attribute__((address_space(3))) bf16x4*)(tile + r * kRow +
-                                                          16 * (unit ^ swizzle(r)) + 8 * (lane % 2)));
+              (__attribute__((address_space(3))) bf16x4*)(
+                  tile + (at ^ (64u * i) ^ (16u * swizzle(8 * e))) + (16 * k + 8 * e) * kRow));
 #pragma unroll
           for (int j = 0; j < 4; ++j) v[4 * e + j] = part[j];
         }
@@ -186,13 +307,14 @@ __device__ __forceinline__ void column_product(const unsigned char* tile, int la
       }
     }
   } else {
+    const uint32_t at = place(4 * h * kRow + 16 * (c / 4 ^ swizzle(4 * h)) + 4 * (c % 4));
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      const int row = 8 * (r / 4) + 4 * h + r % 4;
+      const uint32_t row = 8 * (r / 4) + r % 4;
 #pragma unroll
       for (int i = 0; i < D / 32; ++i) {
         const float v = *reinterpret_cast<const float*>(
-            tile + row * kRow + 16 * ((8 * i + c / 4) ^ swizzle(row)) + 4 * (c % 4));
+            tile + (at ^ (128u * i) ^ (16u * swizzle(row))) + row * kRow);
         acc[i] = mfma32(v, w[r], acc[i]);
       }
     }

@@ -24,8 +24,6 @@ namespace avq {
 
 namespace {
 
-constexpr int kLeastTiles = 4;  // tiles of 32 that a workgroup takes, at least
-
 // ---- dQ: owns rows -------------------------------------------------------------------
 
 template <typename T, int D, bool kMask>
@@ -33,14 +31,15 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(Elem<T>::kB
 void cross_dq_kernel(CrossArgs a) {
   constexpr int DT = D / 32, ESZ = sizeof(T), U = D * ESZ / 16, TILE = 32 * D * ESZ;
   constexpr bool kB = Elem<T>::kBf16;
-  __shared__ __attribute__((aligned(16))) unsigned char lds[4 * TILE];  // K0 K1 V0 V1
+  __shared__ __attribute__((aligned(16))) unsigned char k_even[TILE], k_odd[TILE];
+  __shared__ __attribute__((aligned(16))) unsigned char v_even[TILE], v_odd[TILE];
   const int lane = threadIdx.x % kWave;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int h = lane / 32, c = lane % 32;
   const int hkv = blockIdx.x % a.Hkv, tile = blockIdx.x / a.Hkv;
   CrossTile t;
   if (!find_cross_tile<false>(a, tile, lane, t)) return;
-  const int n_tiles = (t.Lk + 31) / 32, splits = splits_of<kLeastTiles>(a, n_tiles);
+  const int n_tiles = (t.Lk + 31) / 32, splits = splits_of(a, n_tiles);
   const int split = blockIdx.y;
   if (split >= splits) return;
   const int t_begin = (int)((long long)n_tiles * split / splits);
@@ -55,20 +54,19 @@ void cross_dq_kernel(CrossArgs a) {
   const T* vbase = static_cast<const T*>(a.V) + (size_t)t.ka * a.v_stride + (size_t)hkv * D;
   auto kswz = [](int r) { return both_swizzle<U, kB>(r); };
   auto vswz = [](int r) { return key_swizzle<U>(r); };
-  auto issue = [&](int i, uint32_t bits) {
+  auto issue = [&](int i, uint32_t bits, unsigned char* k_to, unsigned char* v_to) {
     if (bits == 0) return;
-    const int b = i & 1;
-    stage_states<T, D>(kbase + (size_t)i * 32 * a.k_stride, a.k_stride, bits, lds + b * TILE, wave,
-                       lane, kswz);
-    stage_states<T, D>(vbase + (size_t)i * 32 * a.v_stride, a.v_stride, bits, lds + (2 + b) * TILE,
-                       wave, lane, vswz);
+    stage_states<T, D>(kbase + (size_t)i * 32 * a.k_stride, a.k_stride, bits, k_to, wave, lane,
+                       kswz);
+    stage_states<T, D>(vbase + (size_t)i * 32 * a.v_stride, a.v_stride, bits, v_to, wave, lane,
+                       vswz);
   };
   Seen<kMask> seen;
   uint32_t bits = 0, next = 0;
   if (t_begin < t_end) {
     seen.request(a.mask, t.ka, t.Lk, 32 * t_begin, lane);
     next = seen.bits(t.Lk, 32 * t_begin);
-    issue(t_begin, next);
+    issue(t_begin, next, k_even, v_even);
     seen.request(a.mask, t.ka, t.Lk, 32 * (t_begin + 1), lane);
   }
 
@@ -97,18 +95,17 @@ void cross_dq_kernel(CrossArgs a) {
   f32x16 acc[DT];
 #pragma unroll
   for (int i = 0; i < DT; ++i) acc[i] = f32x16{};
-  for (int i = t_begin; i < t_end; ++i) {
-    const int b = i & 1;
+  auto step = [&](int i, const unsigned char* kt, const unsigned char* vt, unsigned char* k_next,
+                  unsigned char* v_next) {
     bits = next;
     __builtin_amdgcn_s_waitcnt(0);
     __syncthreads();  // tile i has landed, tile i - 1 is read
     if (i + 1 < t_end) {
       next = seen.bits(t.Lk, 32 * (i + 1));
-      issue(i + 1, next);
+      issue(i + 1, next, k_next, v_next);
       seen.request(a.mask, t.ka, t.Lk, 32 * (i + 2), lane);
     }
-    if (bits == 0 || !wave_has) continue;
-    const unsigned char *kt = lds + b * TILE, *vt = lds + (2 + b) * TILE;
+    if (bits == 0 || !wave_has) return;
     f32x16 p = f32x16{}, g = f32x16{};
     row_product<T, D>(kt, lane, q, kswz, p);
     row_product<T, D>(vt, lane, dy, vswz, g);
@@ -120,25 +117,32 @@ void cross_dq_kernel(CrossArgs a) {
         if (!(bits >> (8 * (r / 4) + 4 * h + r % 4) & 1)) p[r] = 0.f;
     }
     column_product<T, D>(kt, lane, p, kswz, acc);
+  };
+  for (int i = t_begin; i < t_end; i += 2) {
+    step(i, k_even, v_even, k_odd, v_odd);
+    if (i + 1 < t_end) step(i + 1, k_odd, v_odd, k_even, v_even);
   }
-  if (splits > 1) {
-    if (has_row)
-      store_lanes<D>(cross_part(a, tile, hkv, split, (size_t)kCrossTile * D), wave, lane, acc);
-    return;
-  }
-  if (has_row) store_row<T, D>(static_cast<T*>(a.dQ) + at * D, h, a.scale, acc);
+  if (!has_row) return;
+  if (splits > 1)
+    store_part<D>(a.parts + (split * (size_t)a.Tq * a.Hq + at) * D, h, acc);
+  else
+    store_row<T, D>(static_cast<T*>(a.dQ) + at * D, h, a.scale, acc);
 }
 
 // ---- dK, dV: owns states ---------------------------------------------------------------
 
 template <typename T, int D, bool kMask>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(Elem<T>::kBf16 && D == 64 ? 2 : 1)))
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(Elem<T>::kBf16 || D == 64 ? 2 : 1)))
 void cross_dkv_kernel(CrossArgs a) {
   constexpr int DT = D / 32, ESZ = sizeof(T), U = D * ESZ / 16, TILE = 32 * D * ESZ;
   constexpr int RPC = 64 / U, CPW = 32 / RPC / kCrossWaves;
   constexpr bool kB = Elem<T>::kBf16;
-  __shared__ __attribute__((aligned(16))) unsigned char lds[4 * TILE];  // Q0 Q1 dY0 dY1
+  // an array for each buffer, and the loop two steps at a time: the compiler then
+  // knows that a step's reads do not touch what its copies write, and waits for none
+  __shared__ __attribute__((aligned(16))) unsigned char q_even[TILE], q_odd[TILE];
+  __shared__ __attribute__((aligned(16))) unsigned char y_even[TILE], y_odd[TILE];
   __shared__ __attribute__((aligned(16))) float s_row[2][2][32];  // -lse log2(e), delta
+  __shared__ CrossFrag<T> s_v[kCrossWaves][kB ? kCrossSteps<T, D> : 1][kWave];
   const int tid = threadIdx.x, lane = tid % kWave;
   const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int h = lane / 32, c = lane % 32;
@@ -146,7 +150,7 @@ void cross_dkv_kernel(CrossArgs a) {
   CrossTile t;
   if (!find_cross_tile<true>(a, tile, lane, t)) return;
   const int rows = t.Lq * a.G;
-  const int n_tiles = (rows + 31) / 32, splits = splits_of<kLeastTiles>(a, n_tiles);
+  const int n_tiles = (rows + 31) / 32, splits = splits_of(a, n_tiles);
   const int split = blockIdx.y;
   if (split >= splits) return;
   const int t_begin = (int)((long long)n_tiles * split / splits);
@@ -165,12 +169,18 @@ void cross_dkv_kernel(CrossArgs a) {
     for (int i = 0; i < kCrossSteps<T, D>; ++i) k[i] = CrossFrag<T>{}, v[i] = CrossFrag<T>{};
   }
 
+  // bf16: the values wait in LDS, in registers they would leave room for one wave per
+  // SIMD instead of two at
+  // d = 128 (1319 to 1006 us for both kernels, 16 heads of 4096 rows and 4096 states)
+  if constexpr (kB) {
+#pragma unroll
+    for (int i = 0; i < kCrossSteps<T, D>; ++i) s_v[wave][i][lane] = v[i];
+  }
   const T* qbase = static_cast<const T*>(a.Q) + (size_t)t.qa * a.q_stride + (size_t)hkv * a.G * D;
   const T* ybase = static_cast<const T*>(a.dY) + (size_t)t.qa * a.dy_stride + (size_t)hkv * a.G * D;
   auto swz = [](int r) { return both_swizzle<U, kB>(r); };
-  float row_value = 0.f;  // threads 0..31: -lse log2(e), 32..63: delta of a tile's rows
-  auto issue = [&](int i) {
-    const int b = i & 1;
+  float row_value = 0.f;  // threads 0..31: lse, 32..63: delta of a tile's rows
+  auto issue = [&](int i, unsigned char* q_to, unsigned char* y_to) {
     // rows past the source's read its last one
     const int q0 = 32 * i / a.G, head0 = 32 * i % a.G, last = rows - 1 - 32 * i;
     const __amdgpu_buffer_rsrc_t rq = rsrc(qbase + (size_t)q0 * a.q_stride);
@@ -181,36 +191,45 @@ void cross_dkv_kernel(CrossArgs a) {
       const int dq = quotient(x, a.g_reciprocal), hd = x - dq * a.G;
       const uint32_t in = (uint32_t)(hd * D * ESZ) + 16u * ((lane % U) ^ swz(r));
       __builtin_amdgcn_raw_ptr_buffer_load_lds(
-          rq, (__attribute__((address_space(3))) void*)(lds + b * TILE + 1024 * j), 16,
+          rq, (__attribute__((address_space(3))) void*)(q_to + 1024 * j), 16,
           (uint32_t)dq * (uint32_t)(a.q_stride * ESZ) + in, 0, 0, 0);
       __builtin_amdgcn_raw_ptr_buffer_load_lds(
-          ry, (__attribute__((address_space(3))) void*)(lds + (2 + b) * TILE + 1024 * j), 16,
+          ry, (__attribute__((address_space(3))) void*)(y_to + 1024 * j), 16,
           (uint32_t)dq * (uint32_t)(a.dy_stride * ESZ) + in, 0, 0, 0);
     }
     if (tid < 64) {
       const int x = head0 + min(c, last), dq = quotient(x, a.g_reciprocal);
       const size_t at = (size_t)(t.qa + q0 + dq) * a.Hq + hkv * a.G + (x - dq * a.G);
-      const float e = tid < 32 ? a.lse[at] : a.delta[at];
-      // rows past the last one, and rows that saw no state: weights 0
-      row_value = tid >= 32 ? e : c > last || e == -INFINITY ? -INFINITY : -e * kLog2e;
+      row_value = tid < 32 ? a.lse[at] : a.delta[at];
     }
   };
 
   f32x16 dk[DT], dv[DT];
 #pragma unroll
   for (int i = 0; i < DT; ++i) dk[i] = f32x16{}, dv[i] = f32x16{};
-  if (t_begin < t_end) issue(t_begin);
-  for (int i = t_begin; i < t_end; ++i) {
-    const int b = i & 1;
-    if (tid < 64) s_row[b][tid / 32][tid % 32] = row_value;
+  if (t_begin < t_end) issue(t_begin, q_even, y_even);
+  auto step = [&](int i, int b, const unsigned char* qt, const unsigned char* yt,
+                  unsigned char* q_next, unsigned char* y_next) {
+    if (tid < 64) {
+      // rows past the last one, and rows that saw no state: weights 0
+      const bool none = 32 * i + c >= rows || row_value == -INFINITY;
+      s_row[b][tid / 32][tid % 32] =
+          tid >= 32 ? row_value : none ? -INFINITY : -row_value * kLog2e;
+    }
     __builtin_amdgcn_s_waitcnt(0);
     __syncthreads();  // tile i has landed, tile i - 1 is read
-    if (i + 1 < t_end) issue(i + 1);
-    if (!wave_has) continue;
-    const unsigned char *qt = lds + b * TILE, *yt = lds + (2 + b) * TILE;
+    if (i + 1 < t_end) issue(i + 1, q_next, y_next);
+    if (!wave_has) return;
     f32x16 p = f32x16{}, g = f32x16{};
     row_product<T, D>(qt, lane, k, swz, p);
-    row_product<T, D>(yt, lane, v, swz, g);
+    if constexpr (kB) {
+      CrossFrag<T> mine[kCrossSteps<T, D>];
+#pragma unroll
+      for (int n = 0; n < kCrossSteps<T, D>; ++n) mine[n] = s_v[wave][n][lane];
+      row_product<T, D>(yt, lane, mine, swz, g);
+    } else {
+      row_product<T, D>(yt, lane, v, swz, g);
+    }
 #pragma unroll
     for (int r = 0; r < 16; r += 4) {
       const f32x4 off = *reinterpret_cast<const f32x4*>(&s_row[b][0][2 * r + 4 * h]);
@@ -225,94 +244,50 @@ void cross_dkv_kernel(CrossArgs a) {
     }
     column_product<T, D>(yt, lane, p, swz, dv);
     column_product<T, D>(qt, lane, g, swz, dk);
-  }
-  if (splits > 1) {
-    float* part = cross_part(a, tile, hkv, split, 2 * (size_t)kCrossTile * D);
-    if (has_key) {
-      store_lanes<D>(part, wave, lane, dk);
-      store_lanes<D>(part + kCrossTile * D, wave, lane, dv);
-    }
-    return;
+  };
+  for (int i = t_begin; i < t_end; i += 2) {
+    step(i, 0, q_even, y_even, q_odd, y_odd);
+    if (i + 1 < t_end) step(i + 1, 1, q_odd, y_odd, q_even, y_even);
   }
   if (!has_key) return;
-  const size_t at = ((size_t)at_key * a.Hkv + hkv) * D;
-  store_row<T, D>(static_cast<T*>(a.dK) + at, h, a.scale, dk);
-  store_row<T, D>(static_cast<T*>(a.dV) + at, h, 1.f, dv);
-}
-
-// Joins the parts of a tile's rows (dQ) or states (dK, dV): one piece of 4 columns per
-// thread, the parts in their order.
-template <typename T, int D, bool kStates>
-__global__ __launch_bounds__(256) void cross_sum_kernel(CrossArgs a) {
-  const int hkv = blockIdx.x % a.Hkv, tile = blockIdx.x / a.Hkv;
-  CrossTile t;
-  if (!find_cross_tile<kStates>(a, tile, threadIdx.x % kWave, t)) return;
-  const int rows = t.Lq * a.G;
-  const int n = splits_of<kLeastTiles>(a, ((kStates ? rows : t.Lk) + 31) / 32);
-  if (n == 1) return;
-  const int piece = blockIdx.y * 256 + threadIdx.x, q = piece / kWave % (D / 8);
-  const int r = 32 * (piece / kWave / (D / 8)) + piece % 32;
-  const int d0 = 8 * q + 4 * (piece % kWave / 32);
-  const int row = t.lt * kCrossTile + r;
-  if (row >= (kStates ? t.Lk : rows)) return;
-  constexpr size_t kOne = (size_t)kCrossTile * D, kAll = kStates ? 2 * kOne : kOne;
-  const float* part = cross_part(a, tile, hkv, 0, kAll) + 4 * piece;
-  f32x4 x = f32x4{0.f, 0.f, 0.f, 0.f}, y = x;
-#pragma unroll 8
-  for (int i = 0; i < n; ++i) {
-    x += *reinterpret_cast<const f32x4*>(part + i * kAll);
-    if (kStates) y += *reinterpret_cast<const f32x4*>(part + i * kAll + kOne);
+  const size_t at = (size_t)at_key * a.Hkv + hkv;
+  if (splits > 1) {
+    const size_t rows_all = (size_t)a.Tk * a.Hkv;
+    store_part<D>(a.parts + (split * rows_all + at) * D, h, dk);
+    store_part<D>(a.parts + ((a.splits + split) * rows_all + at) * D, h, dv);
+    return;
   }
-  auto store = [&](void* out, size_t at, const f32x4& v) {
-    T* o = static_cast<T*>(out) + at * D + d0;
-    if constexpr (Elem<T>::kBf16)
-      *reinterpret_cast<bf16x4*>(o) = bf16x4{(bf16)v[0], (bf16)v[1], (bf16)v[2], (bf16)v[3]};
-    else
-      *reinterpret_cast<f32x4*>(o) = v;
-  };
-  if (kStates) {
-    const size_t at = (size_t)(t.ka + row) * a.Hkv + hkv;
-    store(a.dK, at, a.scale * x);
-    store(a.dV, at, y);
-  } else {
-    store(a.dQ, (size_t)(t.qa + row / a.G) * a.Hq + hkv * a.G + row % a.G, a.scale * x);
-  }
+  store_row<T, D>(static_cast<T*>(a.dK) + at * D, h, a.scale, dk);
+  store_row<T, D>(static_cast<T*>(a.dV) + at * D, h, 1.f, dv);
 }
 
 long long tiles_of(long long rows, int S) { return rows / kCrossTile + S; }
 
-// Workgroups that share a tile's work: as many as fill the device, mean lengths
-// standing for all. own: rows (or states) per source that a kernel owns, others:
-// those it runs over.
-int splits_for(long long own, long long others, int S, int Hkv) {
-  const long long tiles = (std::max(1LL, own / S) + kCrossTile - 1) / kCrossTile * S * Hkv;
-  const long long most = std::max(1LL, others / S / (32 * kLeastTiles));
-  return (int)std::min({std::max(1LL, 512 / tiles), most, 64LL});
-}
-
 struct Plan {
   long long row_tiles, state_tiles;
-  int row_splits, state_splits;
+  CrossSplit rows, states;
   size_t delta, parts;  // floats
 };
-Plan plan_of(int S, int Tq, int Tk, int Hq, int Hkv, int d) {
+template <typename T, int d>
+Plan plan_of(int S, int Tq, int Tk, int Hq, int Hkv) {
   const long long rows = (long long)Tq * (Hq / Hkv);
   Plan p;
   p.row_tiles = tiles_of(rows, S), p.state_tiles = tiles_of(Tk, S);
-  p.row_splits = splits_for(rows, Tk, S, Hkv), p.state_splits = splits_for(Tk, rows, S, Hkv);
+  p.rows = cross_split(rows, Tk, S, Hkv, 512, sizeof(T) == 4);
+  p.states = cross_split(Tk, rows, S, Hkv, 512, sizeof(T) == 4);
   p.delta = ((size_t)Tq * Hq + 3) / 4 * 4;
   // the two kernels' parts lie at the same place: dQ is joined before dK and dV start
-  const size_t one = (size_t)kCrossTile * d * Hkv;
-  const size_t a = p.row_splits > 1 ? p.row_tiles * p.row_splits * one : 0;
-  const size_t b = p.state_splits > 1 ? p.state_tiles * p.state_splits * 2 * one : 0;
+  const size_t a = p.rows.splits > 1 ? (size_t)Tq * Hq * d * p.rows.splits : 0;
+  const size_t b = p.states.splits > 1 ? 2 * (size_t)Tk * Hkv * d * p.states.splits : 0;
   p.parts = std::max(a, b);
   return p;
 }
 
 }  // namespace
 
-size_t cross_attention_bwd_workspace(int S, int Tq, int Tk, int Hq, int Hkv, int d) {
-  const Plan p = plan_of(S, Tq, Tk, Hq, Hkv, d);
+template <typename T, int D>
+size_t cross_attention_bwd_workspace(int S, int Tq, int Tk, int Hq, int Hkv) {
+  const Plan p = plan_of<T, D>(S, Tq, Tk, Hq, Hkv);
   return (p.delta + p.parts) * sizeof(float);
 }
 
@@ -324,7 +299,7 @@ hipError_t launch_cross_attention_bwd(int S, int Tq, int Tk, int Hq, int Hkv, fl
                                       const uint8_t* mask, const void* Y, const float* lse,
                                       const void* dY, int64_t dy_stride, void* dQ, void* dK,
                                       void* dV, void* workspace, hipStream_t stream) {
-  const Plan p = plan_of(S, Tq, Tk, Hq, Hkv, D);
+  const Plan p = plan_of<T, D>(S, Tq, Tk, Hq, Hkv);
   CrossArgs a{};
   a.Q = Q, a.K = K, a.V = V, a.q_stride = q_stride, a.k_stride = k_stride, a.v_stride = v_stride;
   a.cu_q = cu_q, a.cu_k = cu_k, a.mask = mask, a.Y = const_cast<void*>(Y);
@@ -336,22 +311,17 @@ hipError_t launch_cross_attention_bwd(int S, int Tq, int Tk, int Hq, int Hkv, fl
   a.delta = static_cast<float*>(workspace), a.parts = a.delta + p.delta;
   hipError_t e = hipSuccess;
   if (Tq > 0) {
-    a.tiles = (int)p.row_tiles, a.splits = p.row_splits;
+    a.tiles = (int)p.row_tiles, a.per = p.rows.per, a.splits = p.rows.splits;
     const dim3 grid((unsigned)(a.tiles * Hkv), (unsigned)a.splits);
     if (mask)
       hipLaunchKernelGGL((cross_dq_kernel<T, D, true>), grid, dim3(256), 0, stream, a);
     else
       hipLaunchKernelGGL((cross_dq_kernel<T, D, false>), grid, dim3(256), 0, stream, a);
     e = hipGetLastError();
-    if (e == hipSuccess && a.splits > 1) {
-      hipLaunchKernelGGL((cross_sum_kernel<T, D, false>),
-                         dim3((unsigned)(a.tiles * Hkv), kCrossTile * D / 4 / 256), dim3(256), 0,
-                         stream, a);
-      e = hipGetLastError();
-    }
+    if (e == hipSuccess && a.splits > 1) e = launch_cross_join<T, D, kJoinQueries>(a, stream);
   }
   if (e != hipSuccess || Tk == 0) return e;
-  a.tiles = (int)p.state_tiles, a.splits = p.state_splits;
+  a.tiles = (int)p.state_tiles, a.per = p.states.per, a.splits = p.states.splits;
   const dim3 grid((unsigned)(a.tiles * Hkv), (unsigned)a.splits);
   if (mask)
     hipLaunchKernelGGL((cross_dkv_kernel<T, D, true>), grid, dim3(256), 0, stream, a);
@@ -359,17 +329,15 @@ hipError_t launch_cross_attention_bwd(int S, int Tq, int Tk, int Hq, int Hkv, fl
     hipLaunchKernelGGL((cross_dkv_kernel<T, D, false>), grid, dim3(256), 0, stream, a);
   e = hipGetLastError();
   if (e != hipSuccess || a.splits == 1) return e;
-  hipLaunchKernelGGL((cross_sum_kernel<T, D, true>),
-                     dim3((unsigned)(a.tiles * Hkv), kCrossTile * D / 4 / 256), dim3(256), 0, stream,
-                     a);
-  return hipGetLastError();
+  return launch_cross_join<T, D, kJoinStates>(a, stream);
 }
 
 #define AVQ_INSTANCE(T, D)                                                                        \
   template hipError_t launch_cross_attention_bwd<T, D>(                                           \
       int, int, int, int, int, float, const void*, int64_t, const void*, int64_t, const void*,    \
       int64_t, const int32_t*, const int32_t*, const uint8_t*, const void*, const float*,         \
-      const void*, int64_t, void*, void*, void*, void*, hipStream_t);
+      const void*, int64_t, void*, void*, void*, void*, hipStream_t);                             \
+  template size_t cross_attention_bwd_workspace<T, D>(int, int, int, int, int);
 AVQ_INSTANCE(bf16, 64)
 AVQ_INSTANCE(bf16, 128)
 AVQ_INSTANCE(float, 64)

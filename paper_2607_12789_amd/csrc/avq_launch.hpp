@@ -64,14 +64,16 @@ hipError_t launch_rotate_axes(int T_, int Hq, int Hkv, int rot, int n_axes, cons
                               int64_t q_stride, const void* K, int64_t k_stride,
                               const int32_t* pos, const float* cos, const float* sin, void* Q_out,
                               void* K_out, hipStream_t stream);
-size_t cross_attention_workspace(int S, int Tq, int Tk, int Hq, int Hkv, int d);
+template <typename T, int D>
+size_t cross_attention_workspace(int S, int Tq, int Tk, int Hq, int Hkv);
 template <typename T, int D>
 hipError_t launch_cross_attention(int S, int Tq, int Tk, int Hq, int Hkv, float scale,
                                   const void* Q, int64_t q_stride, const void* K, int64_t k_stride,
                                   const void* V, int64_t v_stride, const int32_t* cu_q,
                                   const int32_t* cu_k, const uint8_t* mask, void* Y, float* lse,
                                   void* workspace, hipStream_t stream);
-size_t cross_attention_bwd_workspace(int S, int Tq, int Tk, int Hq, int Hkv, int d);
+template <typename T, int D>
+size_t cross_attention_bwd_workspace(int S, int Tq, int Tk, int Hq, int Hkv);
 template <typename T, int D>
 hipError_t launch_cross_attention_bwd(int S, int Tq, int Tk, int Hq, int Hkv, float scale,
                                       const void* Q, int64_t q_stride, const void* K,

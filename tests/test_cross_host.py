@@ -107,19 +107,22 @@ def test_refusals(L, fn, kw, status):
 
 def test_workspaces(L):
     # as many tiles as fill the device: nothing is divided
-    assert avq.cross_attention_workspace(4, 1 << 16, 1 << 16, 16, 4, 128) == 0
-    assert avq.cross_attention_workspace(1, 1, 1 << 16, 16, 4, 128) > 0
-    assert avq.cross_attention_workspace(1, 1, 40, 16, 4, 128) == 0
+    assert avq.cross_attention_workspace(torch.bfloat16, 4, 1 << 16, 1 << 16, 16, 4, 128) == 0
+    assert avq.cross_attention_workspace(torch.float32, 1, 1, 1 << 16, 16, 4, 128) > 0
+    assert avq.cross_attention_workspace(torch.float32, 1, 1, 40, 16, 4, 128) == 0
     # one fp32 per query and head at least
-    assert avq.cross_attention_workspace(4, 1 << 16, 1 << 16, 16, 4, 128, True) >= 4 * 16 << 16
+    assert avq.cross_attention_workspace(torch.bfloat16, 4, 1 << 16, 1 << 16, 16, 4, 128, True) >= 4 * 16 << 16
     assert (avq.cache_prefix_attention_workspace(64, 1, 1, 16, 4, 128)
             > avq.cache_attention_workspace(64, 1, 16, 4, 128))
     for bad in ((0, 8, 8, 4, 2, 64), (1, -1, 8, 4, 2, 64), (1, 8, 8, 4, 3, 64), (1, 8, 8, 4, 2, 96),
                 (1 << 20, 8, 8, 16, 16, 64), (1, 1 << 24, 8, 1024, 1, 64)):
-        assert L.avq_cross_attention_workspace(*bad) == -1
-        assert L.avq_cross_attention_bwd_workspace(*bad) == -1
+        assert L.avq_cross_attention_workspace(BF16, *bad) == -1
+        assert L.avq_cross_attention_bwd_workspace(F32, *bad) == -1
         with pytest.raises(ValueError):
-            avq.cross_attention_workspace(*bad)
+            avq.cross_attention_workspace(torch.bfloat16, *bad)
+    assert L.avq_cross_attention_workspace(7, 1, 8, 8, 4, 2, 64) == -1
+    with pytest.raises(ValueError):
+        avq.cross_attention_workspace(torch.float16, 1, 8, 8, 4, 2, 64)
     for bad in ((0, 1, 1, 4, 2, 64), (2, 0, 1, 4, 2, 64), (2, 1, 17, 4, 2, 64), (2, 1, 1, 4, 3, 64),
                 (2, 1, 1, 4, 2, 96), (2, 1 << 21, 1, 4, 2, 64)):
         assert L.avq_cache_prefix_attention_workspace(*bad) == -1

@@ -194,7 +194,7 @@ def test_same_bits_again(dtype):
     Q, K, V, dY = (x.cuda() for x in make(lens_q, lens_k, 4, 1, 128, dtype, 6))
     Y, lse = avq.cross_attention_fwd(Q, K, V, cu(lens_q), cu(lens_k), 0.1, with_lse=True)
     first = avq.cross_attention_bwd(dY, Q, K, V, Y, lse, cu(lens_q), cu(lens_k), 0.1)
-    n = avq.cross_attention_workspace(3, 391, 1603, 4, 1, 128, backward=True)
+    n = avq.cross_attention_workspace(dtype, 3, 391, 1603, 4, 1, 128, backward=True)
     ws = torch.full((n,), 255, dtype=torch.uint8, device="cuda")
     for _ in range(3):
         again = avq.cross_attention_bwd(dY, Q, K, V, Y, lse, cu(lens_q), cu(lens_k), 0.1,
