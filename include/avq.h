@@ -675,19 +675,21 @@ int64_t avq_cache_prefix_attention_workspace(int32_t S, int32_t n_groups, int32_
  * first shared[g] positions are the same ones: their block tables may name the same
  * pages for them, or copies (of the page in which the shared positions end, say).
  * Positions below P_g = min(shared[g], lens[cu_groups[g]]) are read through the
- * table of the group's first sequence only, for all of its sequences; a sequence
- * whose own positions there differ is answered as if they did not. A group of one
- * sequence, and sequences of no group, share nothing. If the first sequence of a
- * group is idle (lens 0), so is the sharing: P_g = 0, and every sequence reads its
- * own pages. Y and lse are those of avq_cache_attention_fwd on the same arguments,
- * but for the rounding of the sums.
+ * table of the group's first sequence, for all of its sequences (where sharing does
+ * not pay, through each one's own; a group whose sequences do not hold the same there
+ * gets unspecified outputs). A group of one sequence, and sequences of no group, share
+ * nothing. If the first sequence of a group is idle (lens 0), so is the sharing: P_g =
+ * 0, and every sequence reads its own pages. Y and lse are those of
+ * avq_cache_attention_fwd on the same arguments, but for the rounding of the sums.
  *
  *   cu_groups    [n_groups + 1] int32; it must not decrease (if it does, outputs are
  *                unspecified); values outside [0, S] are taken as the nearest
  *   shared       [n_groups] int32, below 0: none
  *   others       as avq_cache_attention_fwd
- *   workspace    avq_cache_prefix_attention_workspace() bytes
- * n_groups >= 1; (S n_q Hq / Hkv / 128 + n_groups) Hkv < 2^24. Two launches.
+ *   workspace    avq_cache_prefix_attention_workspace() bytes; NULL allowed if
+ *                max_pages * page_size <= AVQ_CACHE_UNDIVIDED (nothing is then shared)
+ * n_groups >= 1; (S n_q Hq / Hkv / 128 + n_groups) Hkv < 2^24. Two launches, one without a
+ * workspace. It pays from a few tens of megabytes on that are read less.
  */
 avq_status_t avq_cache_prefix_attention_fwd(avq_dtype_t dtype, avq_cache_t format, int32_t S,
                                             int32_t n_groups, int32_t n_q, int32_t Hq, int32_t Hkv,

@@ -899,7 +899,7 @@ def cache_prefix_attention_fwd(Q, cache, block_table, lens, cu_groups, shared, p
     cu_groups[g + 1] - 1; shared int32 [groups]: how many first positions they have in
     common. The other arguments, and what is returned, are those of
     ``cache_attention_fwd``; workspace: a uint8 tensor of
-    ``cache_prefix_attention_workspace(...)`` bytes (allocated if not given).
+    ``cache_prefix_attention_workspace(...)`` bytes (allocated if needed and not given).
     """
     S, n_q, Hq, d, q_stride = _newest(Q)
     n_pages, Hkv, _, max_pages = _cache(cache, block_table, Q.dtype, page_size, d, fp4, S)
@@ -921,17 +921,18 @@ def cache_prefix_attention_fwd(Q, cache, block_table, lens, cu_groups, shared, p
     if workspace is not None:
         _dev(workspace, "workspace", torch.uint8)
     else:
-        n = _prefix_workspace_of(S, n_groups, n_q, Hq, Hkv, d)
-        workspace = _empty(stream, (n,), torch.uint8, Q.device)
+        n = _prefix_workspace_of(S, n_groups, n_q, Hq, Hkv, d)  # refuses unsupported sizes
+        if max_pages * page_size > CACHE_UNDIVIDED:
+            workspace = _empty(stream, (n,), torch.uint8, Q.device)
     at = Q.get_device()
     if (not cache.get_device() == block_table.get_device() == lens.get_device()
-            == cu_groups.get_device() == shared.get_device() == Y.get_device()
-            == workspace.get_device() == at or _elsewhere(lse, at)):
+            == cu_groups.get_device() == shared.get_device() == Y.get_device() == at
+            or _elsewhere(workspace, at) or _elsewhere(lse, at)):
         _same_device(Q, cache=cache, block_table=block_table, lens=lens, cu_groups=cu_groups,
                      shared=shared, Y=Y, lse=lse, workspace=workspace)
     _check(lib().avq_cache_prefix_attention_fwd(
         _dtype_code(Q), int(bool(fp4)), S, n_groups, n_q, Hq, Hkv, d, n_pages, page_size, max_pages,
         float(scale), Q.data_ptr(), q_stride, cache.data_ptr(), lens.data_ptr(),
         block_table.data_ptr(), cu_groups.data_ptr(), shared.data_ptr(), Y.data_ptr(), _ptr(lse),
-        workspace.data_ptr(), workspace.numel(), s))
+        _ptr(workspace), 0 if workspace is None else workspace.numel(), s))
     return (Y, lse) if with_lse else Y

@@ -754,9 +754,11 @@ avq_status_t avq_cache_prefix_attention_fwd(avq_dtype_t dtype, avq_cache_t forma
       !aligned16(cu_groups) || !aligned16(shared) || !aligned16(Y) || !aligned16(lse) ||
       !aligned16(workspace))
     return misaligned(name);
-  st = check_workspace(name, avq_cache_prefix_attention_workspace(S, n_groups, n_q, Hq, Hkv, d),
-                       workspace, workspace_bytes);
-  if (st != AVQ_OK) return st;
+  if (workspace || (int64_t)max_pages * page_size > AVQ_CACHE_UNDIVIDED) {
+    st = check_workspace(name, avq_cache_prefix_attention_workspace(S, n_groups, n_q, Hq, Hkv, d),
+                         workspace, workspace_bytes);
+    if (st != AVQ_OK) return st;
+  }
   const avq::CacheShape c{format == AVQ_CACHE_FP4, n_pages, page_size, max_pages, Hkv};
   hipStream_t s = static_cast<hipStream_t>(stream);
   return from_hip(AVQ_BY_TYPE(launch_prefix_attention, c, S, n_groups, n_q, Hq, scale, Q, q_stride,

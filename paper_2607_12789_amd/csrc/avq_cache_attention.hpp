@@ -29,7 +29,8 @@ struct CacheAttnArgs {
   float* lse;           // nullable
   float* parts;         // [workgroups][2] of part_floats(D): see there
   int32_t* joins;       // [segments][2]: first workgroup and its slot, parts;
-                        // null where no segment is divided
+                        // null where no segment is divided. With groups
+                        // [segments][4]: these and the shared positions
   int S, n_q, Hq, G, row_tiles;
   int unit;  // keys per unit, a multiple of kUnit
   float scale_log2;
@@ -117,15 +118,20 @@ __device__ __forceinline__ void load_words(const unsigned char* p, uint32_t* w) 
 template <typename T, int D, bool FP4, int NT>
 constexpr int kPerCu = NT == 2 || (!Elem<T>::kBf16 && D == 128 && !FP4) ? 2 : 3;
 
-// Where a workgroup's waves exchange their numerators.
+// Where a workgroup's waves exchange their numerators: 4 columns of a wave's row.
 template <int D>
-using Exchange = float[kWaves][kRows][D + 4];
+struct Exchange {
+  float o[kWaves][kRows][D + 4];
+  __device__ __forceinline__ f32x4& unit(int wave, int row, int u) {
+    return *reinterpret_cast<f32x4*>(&o[wave][row][4 * u]);
+  }
+};
 
 // Workgroup w of n_workgroups. kGroups: sequences start behind the positions that
 // their group shares, and leave their state where others join it.
-template <typename T, int D, bool FP4, int NT, bool kGroups>
+template <typename T, int D, bool FP4, int NT, bool kGroups, typename Area>
 __device__ __forceinline__ void cache_attention_run(const CacheAttnArgs& a, const int w,
-                                                    const int n_workgroups, Exchange<D>& s_o) {
+                                                    const int n_workgroups, Area& s_o) {
   constexpr bool kB = Elem<T>::kBf16;
   using Raw = Keys<T, D, FP4>;
   constexpr int H2 = D / 64, R = NT * kRows;
@@ -517,8 +523,10 @@ __device__ __forceinline__ void cache_attention_run(const CacheAttnArgs& a, cons
     if (tid == 0 && x == 0 && (kGroups || a.joins)) {
       // the workgroup that holds unit v is ((v + 1) W - 1) / U
       const long long w_last = ((u + n_units) * W - 1) / U;
-      a.joins[2 * seg] = 2 * w + slot;
-      a.joins[2 * seg + 1] = whole ? 1 : (int)(w_last - w) + 1;
+      int32_t* join = a.joins + (kGroups ? 4 : 2) * seg;
+      join[0] = 2 * w + slot;
+      join[1] = whole ? 1 : (int)(w_last - w) + 1;
+      if constexpr (kGroups) join[2] = start;
     }
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
@@ -533,7 +541,7 @@ __device__ __forceinline__ void cache_attention_run(const CacheAttnArgs& a, cons
       for (int h = 0; h < H2; ++h)
 #pragma unroll
         for (int r = 0; r < 4; ++r)
-          *reinterpret_cast<f32x4*>(&s_o[wave][c][64 * h + 16 * g + 4 * r]) =
+          s_o.unit(wave, c, 16 * h + 4 * g + r) =
               f32x4{o[n][h][0][r], o[n][h][1][r], o[n][h][2][r], o[n][h][3][r]};
       __syncthreads();
       constexpr int C = D / 16;  // columns per thread
@@ -545,7 +553,7 @@ __device__ __forceinline__ void cache_attention_run(const CacheAttnArgs& a, cons
         const float f = exp2_hw(s_m[i][rr] - mm);
         ll = fmaf(f, s_l[i][rr], ll);
 #pragma unroll
-        for (int k = 0; k < C; ++k) acc[k] = fmaf(f, s_o[i][rr][d0 + k], acc[k]);
+        for (int k = 0; k < C; ++k) acc[k] = fmaf(f, s_o.unit(i, rr, (d0 + k) / 4)[k % 4], acc[k]);
       }
       const int row = kRows * n + rr, out_row = row0 + row;
       if (out_row < rows_all) {

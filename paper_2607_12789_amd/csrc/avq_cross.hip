@@ -18,7 +18,6 @@
 #include "avq_launch.hpp"
 
 #include <algorithm>
-#include <type_traits>
 
 #include "avq_cross.hpp"
 
@@ -50,7 +49,7 @@ void cross_kernel(CrossArgs a) {
   const int rows = t.Lq * a.G, row0 = t.lt * kCrossTile + 32 * wave, row = row0 + c;
   const bool has_row = row < rows, wave_has = row0 < rows;
   const int at_row = min(row, rows - 1), qi = t.qa + at_row / a.G, hq = hkv * a.G + at_row % a.G;
-  CrossFrag<T> q[kCrossSteps<T, D>];
+  RowFrag<T> q[kRowSteps<T, D>];
   load_row<T, D>(static_cast<const T*>(a.Q) + (size_t)qi * a.q_stride + (size_t)hq * D, h, q);
 
   const T* kbase = static_cast<const T*>(a.K) + (size_t)t.ka * a.k_stride + (size_t)hkv * D;
@@ -96,7 +95,7 @@ void cross_kernel(CrossArgs a) {
     }
     if (bits == 0 || !wave_has) continue;
     f32x16 sc = f32x16{};
-    row_product<T, D>(lds + b * TILE, lane, q, kswz, sc);
+    row_product<T, D>(lds + b * TILE, lane, c, q, kswz, sc);
     if (bits != ~0u) {
 #pragma unroll
       for (int r = 0; r < 16; ++r)
@@ -142,7 +141,7 @@ void cross_kernel(CrossArgs a) {
   const size_t at = (size_t)qi * a.Hq + hq;
   if (splits > 1) {
     const size_t rows_all = (size_t)a.Tq * a.Hq, part = split * rows_all + at;
-    store_part<D>(a.parts + part * D, h, o);
+    store_row<float, D>(a.parts + part * D, h, 1.f, o);
     if (h == 0) {
       a.parts[a.splits * rows_all * D + part] = ms;
       a.parts[a.splits * rows_all * (D + 1) + part] = l;

@@ -16,7 +16,6 @@
 #include "avq_launch.hpp"
 
 #include <algorithm>
-#include <type_traits>
 
 #include "avq_cross.hpp"
 
@@ -71,15 +70,15 @@ void cross_dq_kernel(CrossArgs a) {
   }
 
   // the row's operands, delta and -lse log2(e) (a row that saw no state: weights 0)
-  CrossFrag<T> q[kCrossSteps<T, D>], dy[kCrossSteps<T, D>];
+  RowFrag<T> q[kRowSteps<T, D>], dy[kRowSteps<T, D>];
   load_row<T, D>(static_cast<const T*>(a.Q) + (size_t)qi * a.q_stride + (size_t)hq * D, h, q);
   load_row<T, D>(static_cast<const T*>(a.dY) + (size_t)qi * a.dy_stride + (size_t)hq * D, h, dy);
   float delta = 0.f;
   {
-    CrossFrag<T> y[kCrossSteps<T, D>];
+    RowFrag<T> y[kRowSteps<T, D>];
     load_row<T, D>(static_cast<const T*>(a.Y) + at * D, h, y);
 #pragma unroll
-    for (int k = 0; k < kCrossSteps<T, D>; ++k) {
+    for (int k = 0; k < kRowSteps<T, D>; ++k) {
       if constexpr (kB) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) delta = fmaf((float)y[k][e], (float)dy[k][e], delta);
@@ -107,8 +106,8 @@ void cross_dq_kernel(CrossArgs a) {
     }
     if (bits == 0 || !wave_has) return;
     f32x16 p = f32x16{}, g = f32x16{};
-    row_product<T, D>(kt, lane, q, kswz, p);
-    row_product<T, D>(vt, lane, dy, vswz, g);
+    row_product<T, D>(kt, lane, c, q, kswz, p);
+    row_product<T, D>(vt, lane, c, dy, vswz, g);
 #pragma unroll
     for (int r = 0; r < 16; ++r) p[r] = exp2_hw(fmaf(p[r], a.scale_log2, off)) * (g[r] - delta);
     if (bits != ~0u) {
@@ -124,7 +123,7 @@ void cross_dq_kernel(CrossArgs a) {
   }
   if (!has_row) return;
   if (splits > 1)
-    store_part<D>(a.parts + (split * (size_t)a.Tq * a.Hq + at) * D, h, acc);
+    store_row<float, D>(a.parts + (split * (size_t)a.Tq * a.Hq + at) * D, h, 1.f, acc);
   else
     store_row<T, D>(static_cast<T*>(a.dQ) + at * D, h, a.scale, acc);
 }
@@ -142,7 +141,7 @@ void cross_dkv_kernel(CrossArgs a) {
   __shared__ __attribute__((aligned(16))) unsigned char q_even[TILE], q_odd[TILE];
   __shared__ __attribute__((aligned(16))) unsigned char y_even[TILE], y_odd[TILE];
   __shared__ __attribute__((aligned(16))) float s_row[2][2][32];  // -lse log2(e), delta
-  __shared__ CrossFrag<T> s_v[kCrossWaves][kB ? kCrossSteps<T, D> : 1][kWave];
+  __shared__ RowFrag<T> s_v[kCrossWaves][kB ? kRowSteps<T, D> : 1][kWave];
   const int tid = threadIdx.x, lane = tid % kWave;
   const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int h = lane / 32, c = lane % 32;
@@ -161,12 +160,12 @@ void cross_dkv_kernel(CrossArgs a) {
   const int at_key = t.ka + min(key, t.Lk - 1);
   const bool seen = has_key && (!kMask || a.mask[at_key] != 0);
   // a state that takes no part may hold anything: it is taken as 0
-  CrossFrag<T> k[kCrossSteps<T, D>], v[kCrossSteps<T, D>];
+  RowFrag<T> k[kRowSteps<T, D>], v[kRowSteps<T, D>];
   load_row<T, D>(static_cast<const T*>(a.K) + (size_t)at_key * a.k_stride + (size_t)hkv * D, h, k);
   load_row<T, D>(static_cast<const T*>(a.V) + (size_t)at_key * a.v_stride + (size_t)hkv * D, h, v);
   if (kMask && !seen) {
 #pragma unroll
-    for (int i = 0; i < kCrossSteps<T, D>; ++i) k[i] = CrossFrag<T>{}, v[i] = CrossFrag<T>{};
+    for (int i = 0; i < kRowSteps<T, D>; ++i) k[i] = RowFrag<T>{}, v[i] = RowFrag<T>{};
   }
 
   // bf16: the values wait in LDS, in registers they would leave room for one wave per
@@ -174,7 +173,7 @@ void cross_dkv_kernel(CrossArgs a) {
   // d = 128 (1319 to 1006 us for both kernels, 16 heads of 4096 rows and 4096 states)
   if constexpr (kB) {
 #pragma unroll
-    for (int i = 0; i < kCrossSteps<T, D>; ++i) s_v[wave][i][lane] = v[i];
+    for (int i = 0; i < kRowSteps<T, D>; ++i) s_v[wave][i][lane] = v[i];
   }
   const T* qbase = static_cast<const T*>(a.Q) + (size_t)t.qa * a.q_stride + (size_t)hkv * a.G * D;
   const T* ybase = static_cast<const T*>(a.dY) + (size_t)t.qa * a.dy_stride + (size_t)hkv * a.G * D;
@@ -221,14 +220,14 @@ void cross_dkv_kernel(CrossArgs a) {
     if (i + 1 < t_end) issue(i + 1, q_next, y_next);
     if (!wave_has) return;
     f32x16 p = f32x16{}, g = f32x16{};
-    row_product<T, D>(qt, lane, k, swz, p);
+    row_product<T, D>(qt, lane, c, k, swz, p);
     if constexpr (kB) {
-      CrossFrag<T> mine[kCrossSteps<T, D>];
+      RowFrag<T> mine[kRowSteps<T, D>];
 #pragma unroll
-      for (int n = 0; n < kCrossSteps<T, D>; ++n) mine[n] = s_v[wave][n][lane];
-      row_product<T, D>(yt, lane, mine, swz, g);
+      for (int n = 0; n < kRowSteps<T, D>; ++n) mine[n] = s_v[wave][n][lane];
+      row_product<T, D>(yt, lane, c, mine, swz, g);
     } else {
-      row_product<T, D>(yt, lane, v, swz, g);
+      row_product<T, D>(yt, lane, c, v, swz, g);
     }
 #pragma unroll
     for (int r = 0; r < 16; r += 4) {
@@ -253,8 +252,8 @@ void cross_dkv_kernel(CrossArgs a) {
   const size_t at = (size_t)at_key * a.Hkv + hkv;
   if (splits > 1) {
     const size_t rows_all = (size_t)a.Tk * a.Hkv;
-    store_part<D>(a.parts + (split * rows_all + at) * D, h, dk);
-    store_part<D>(a.parts + ((a.splits + split) * rows_all + at) * D, h, dv);
+    store_row<float, D>(a.parts + (split * rows_all + at) * D, h, 1.f, dk);
+    store_row<float, D>(a.parts + ((a.splits + split) * rows_all + at) * D, h, 1.f, dv);
     return;
   }
   store_row<T, D>(static_cast<T*>(a.dK) + at * D, h, a.scale, dk);

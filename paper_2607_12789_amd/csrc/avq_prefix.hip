@@ -13,9 +13,10 @@
 // an octet of one column, which lies together in the page.
 //
 // Behind P_g every sequence is attended to as in avq_cache_attention.hip. Both are
-// one launch: its first workgroups take the shared positions of a tile of rows, in
-// a.splits equal runs, the others the sequences' own ones. All leave running maxima,
-// sums and numerators, and a second launch joins them, row by row.
+// one launch: its first workgroups take the shared positions, those of each tile of
+// rows in as many runs of equal length as give every workgroup its share of the
+// whole; the others take the sequences' own positions. All leave running maxima, sums
+// and numerators, and a second launch joins them, row by row.
 #include "avq_cache_attention.hpp"
 #include "avq_launch.hpp"
 
@@ -29,39 +30,37 @@ constexpr int kTile = 128;       // rows of a workgroup
 constexpr int kLeastTiles = 4;   // tiles of 32 positions that a workgroup takes, at least
 constexpr int kMaxSplits = 64;
 
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-
 struct PrefixArgs {
   CacheAttnArgs c;
-  int tiles, splits;   // tiles of rows, at most; workgroups that share one's positions
-  int shared_blocks;   // workgroups for the shared positions
-  float lazy;          // kLazy / scale_log2
-  float* shared_parts; // [tiles][Hkv][splits] of part_floats(kTile, D)
+  int shared_blocks;    // workgroups for the shared positions
+  int splits;           // runs of one tile of rows, at most
+  float lazy;           // kLazy / scale_log2
+  float* shared_parts;  // numerators [splits][S n_q Hq][D], then maxima and sums
+                        // [splits][S n_q Hq] each
+  int32_t* per;         // tiles of 32 positions of a run, for the joining launch
 };
 
-struct RowTile {
-  int first, rows, r0;  // the group's first sequence, its rows, the tile's first one
-  int P;                // shared positions
+struct Group {
+  int first, rows, P;  // first sequence, rows per key-value head, shared positions
+  __device__ __forceinline__ int row_tiles() const { return P > 0 ? (rows + kTile - 1) / kTile : 0; }
+  __device__ __forceinline__ int tiles() const { return (P + 31) / 32; }
 };
-
-__device__ __forceinline__ long long tile_of(int first, int g, int per) {
-  return (long long)first * per / kTile + g;
+__device__ __forceinline__ Group group_of(const CacheAttnArgs& a, int g) {
+  Group x;
+  x.first = group_first(a, g);
+  const int end = max(group_first(a, g + 1), x.first);
+  x.rows = (end - x.first) * a.n_q * a.G;
+  x.P = shared_length(a, g, x.first, end);
+  return x;
 }
-// Runs of P positions, the same on the joining side.
-__device__ __forceinline__ int runs_of(int P, int splits) {
-  return max(1, min(splits, (P + 31) / 32 / kLeastTiles));
+// Runs of n tiles, the same on the joining side.
+__device__ __forceinline__ int runs_of(int n, int per, int splits) {
+  return max(1, min(splits, (n + per - 1) / per));
 }
-__device__ __forceinline__ bool find_rows(const CacheAttnArgs& a, int tile, int lane, RowTile& t) {
-  const int per = a.n_q * a.G;
-  const int g = find_sequence(a.n_groups, tile, lane,
-                              [&](int k) { return tile_of(group_first(a, k), k, per); });
-  t.first = group_first(a, g);
-  const int end = group_first(a, g + 1);
-  t.rows = (end - t.first) * per;
-  t.r0 = (int)(tile - tile_of(t.first, g, per)) * kTile;
-  if (t.r0 < 0 || t.r0 >= t.rows) return false;
-  t.P = shared_length(a, g, t.first, end);
-  return t.P > 0;
+__device__ __forceinline__ float wave_sum(float x) {  // the same bits in every lane
+#pragma unroll
+  for (int k = 1; k < kWave; k *= 2) x += __shfl_xor(x, k, kWave);
+  return x;
 }
 
 // Four values of a byte's word: the positions' bytes with their scales.
@@ -84,48 +83,119 @@ __device__ __forceinline__ void decode4(uint32_t w, const float* f, T (*e)[2]) {
   }
 }
 
-// Run `split` of the shared positions of one tile of rows and one key-value head.
+// The operands of a tile's two products, as read from LDS: keys row by row (lane c the
+// row r), values in octets, [octet][column][8]. bf16 reads all of them before the first
+// product: one by one, each product would wait for its own read, and a workgroup of
+// these is alone with its latencies (1 to 2 waves per SIMD).
+template <typename T, int D>
+struct Operands {
+  static constexpr bool kB = Elem<T>::kBf16;
+  bf16x8 k[kB ? D / 16 : 1], v[kB ? D / 16 : 1];
+
+  __device__ __forceinline__ void read(const unsigned char* kt, const unsigned char* vt, int lane,
+                                       uint32_t r) {
+    if constexpr (kB) {
+      const uint32_t h = lane / 32, c = lane % 32;
+      const uint32_t at_k = place(r * (2 * D) + 16 * (h ^ key_swizzle<D / 8>(r)));
+      const uint32_t at_v = place((h * D + c) * 16);
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) k[i] = *reinterpret_cast<const bf16x8*>(kt + (at_k ^ (32u * i)));
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i)  // octets h and 2 + h, D / 32 columns each
+        v[i] = *reinterpret_cast<const bf16x8*>(vt + at_v +
+                                                (2 * (i / (D / 32)) * D + 32 * (i % (D / 32))) * 16);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+  __device__ __forceinline__ void logits(const unsigned char* kt, int lane, uint32_t r,
+                                         const RowFrag<T> (&q)[kRowSteps<T, D>], f32x16& s) const {
+    if constexpr (kB) {
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) s = mfma32(k[i], q[i], s);
+    } else {
+      row_product<T, D>(kt, lane, r, q, [](int x) { return key_swizzle<D * sizeof(T) / 16>(x); }, s);
+    }
+  }
+  // o += V^T P^T: register 8 j + e of the weights is position e of octet 2 j + h. bf16:
+  // the matrix product takes the weights rounded to bf16 (by at most half a step, 2^-8;
+  // their sum is of the unrounded ones).
+  __device__ __forceinline__ void values(const unsigned char* vt, int lane, const f32x16& w,
+                                         f32x16 (&o)[D / 32]) const {
+    const uint32_t h = lane / 32, c = lane % 32, at = place((h * D + c) * 8 * sizeof(T));
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      if constexpr (kB) {
+        bf16x8 p;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) p[e] = (bf16)w[8 * j + e];
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) o[i] = mfma32(v[j * (D / 32) + i], p, o[i]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+          for (int e = 0; e < 8; e += 4) {
+            const f32x4 x =
+                *reinterpret_cast<const f32x4*>(vt + at + (2 * j * D + 32 * i) * 32 + 4 * e);
+#pragma unroll
+            for (int n = 0; n < 4; ++n) o[i] = mfma32(x[n], w[8 * j + e + n], o[i]);
+          }
+      }
+    }
+  }
+};
+
+// Buffers of staged tiles, as far ahead as the copies are issued: a tile of a workgroup
+// alone on its CU takes less time than a copy needs to land. Three native buffers, two
+// tiles ahead; two where a third would take the LDS of a second workgroup (fp32, d =
+// 128). 4 bits wait in registers, two tiles ahead, and are decoded to two buffers.
+// Each is an array of its own, and the loop unrolled over them: the compiler then
+// knows that a step's reads do not touch what its copies write, and waits for none.
 template <typename T, int D, bool FP4>
-__device__ __forceinline__ void shared_run(const PrefixArgs& p, int tile, int hkv, int split,
-                                           unsigned char* lds) {
+constexpr int kBuffers = !FP4 && 32 * D * sizeof(T) <= 8192 ? 3 : 2;
+template <typename T, int D, bool FP4>
+constexpr int kTilesAhead = FP4 || kBuffers<T, D, FP4> == 3 ? 2 : 1;
+struct Buffers {
+  unsigned char *k[3], *v[3];
+};
+// The same arrays as the exchange area of the other workgroups (one for each wave),
+// the units of consecutive rows permuted.
+template <int D>
+struct SharedExchange {
+  unsigned char* o[kWaves];
+  __device__ __forceinline__ f32x4& unit(int wave, int row, int u) {
+    unsigned char* p = wave == 0 ? o[0] : wave == 1 ? o[1] : wave == 2 ? o[2] : o[3];
+    return reinterpret_cast<f32x4*>(p)[row * (D / 4) + (u ^ row % 16)];
+  }
+};
+
+// Run `split` of `runs` of the shared positions of rows r0 .. r0 + 127 of a group
+// and one key-value head.
+template <typename T, int D, bool FP4>
+__device__ __forceinline__ void shared_run(const PrefixArgs& p, const Group& t, int r0, int hkv,
+                                           int split, int runs, const Buffers& lds) {
   constexpr bool kB = Elem<T>::kBf16;
-  constexpr int ESZ = sizeof(T), U = D * ESZ / 16, TILE = 32 * D * ESZ;
+  constexpr int ESZ = sizeof(T), U = D * ESZ / 16;
   constexpr int RPC = 64 / U, CPW = 8 / RPC, DT = D / 32;
-  constexpr int KQ = kB ? D / 16 : D / 2;
-  using Frag = typename std::conditional<kB, bf16x8, float>::type;
   const CacheAttnArgs& a = p.c;
   const int lane = threadIdx.x % kWave;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int h = lane / 32, c = lane % 32;
-  RowTile t;
-  if (!find_rows(a, tile, lane, t)) return;
-  const int n_tiles = (t.P + 31) / 32, runs = runs_of(t.P, p.splits);
-  if (split >= runs) return;
+  const int n_tiles = t.tiles();
   const int t_begin = (int)((long long)n_tiles * split / runs);
   const int t_end = (int)((long long)n_tiles * (split + 1) / runs);
 
   // ---- the lane's row -------------------------------------------------------------
   const int per = a.n_q * a.G;
-  const int row0 = t.r0 + 32 * wave, row = row0 + c;
+  const int row0 = r0 + 32 * wave, row = row0 + c;
   const bool has_row = row < t.rows, wave_has = row0 < t.rows;
   const int at_row = min(row, t.rows - 1), s = t.first + at_row / per;
   const int qi = at_row % per / a.G, hq = hkv * a.G + at_row % a.G;
   const int see = min(t.P, length_of(a, s) - a.n_q + qi + 1);  // positions it sees
-  Frag q[KQ];
-  {
-    const T* qp = static_cast<const T*>(a.Q) + ((size_t)s * a.n_q + qi) * a.q_stride +
-                  (size_t)hq * D;
-#pragma unroll
-    for (int k = 0; k < KQ; ++k) {
-      if constexpr (kB) {
-        q[k] = *reinterpret_cast<const bf16x8*>(qp + 16 * k + 8 * h);
-      } else if (k % 4 == 0) {
-        const f32x4 v = *reinterpret_cast<const f32x4*>(qp + 2 * k + 4 * h);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) q[k + e] = v[e];
-      }
-    }
-  }
+  RowFrag<T> q[kRowSteps<T, D>];
+  load_row<T, D>(static_cast<const T*>(a.Q) + ((size_t)s * a.n_q + qi) * a.q_stride +
+                     (size_t)hq * D,
+                 h, q);
 
   // ---- pages, and tiles to LDS -------------------------------------------------------
   // A tile lies in one page, or (16 positions a page) in two; wave w copies its
@@ -133,50 +203,56 @@ __device__ __forceinline__ void shared_run(const PrefixArgs& p, int tile, int hk
   // the positions take no part.
   const PageLayout L = page_layout(FP4, ESZ, 1 << a.cache.ps_log2, D);
   const int ps_mask = (1 << a.cache.ps_log2) - 1;
-  const int32_t* pages = a.cache.table + (size_t)t.first * a.cache.max_pages;
+  // read as constants (no kernel writes the table): scalar loads, which do not stand
+  // behind the copies
+  const auto pages = (const __attribute__((address_space(4))) int32_t*)(
+      uintptr_t)(a.cache.table + (size_t)t.first * a.cache.max_pages);
   struct Pages {
-    int id[2];  // -1: none
+    int id[2];
   };
+  // asked for a tile before they are used, so nothing is decided on them here;
+  // positions past the last one ask for its page
   auto lookup = [&](int i) {
-    Pages r{{-1, -1}};
-    if (i >= t_end) return r;
+    Pages r;
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      const int pos = 32 * i + 16 * k;
-      if (pos >= t.P) continue;
-      const int id = pages[pos >> a.cache.ps_log2];
-      r.id[k] = (unsigned)id < (unsigned)a.cache.n_pages ? id : -1;
-    }
+    for (int k = 0; k < 2; ++k) r.id[k] = pages[min(32 * i + 16 * k, t.P - 1) >> a.cache.ps_log2];
     return r;
   };
+  auto exists = [&](int id) { return (unsigned)id < (unsigned)a.cache.n_pages; };
   auto bits_of = [&](int i, const Pages& g) {  // positions that can be read
     const int n = t.P - 32 * i;
     const uint32_t in = n >= 32 ? ~0u : (1u << n) - 1u;
-    return in & ((g.id[0] < 0 ? 0u : 0xffffu) | (g.id[1] < 0 ? 0u : 0xffff0000u));
+    return in & ((exists(g.id[0]) ? 0xffffu : 0u) | (exists(g.id[1]) ? 0xffff0000u : 0u));
   };
-  struct Raw {  // 4 bits: a thread's share of a tile
-    uint32_t k[D / 64], v[D / 64], vs[D / 64], ks;
+  typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+  struct Raw {  // 4 bits: a thread's share of a tile (d = 64: the first words)
+    u32x2 k, v, vs;
+    uint32_t ks;
   };
   auto block_of = [&](const Pages& g) {
-    const int id = max(wave < 2 ? g.id[0] : g.id[1], 0);
-    return a.cache.pool + ((size_t)id * a.cache.Hkv + hkv) * L.bytes;
+    const int id = wave < 2 ? g.id[0] : g.id[1];
+    return a.cache.pool + ((size_t)(exists(id) ? id : 0) * a.cache.Hkv + hkv) * L.bytes;
   };
-  auto issue = [&](int i, const Pages& g, Raw& raw) {
+  auto issue = [&](int i, const Pages& g, Raw& raw, unsigned char* k_to, unsigned char* v_to) {
     const unsigned char* block = block_of(g);
-    const int slot0 = (32 * i + 8 * wave) & ps_mask, b = i & 1;
+    const int slot0 = (32 * i + 8 * wave) & ps_mask;
     if constexpr (FP4) {
-      const unsigned char* kp = block + (slot0 + lane / 8) * (D / 2) + lane % 8 * (D / 16);
-      const unsigned char* vp = block + L.v + slot0 / 8 * (D * 4) + lane * (D / 16);
+      // a wave's share of codes, and of scales, lies together
+      const __amdgpu_buffer_rsrc_t from = rsrc(block);
+      const int codes = slot0 * (D / 2), scales = slot0 * (D / 32), pair = D == 128 ? lane : lane / 2;
+      const int at = lane * (D / 16);
       // K scales: of the lane's D / 8 dimensions; V scales: of its positions
-      raw.ks = block[L.ks + (slot0 + lane / 8) * (D / 32) + lane % 8 * (D / 8) / 32];
-      const int pair = D == 128 ? lane : lane / 2;
-      const unsigned char* sp = block + L.vs + (slot0 / 8 * (D / 32) + pair / 16) * 8 +
-                                (D == 128 ? 0 : lane % 2 * 4);
-#pragma unroll
-      for (int n = 0; n < D / 64; ++n) {
-        raw.k[n] = reinterpret_cast<const uint32_t*>(kp)[n];
-        raw.v[n] = reinterpret_cast<const uint32_t*>(vp)[n];
-        raw.vs[n] = reinterpret_cast<const uint32_t*>(sp)[n];
+      const int at_ks = lane / 8 * (D / 32) + lane % 8 * (D / 8) / 32;
+      const int at_vs = pair / 16 * 8 + (D == 128 ? 0 : lane % 2 * 4);
+      raw.ks = __builtin_amdgcn_raw_buffer_load_b8(from, at_ks, L.ks + scales, 0);
+      if constexpr (D == 128) {
+        raw.k = __builtin_amdgcn_raw_buffer_load_b64(from, at, codes, 0);
+        raw.v = __builtin_amdgcn_raw_buffer_load_b64(from, at, L.v + codes, 0);
+        raw.vs = __builtin_amdgcn_raw_buffer_load_b64(from, at_vs, L.vs + scales, 0);
+      } else {
+        raw.k[0] = __builtin_amdgcn_raw_buffer_load_b32(from, at, codes, 0);
+        raw.v[0] = __builtin_amdgcn_raw_buffer_load_b32(from, at, L.v + codes, 0);
+        raw.vs[0] = __builtin_amdgcn_raw_buffer_load_b32(from, at_vs, L.vs + scales, 0);
       }
     } else {
       const __amdgpu_buffer_rsrc_t rk = rsrc(block + (size_t)slot0 * D * ESZ);
@@ -186,18 +262,16 @@ __device__ __forceinline__ void shared_run(const PrefixArgs& p, int tile, int hk
         const int r = RPC * n + lane / U;  // of the wave's 8 positions
         const uint32_t ko = r * D * ESZ + 16u * ((lane % U) ^ key_swizzle<U>(8 * wave + r));
         __builtin_amdgcn_raw_ptr_buffer_load_lds(
-            rk, (__attribute__((address_space(3))) void*)(lds + b * TILE + 1024 * (wave * CPW + n)),
-            16, ko, 0, 0, 0);
+            rk, (__attribute__((address_space(3))) void*)(k_to + 1024 * (wave * CPW + n)), 16, ko, 0,
+            0, 0);
         __builtin_amdgcn_raw_ptr_buffer_load_lds(
-            rv,
-            (__attribute__((address_space(3))) void*)(lds + (2 + b) * TILE + 1024 * (wave * CPW + n)),
-            16, 1024 * n + 16 * lane, 0, 0, 0);
+            rv, (__attribute__((address_space(3))) void*)(v_to + 1024 * (wave * CPW + n)), 16,
+            1024 * n + 16 * lane, 0, 0, 0);
       }
     }
   };
-  auto unpack = [&](int i, const Raw& raw) {  // 4 bits to the tile's buffer
+  auto unpack = [&](const Raw& raw, unsigned char* kt, unsigned char* vt) {  // 4 bits to LDS
     if constexpr (FP4) {
-      unsigned char *kt = lds + (i & 1) * TILE, *vt = lds + (2 + (i & 1)) * TILE;
       const int r = 8 * wave + lane / 8;
       const float f = __uint_as_float(raw.ks << 23);
       const float fs[4] = {f, f, f, f};
@@ -220,21 +294,22 @@ __device__ __forceinline__ void shared_run(const PrefixArgs& p, int tile, int hk
       // values: columns 2 pair, 2 pair + 1 of 8 positions (or 4 of them at d = 64)
       const int pair = D == 128 ? lane : lane / 2;
       unsigned char* vp = vt + (wave * D + 2 * pair) * 8 * ESZ + (D == 128 ? 0 : lane % 2 * 4 * ESZ);
+      constexpr int N = D / 16;  // positions
+      T e[N][2];
 #pragma unroll
       for (int n = 0; n < D / 64; ++n) {
         float g[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) g[k] = __uint_as_float((raw.vs[n] >> (8 * k) & 0xffu) << 23);
-        T e[4][2];
-        decode4<T>(raw.v[n], g, e);
+        decode4<T>(raw.v[n], g, e + 4 * n);
+      }
+      typedef T Column __attribute__((ext_vector_type(N)));
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          unsigned char* to = vp + k * 8 * ESZ + n * 4 * ESZ;
-          if constexpr (kB)
-            *reinterpret_cast<bf16x4*>(to) = bf16x4{e[0][k], e[1][k], e[2][k], e[3][k]};
-          else
-            *reinterpret_cast<f32x4*>(to) = f32x4{e[0][k], e[1][k], e[2][k], e[3][k]};
-        }
+      for (int k = 0; k < 2; ++k) {
+        Column x;
+#pragma unroll
+        for (int n = 0; n < N; ++n) x[n] = e[n][k];
+        *reinterpret_cast<Column*>(vp + k * 8 * ESZ) = x;
       }
     }
   };
@@ -247,36 +322,57 @@ __device__ __forceinline__ void shared_run(const PrefixArgs& p, int tile, int hk
   for (int i = 0; i < DT; ++i) o[i] = f32x16{};
   const int key_row = (c & 0x13) | (c & 4) << 1 | (c & 8) >> 1;  // bits 2 and 3 exchanged
 
-  Raw raw;
-  Pages now = lookup(t_begin), ahead = lookup(t_begin + 1);
-  issue(t_begin, now, raw);
-  unpack(t_begin, raw);
-  for (int i = t_begin; i < t_end; ++i) {
-    const int b = i & 1;
-    const uint32_t bits = bits_of(i, now);
-    now = ahead;
-    __builtin_amdgcn_s_waitcnt(0);
-    __syncthreads();  // tile i has landed, tile i - 1 is read
-    const bool more = i + 1 < t_end;
-    if (more) {
-      issue(i + 1, now, raw);
-      ahead = lookup(i + 2);
+  constexpr int NB = kBuffers<T, D, FP4>, AHEAD = kTilesAhead<T, D, FP4>;
+  Raw raw[2];
+  uint32_t bits_in[NB];
+#pragma unroll
+  for (int x = 0; x < AHEAD; ++x)
+    if (t_begin + x < t_end) {
+      const Pages g = lookup(t_begin + x);
+      bits_in[x] = bits_of(t_begin + x, g);
+      issue(t_begin + x, g, raw[x % 2], lds.k[x], lds.v[x]);
+    }
+  Pages ahead = lookup(t_begin + AHEAD);
+  // the queries arrive here, before the loop: a wait for them inside it would be one
+  // for the copies too
+#pragma unroll
+  for (int k = 0; k < kRowSteps<T, D>; ++k) asm volatile("" : "+v"(q[k]));
+  unpack(raw[0], lds.k[0], lds.v[0]);
+  auto step = [&](int i, auto slot) {
+    constexpr int S = decltype(slot)::value, N = (S + AHEAD) % NB;
+    unsigned char *kt = lds.k[S], *vt = lds.v[S];
+    const uint32_t bits = bits_in[S];
+    // this wave's copies of tile i have landed (those of tile i + 1 may be on their
+    // way), and what it has decoded is written; then everyone's, and tile i - 1 is read
+    constexpr int kNoVm = 0xc00f, kNoExp = 0x70;
+    if (FP4)
+      __builtin_amdgcn_s_waitcnt(kNoVm | kNoExp);
+    else if (AHEAD == 2 && i + 1 < t_end)
+      __builtin_amdgcn_s_waitcnt(2 * CPW | kNoExp);
+    else
+      __builtin_amdgcn_s_waitcnt(kNoExp);
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    if (i + AHEAD < t_end) {
+      bits_in[N] = bits_of(i + AHEAD, ahead);
+      issue(i + AHEAD, ahead, raw[N % 2], lds.k[N], lds.v[N]);
+      ahead = lookup(i + AHEAD + 1);
+    }
+    // Positions that cannot be read (behind the last shared one, or without a page)
+    // have weight 0, and what lies there may be anything, also infinities and NaN:
+    // their values are cleared, by each wave in its octet.
+    if (bits != ~0u && bits != 0) {
+      T* oct = reinterpret_cast<T*>(vt) + wave * D * 8;
+      for (int x = lane; x < D * 8; x += kWave)
+        if (!(bits >> (8 * wave + x % 8) & 1)) oct[x] = (T)0.f;
+      __syncthreads();
     }
     if (wave_has && bits != 0) {
-      const unsigned char *kt = lds + b * TILE, *vt = lds + (2 + b) * TILE;
+      Operands<T, D> in;
+      in.read(kt, vt, lane, key_row);
       f32x16 sc = f32x16{};
-      const unsigned char* rowp = kt + key_row * (D * ESZ);
-#pragma unroll
-      for (int k = 0; k < U / 2; ++k) {
-        const unsigned char* x = rowp + 16 * ((2 * k + h) ^ key_swizzle<U>(key_row));
-        if constexpr (kB) {
-          sc = mfma32(*reinterpret_cast<const bf16x8*>(x), q[k], sc);
-        } else {
-          const f32x4 v = *reinterpret_cast<const f32x4*>(x);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) sc = mfma32(v[e], q[4 * k + e], sc);
-        }
-      }
+      in.logits(kt, lane, key_row, q, sc);
       // register 8 j + e: position e of octet 2 j + h
       const bool masked = bits != ~0u || __any(32 * i + 32 > see);
       if (masked) {
@@ -315,123 +411,142 @@ __device__ __forceinline__ void shared_run(const PrefixArgs& p, int tile, int hk
         sc[r] = exp2_hw(fmaf(sc[r], a.scale_log2, -ms));
         l += sc[r];
       }
-      // Positions that cannot be read have weight 0, and what lies there may be
-      // anything, also infinities and NaN: their values are cleared. bf16: the matrix
-      // product takes the weights rounded to bf16 (by at most half a step, 2^-8),
-      // their sum l is of the unrounded ones.
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const uint32_t ok = bits >> (16 * j + 8 * h) & 0xffu;
-        const unsigned char* oct = vt + (2 * j + h) * D * 8 * ESZ;
-        if constexpr (kB) {
-          bf16x8 w;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) w[e] = (bf16)sc[8 * j + e];
-#pragma unroll
-          for (int k = 0; k < DT; ++k) {
-            u32x4 x = *reinterpret_cast<const u32x4*>(oct + (32 * k + c) * 16);
-            if (bits != ~0u) {
-#pragma unroll
-              for (int e = 0; e < 4; ++e)
-                x[e] &= (ok >> (2 * e) & 1 ? 0xffffu : 0u) |
-                        (ok >> (2 * e + 1) & 1 ? 0xffff0000u : 0u);
-            }
-            o[k] = mfma32(__builtin_bit_cast(bf16x8, x), w, o[k]);
-          }
-        } else {
-#pragma unroll
-          for (int k = 0; k < DT; ++k)
-#pragma unroll
-            for (int e = 0; e < 8; e += 4) {
-              f32x4 x = *reinterpret_cast<const f32x4*>(oct + ((32 * k + c) * 8 + e) * 4);
-#pragma unroll
-              for (int n = 0; n < 4; ++n) {
-                if (bits != ~0u && !(ok >> (e + n) & 1)) x[n] = 0.f;
-                o[k] = mfma32(x[n], sc[8 * j + e + n], o[k]);
-              }
-            }
-        }
-      }
+      in.values(vt, lane, sc, o);
     }
-    if (more) unpack(i + 1, raw);
+    if (FP4 && i + 1 < t_end) unpack(raw[(S + 1) % 2], lds.k[(S + 1) % NB], lds.v[(S + 1) % NB]);
+  };
+  for (int i = t_begin; i < t_end; i += NB) {
+    step(i, std::integral_constant<int, 0>());
+    if (i + 1 < t_end) step(i + 1, std::integral_constant<int, 1>());
+    if constexpr (NB == 3)
+      if (i + 2 < t_end) step(i + 2, std::integral_constant<int, 2>());
   }
 
   // ---- the rows' states, row by row --------------------------------------------------
   l = add_xor<32>(l);
   if (!fused) ms = m * a.scale_log2;
-  float* part = p.shared_parts +
-                (((size_t)tile * a.cache.Hkv + hkv) * p.splits + split) * part_floats(kTile, D);
-  const int r0 = 32 * wave + c;
   if (!has_row) return;
+  const size_t rows_all = (size_t)a.S * a.n_q * a.Hq;
+  const size_t part = split * rows_all + ((size_t)s * a.n_q + qi) * a.Hq + hq;
   if (h == 0) {
-    part[kTile * D + r0] = ms;
-    part[kTile * (D + 1) + r0] = l;
+    p.shared_parts[p.splits * rows_all * D + part] = ms;
+    p.shared_parts[p.splits * rows_all * (D + 1) + part] = l;
   }
-#pragma unroll
-  for (int i = 0; i < DT; ++i)
-#pragma unroll
-    for (int r = 0; r < 16; r += 4)
-      *reinterpret_cast<f32x4*>(part + r0 * D + 32 * i + 2 * r + 4 * h) =
-          f32x4{o[i][r], o[i][r + 1], o[i][r + 2], o[i][r + 3]};
+  store_row<float, D>(p.shared_parts + part * D, h, 1.f, o);
+}
+
+// Tiles of 32 positions of a run: the fewest that leave no workgroup a second run, if
+// there are that many workgroups. Runs are whole tiles, so with t tiles of rows and
+// heads, n positions' tiles in all and W workgroups that is between n / W and
+// n / (W - t); for up to 16 groups the lanes try 64 lengths between (80 sequences of 5
+// groups in 4 bits 58 to 44 us).
+__device__ __forceinline__ int run_tiles(const PrefixArgs& p, int lane) {
+  const CacheAttnArgs& a = p.c;
+  const float W = p.shared_blocks, heads = a.cache.Hkv;
+  float n = 0.f, t = 0.f;
+  Group mine{0, 0, 0};
+  for (int g = lane; g < a.n_groups; g += kWave) {
+    mine = group_of(a, g);
+    n += (float)mine.row_tiles() * (float)mine.tiles() * heads;
+    t += (float)mine.row_tiles() * heads;
+  }
+  n = wave_sum(n), t = wave_sum(t);
+  const int lo = max(kLeastTiles, (int)fminf(ceilf(n / W), 1e9f));
+  if (t >= W) return __builtin_amdgcn_readfirstlane(lo);
+  const int hi = max(lo, (int)fminf(ceilf(n / (W - t)), 1e9f));
+  if (a.n_groups > 16) return __builtin_amdgcn_readfirstlane(hi);
+  const int per = lo + (int)((long long)(hi - lo) * lane / (kWave - 1));
+  float runs = 0.f;
+  for (int g = 0; g < a.n_groups; ++g) {
+    const Group x{0, __builtin_amdgcn_readlane(mine.rows, g), __builtin_amdgcn_readlane(mine.P, g)};
+    runs += (float)x.row_tiles() * (float)runs_of(x.tiles(), per, p.splits) * heads;
+  }
+  const unsigned long long fits = __ballot(runs <= W);
+  return __builtin_amdgcn_readlane(per, fits ? (int)__builtin_ctzll(fits) : kWave - 1);
+}
+
+// Workgroup w of those that take shared positions: the runs of all groups, row tiles
+// and key-value heads in one line, of which it takes every p.shared_blocks-th. Groups
+// are looked at 64 at a time, one per lane.
+template <typename T, int D, bool FP4>
+__device__ __forceinline__ void shared_runs(const PrefixArgs& p, int w, const Buffers& lds) {
+  const CacheAttnArgs& a = p.c;
+  const int lane = threadIdx.x % kWave;
+  const int per = run_tiles(p, lane);
+  if (w == 0 && threadIdx.x == 0) *p.per = per;
+  long long before = 0;  // runs of the groups before g0
+  long long next = w;
+  for (int g0 = 0; g0 < a.n_groups; g0 += kWave) {
+    Group mine{0, 0, 0};
+    if (g0 + lane < a.n_groups) mine = group_of(a, g0 + lane);
+    const int runs = runs_of(mine.tiles(), per, p.splits);
+    const int n = mine.row_tiles() * runs * a.cache.Hkv;  // at most 2^24 tiles of 64 runs
+    const int incl = wave_incl_scan(n), all = last_lane(incl);
+    while (next < before + all) {
+      const int x = (int)(next - before);
+      const int at = __popcll(__ballot(incl <= x));
+      const Group t{__builtin_amdgcn_readlane(mine.first, at),
+                    __builtin_amdgcn_readlane(mine.rows, at),
+                    __builtin_amdgcn_readlane(mine.P, at)};
+      const int i = x - __builtin_amdgcn_readlane(incl - n, at);
+      const int r = __builtin_amdgcn_readlane(runs, at);
+      // runs of one row tile and head, then heads, then row tiles: those that read the
+      // same positions lie a multiple of the runs apart
+      shared_run<T, D, FP4>(p, t, i / (r * a.cache.Hkv) * kTile, i / r % a.cache.Hkv, i % r, r, lds);
+      __syncthreads();  // the tiles in LDS are read
+      next += p.shared_blocks;
+    }
+    before += all;
+  }
 }
 
 template <typename T, int D, bool FP4, int NT>
-constexpr int kPrefixPerCu = sizeof(T) == 4 && D == 128 ? 2 : kPerCu<T, D, FP4, NT>;
+constexpr int kPrefixPerCu = D == 128 ? 2 : kPerCu<T, D, FP4, NT>;
 
 template <typename T, int D, bool FP4, int NT>
 __global__ __launch_bounds__(kThreads)
 __attribute__((amdgpu_waves_per_eu(kPrefixPerCu<T, D, FP4, NT>)))
 void prefix_kernel(PrefixArgs a) {
-  constexpr int kTiles = 4 * 32 * D * sizeof(T);
-  __shared__ __attribute__((aligned(16))) unsigned char lds[std::max<int>(kTiles, sizeof(Exchange<D>))];
-  if ((int)blockIdx.x < a.shared_blocks) {
-    const int i = blockIdx.x / a.splits;
-    shared_run<T, D, FP4>(a, i / a.c.cache.Hkv, i % a.c.cache.Hkv, blockIdx.x % a.splits, lds);
+  constexpr int TILE = 32 * D * sizeof(T), kThird = kBuffers<T, D, FP4> == 3 ? TILE : 16;
+  __shared__ __attribute__((aligned(16))) unsigned char k0[TILE], k1[TILE], k2[kThird];
+  __shared__ __attribute__((aligned(16))) unsigned char v0[TILE], v1[TILE], v2[kThird];
+  const int n = a.shared_blocks;
+  if ((int)blockIdx.x < n) {
+    shared_runs<T, D, FP4>(a, blockIdx.x, Buffers{{k0, k1, k2}, {v0, v1, v2}});
   } else {
-    cache_attention_run<T, D, FP4, NT, true>(a.c, blockIdx.x - a.shared_blocks,
-                                             gridDim.x - a.shared_blocks,
-                                             *reinterpret_cast<Exchange<D>*>(lds));
+    SharedExchange<D> area{{k0, k1, v0, v1}};
+    cache_attention_run<T, D, FP4, NT, true>(a.c, blockIdx.x - n, gridDim.x - n, area);
   }
 }
 
-// Joins one row's states: those of its own positions (parts of its segment, or the one
-// that a whole segment left) and those of the shared ones.
+// Joins one row's states, a wave a row: those of its own positions (parts of its
+// segment, or the one that a whole segment left) and those of the shared ones. The
+// lanes take 4 columns of 256 / D states each at a time.
 template <typename T, int D, int NT>
 __global__ __launch_bounds__(kThreads) void prefix_join_kernel(PrefixArgs p) {
-  constexpr int R = NT * kRows;
-  constexpr int TPP = D / 4;          // threads per state
-  constexpr int PG = kThreads / TPP;  // states in flight
-  __shared__ float s_f[kMaxWorkgroups + kMaxSplits];  // weight of each state
-  __shared__ float s_red[2 * kWaves];
-  __shared__ __attribute__((aligned(16))) float s_acc[PG][D];
+  constexpr int R = NT * kRows, TPP = D / 4, PG = kWave / TPP;
   const CacheAttnArgs& a = p.c;
-  const int tid = threadIdx.x, wave = tid / kWave, lane = tid % kWave;
-  const int seg = blockIdx.x, rr = blockIdx.y, heads = a.cache.Hkv * a.row_tiles;
+  const int lane = threadIdx.x % kWave;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int seg = blockIdx.x, heads = a.cache.Hkv * a.row_tiles;
+  const int rr = blockIdx.y * kWaves + wave;
   const int s = seg / heads, hr = seg % heads;
-  const int kvh = hr / a.row_tiles, row = hr % a.row_tiles * R + rr, per = a.n_q * a.G;
-  if (row >= per) return;
-  // the group's shared positions, and its tile that holds the row
-  const int g = find_sequence(a.n_groups, s, lane,
-                              [&](int k) { return (long long)group_first(a, k); });
-  const int first = group_first(a, g), end = group_first(a, g + 1);
-  const int P = s >= first && s < end ? shared_length(a, g, first, end) : 0;
-  const int n_own = a.joins[2 * (size_t)seg + 1], first_own = a.joins[2 * (size_t)seg];
+  const int kvh = hr / a.row_tiles, row = hr % a.row_tiles * R + rr;
+  if (rr >= R || row >= a.n_q * a.G) return;
+  const int4 join = *reinterpret_cast<const int4*>(a.joins + 4 * (size_t)seg);
+  const int first_own = join.x, n_own = join.y, P = join.z;
   if (n_own == 1 && P == 0) return;  // stored already
-  const int n_shared = P > 0 ? runs_of(P, p.splits) : 0, n = n_own + n_shared;
+  const int n_shared = P > 0 ? runs_of((P + 31) / 32, *p.per, p.splits) : 0, n = n_own + n_shared;
   const size_t at = ((size_t)s * a.n_q + row / a.G) * a.Hq + kvh * a.G + row % a.G;
   const size_t rows_all = (size_t)a.S * a.n_q * a.Hq;
-  const int r = (s - first) * per + row, rt = r % kTile;
-  const float* shared_parts =
-      p.shared_parts +
-      ((size_t)(tile_of(first, g, per) + r / kTile) * a.cache.Hkv + kvh) * p.splits *
-          part_floats(kTile, D);
   struct State {
     const float *o, *m, *l;
   };
   auto state = [&](int i) {
     if (i >= n_own) {
-      const float* x = shared_parts + (size_t)(i - n_own) * part_floats(kTile, D);
-      return State{x + rt * D, x + kTile * D + rt, x + kTile * (D + 1) + rt};
+      const size_t part = (i - n_own) * rows_all + at;
+      return State{p.shared_parts + part * D, p.shared_parts + p.splits * rows_all * D + part,
+                   p.shared_parts + p.splits * rows_all * (D + 1) + part};
     }
     if (n_own == 1)
       return State{a.states + at * D, a.states + rows_all * D + at,
@@ -440,63 +555,61 @@ __global__ __launch_bounds__(kThreads) void prefix_join_kernel(PrefixArgs p) {
         a.parts + (size_t)(i == 0 ? first_own : 2 * (first_own / 2 + i)) * part_floats(R, D);
     return State{x + rr * D, x + R * D + rr, x + R * (D + 1) + rr};
   };
-  float m = kMaxFloor;
-  for (int i = tid; i < n; i += kThreads) {
-    s_f[i] = *state(i).m;
-    m = fmaxf(m, s_f[i]);
+  float m = kMaxFloor, l = 0.f;
+  for (int i = lane; i < n; i += kWave) {  // a running sum per lane, then over the lanes
+    const State x = state(i);
+    const float mi = *x.m, mn = fmaxf(m, mi);
+    l = l * exp2_hw(m - mn) + *x.l * exp2_hw(mi - mn);
+    m = mn;
   }
+  const float mine = m;
 #pragma unroll
   for (int k = 1; k < kWave; k *= 2) m = fmaxf(m, __shfl_xor(m, k, kWave));
-  if (lane == 0) s_red[wave] = m;
-  __syncthreads();
-  for (int i = 0; i < kWaves; ++i) m = fmaxf(m, s_red[i]);
-  float l = 0.f;
-  for (int i = tid; i < n; i += kThreads) {
-    const float f = exp2_hw(s_f[i] - m);
-    s_f[i] = f;
-    l = fmaf(f, *state(i).l, l);
-  }
+  l *= exp2_hw(mine - m);
 #pragma unroll
   for (int k = 1; k < kWave; k *= 2) l += __shfl_xor(l, k, kWave);
-  if (lane == 0) s_red[kWaves + wave] = l;
-  __syncthreads();
-  l = 0.f;
-  for (int i = 0; i < kWaves; ++i) l += s_red[kWaves + i];
-  const int pg = tid / TPP, d0 = tid % TPP * 4;
+  const int d0 = lane % TPP * 4;
   f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-  for (int i = pg; i < n; i += PG) acc += s_f[i] * *reinterpret_cast<const f32x4*>(state(i).o + d0);
-  *reinterpret_cast<f32x4*>(&s_acc[pg][d0]) = acc;
-  __syncthreads();
-  const float inv = l > 0.f ? 1.f / l : 0.f;
-  if (tid < D) {
-    float y = 0.f;
-#pragma unroll
-    for (int i = 0; i < PG; ++i) y += s_acc[i][tid];
-    static_cast<T*>(a.Y)[at * D + tid] = (T)(y * inv);
+#pragma unroll 8
+  for (int i = lane / TPP; i < n; i += PG) {
+    const State x = state(i);
+    acc += exp2_hw(*x.m - m) * *reinterpret_cast<const f32x4*>(x.o + d0);
   }
-  if (a.lse && tid == 0) a.lse[at] = l > 0.f ? (m + log2_hw(l)) * kLn2 : -INFINITY;
+#pragma unroll
+  for (int k = TPP; k < kWave; k *= 2)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], k, kWave);
+  if (lane >= TPP) return;
+  const float inv = l > 0.f ? 1.f / l : 0.f;
+  T* y = static_cast<T*>(a.Y) + at * D + d0;
+  if constexpr (Elem<T>::kBf16)
+    *reinterpret_cast<bf16x4*>(y) = bf16x4{(bf16)(acc[0] * inv), (bf16)(acc[1] * inv),
+                                           (bf16)(acc[2] * inv), (bf16)(acc[3] * inv)};
+  else
+    *reinterpret_cast<f32x4*>(y) = acc * inv;
+  if (a.lse && lane == 0) a.lse[at] = l > 0.f ? (m + log2_hw(l)) * kLn2 : -INFINITY;
 }
 
 int row_tiles_of(int n_q, int G, int NT) { return (n_q * G + NT * kRows - 1) / (NT * kRows); }
 
-// Parts of the workspace, in floats (joins: as many 4-byte integers).
+// Parts of the workspace, in floats (joins and per: as many 4-byte integers).
 struct Plan {
-  long long tiles;
   int splits;
   size_t parts, states, shared, joins;
 };
 Plan plan_of(int S, int n_groups, int n_q, int Hq, int Hkv, int D) {
   const long long rows = (long long)S * n_q * (Hq / Hkv);
   Plan p;
-  p.tiles = rows / kTile + n_groups;
-  // as if all groups had as many sequences; about a workgroup per CU
+  // four times the runs of a tile that fill the device if all groups were alike: the
+  // longest shared positions are divided finer; none where the tiles alone fill it
   const long long own = std::max((rows + kTile - 1) / kTile, (long long)n_groups) * Hkv;
-  p.splits = (int)std::min<long long>(std::max(1LL, 256 / own), kMaxSplits);
+  constexpr int kBlocks = 256;
+  p.splits = own >= kBlocks ? 1
+                            : (int)std::min<long long>(4 * ((kBlocks + own - 1) / own), kMaxSplits);
   p.parts = kMaxWorkgroups * 2 * part_floats(kRows, D);
   p.states = ((size_t)S * n_q * Hq * (D + 2) + 3) / 4 * 4;
-  p.shared = (size_t)p.tiles * Hkv * p.splits * part_floats(kTile, D);
-  p.joins = (size_t)S * Hkv * row_tiles_of(n_q, Hq / Hkv, 1) * 2;
+  p.shared = ((size_t)S * n_q * Hq * p.splits * (D + 2) + 3) / 4 * 4;
+  p.joins = (size_t)S * Hkv * row_tiles_of(n_q, Hq / Hkv, 1) * 4;
   return p;
 }
 
@@ -504,22 +617,22 @@ template <typename T, int D, bool FP4, int NT>
 hipError_t launch_tiles(PrefixArgs& a, hipStream_t stream) {
   a.c.row_tiles = row_tiles_of(a.c.n_q, a.c.G, NT);
   const long long segs = (long long)a.c.S * a.c.cache.Hkv * a.c.row_tiles;
-  // short sequences are not divided, as without groups
-  const long long room =
-      (((long long)a.c.cache.max_pages << a.c.cache.ps_log2) + kUnit - 1) / kUnit;
-  a.c.unit = kUnit * (room <= kWholeSteps ? (int)room : 1);
-  const long long cap = room <= kWholeSteps ? 1 : room;  // units of a segment, at most
+  a.c.unit = kUnit;
   DeviceInfo dev;
   hipError_t e = device_info(&dev);
   if (e != hipSuccess) return e;
-  const long long slots = std::min(kMaxWorkgroups / NT, dev.cus * kPrefixPerCu<T, D, FP4, NT>);
-  const unsigned W = (unsigned)std::min(segs * cap, slots);
-  hipLaunchKernelGGL((prefix_kernel<T, D, FP4, NT>), dim3((unsigned)a.shared_blocks + W),
-                     dim3(kThreads), 0, stream, a);
+  // As many workgroups as run at once, one per CU of them (the first) for the shared
+  // positions: two of these on a CU take nearly twice as long. us (d = 128, bf16) with
+  // 256 of 512 workgroups and with as many as the work's proportion asks for, up to 448:
+  // 256 sequences that share 32000 positions 139 / 163, 64 that share 16000 41 / 42.
+  const int W = std::min(kMaxWorkgroups / NT, dev.cus * kPrefixPerCu<T, D, FP4, NT>);
+  a.shared_blocks = std::min(dev.cus, W / 2);
+  hipLaunchKernelGGL((prefix_kernel<T, D, FP4, NT>), dim3((unsigned)W), dim3(kThreads), 0, stream, a);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL((prefix_join_kernel<T, D, NT>),
-                     dim3((unsigned)segs, (unsigned)std::min(NT * kRows, a.c.n_q * a.c.G)),
+                     dim3((unsigned)segs, (unsigned)(std::min(NT * kRows, a.c.n_q * a.c.G) + kWaves - 1) /
+                                              kWaves),
                      dim3(kThreads), 0, stream, a);
   return hipGetLastError();
 }
@@ -528,7 +641,7 @@ hipError_t launch_tiles(PrefixArgs& a, hipStream_t stream) {
 
 size_t prefix_attention_workspace(int S, int n_groups, int n_q, int Hq, int Hkv, int d) {
   const Plan p = plan_of(S, n_groups, n_q, Hq, Hkv, d);
-  return (p.parts + p.states + p.shared + p.joins) * sizeof(float);
+  return (p.parts + p.states + p.shared + p.joins + 4) * sizeof(float);
 }
 
 template <typename T, int D>
@@ -537,6 +650,12 @@ hipError_t launch_prefix_attention(const CacheShape& c, int S, int n_groups, int
                                    const int32_t* lens, const int32_t* table,
                                    const int32_t* cu_groups, const int32_t* shared, void* Y,
                                    float* lse, void* workspace, hipStream_t stream) {
+  // Caches with room for few positions are attended to without sharing, by one launch:
+  // 4 sequences that share 300 positions 7.6 us instead of 11.7, 64 that share 400 of
+  // 512 11.7 instead of 17.4.
+  if ((long long)c.max_pages * c.page_size <= AVQ_CACHE_UNDIVIDED)
+    return launch_cache_attention<T, D>(c, S, n_q, Hq, scale, Q, q_stride, cache, lens, table, Y,
+                                        lse, nullptr, stream);
   const Plan plan = plan_of(S, n_groups, n_q, Hq, c.Hkv, D);
   PrefixArgs p{};
   CacheAttnArgs& a = p.c;
@@ -550,8 +669,8 @@ hipError_t launch_prefix_attention(const CacheShape& c, int S, int n_groups, int
   a.states = a.parts + plan.parts;
   p.shared_parts = a.states + plan.states;
   a.joins = reinterpret_cast<int32_t*>(p.shared_parts + plan.shared);
-  p.tiles = (int)plan.tiles, p.splits = plan.splits;
-  p.shared_blocks = (int)(plan.tiles * c.Hkv * plan.splits);
+  p.per = a.joins + plan.joins;
+  p.splits = plan.splits;
   p.lazy = kLazy / a.scale_log2;
   if constexpr (Elem<T>::kBf16) {
     if (n_q * a.G > kRows)

@@ -94,8 +94,8 @@ CASES = {
         (dict(scale=NAN), INVALID), (dict(cache=None), INVALID), (dict(lens=None), INVALID),
         (dict(table=None), INVALID), (dict(cu=None), INVALID), (dict(shared=None), INVALID),
         (dict(Y=None), INVALID), (dict(cu=ODD), INVALID), (dict(shared=ODD), INVALID),
-        (dict(lse=ODD), INVALID), (dict(ws=None), INVALID), (dict(ws=ODD), INVALID),
-        (dict(ws_bytes=64), INVALID), (dict(S=1024, ps=256, max_pages=1 << 20), UNSUPPORTED)],
+        (dict(lse=ODD), INVALID), (dict(ws=None, max_pages=33), INVALID),
+        (dict(ws=ODD), INVALID), (dict(ws_bytes=64), INVALID), (dict(S=1024, ps=256, max_pages=1 << 20), UNSUPPORTED)],
 }
 
 

@@ -14,9 +14,10 @@ BF16, F32 = torch.bfloat16, torch.float32
 
 class Setup:
     """groups: (shared positions, lengths of the group's sequences); a sequence's
-    shared positions are those it has of them. Slots behind the lengths hold anything."""
+    shared positions are those it has of them. Slots behind the lengths hold anything.
+    The tables have room for `room` positions (nothing is shared up to 512)."""
 
-    def __init__(self, groups, Hq, Hkv, d, dtype, fp4=False, ps=16, n_q=1, seed=0):
+    def __init__(self, groups, Hq, Hkv, d, dtype, fp4=False, ps=16, n_q=1, seed=0, room=513):
         self.__dict__.update(Hq=Hq, Hkv=Hkv, d=d, dtype=dtype, fp4=fp4, ps=ps, n_q=n_q)
         g = torch.Generator().manual_seed(seed)
         self.lens = [n for _, lens in groups for n in lens]
@@ -47,7 +48,8 @@ class Setup:
                     holder, held = row, n
         self.n_pages = next_page + 2
         order = torch.randperm(self.n_pages, generator=g).tolist()
-        self.table = torch.full((self.S, max(1, max(map(len, rows)))), -7, dtype=torch.int32)
+        columns = max(1, -(-room // ps), max(map(len, rows)))
+        self.table = torch.full((self.S, columns), -7, dtype=torch.int32)
         for i, row in enumerate(rows):
             self.table[i, :len(row)] = torch.tensor([order[p] for p in row], dtype=torch.int32)
         E = avq.cache_page_bytes(dtype, ps, d, fp4)
@@ -135,6 +137,18 @@ def test_groups(groups, d, fp4, dtype):
     s.check(*s.run())
 
 
+@pytest.mark.parametrize("fp4", [False, True])
+def test_room_for_few_positions(fp4):
+    """Up to 512 positions nothing is shared: no workspace, the same bits as without
+    groups."""
+    s = Setup([(100, [101, 160, 0]), (30, [40, 41])], 4, 2, 64, BF16, fp4, 16, room=512)
+    Y, lse = s.run()
+    s.check(Y, lse)
+    y, l = avq.cache_attention_fwd(*(x.cuda() for x in (s.Q, s.cache, s.table, torch.tensor(
+        s.lens, dtype=torch.int32))), 16, 0.2, fp4=fp4, with_lse=True)
+    assert torch.equal(y.cpu(), Y) and torch.equal(l.cpu(), lse)
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("fp4", [False, True])
 @pytest.mark.parametrize("ps", [16, 32, 64, 256])
@@ -195,12 +209,11 @@ def test_positions_without_a_page(fp4):
     s = Setup([(96, [100, 120, 110])], 4, 2, 64, BF16, fp4, 16, seed=7)
     s.table[:, 1], s.table[:, 4] = 10 ** 6, -1
     s.check(*s.run())
-    s = Setup([(96, [128, 120, 110])], 4, 2, 64, BF16, fp4, 16, seed=8)
-    lens = list(s.lens)
-    s.lens = [10 ** 9, 120, -5]
-    Y, lse = s.run()
-    s.check(Y, lse, lens=[128, 120, 0])
-    s.lens = lens
+    for longest in (128, 640):  # not shared and shared
+        s = Setup([(96, [longest, 120, 110])], 4, 2, 64, BF16, fp4, 16, seed=8, room=0)
+        s.lens = [10 ** 9, 120, -5]
+        Y, lse = s.run()
+        s.check(Y, lse, lens=[longest, 120, 0])
 
 
 @pytest.mark.parametrize("fp4", [False, True])
@@ -238,6 +251,7 @@ def test_strided_queries_and_untouched_cache():
 
 def test_refusals_on_the_gpu():
     s = Setup([(40, [41, 50])], 2, 1, 64, BF16)
+    assert s.table.shape[1] * 16 > 512
     lens = torch.tensor(s.lens, dtype=torch.int32)
     names = ("Q", "cache", "block_table", "lens", "cu_groups", "shared")
     good = dict(zip(names, (x.cuda() for x in (s.Q, s.cache, s.table, lens, s.cu, s.shared))))

@@ -83,10 +83,10 @@ def test_answers_to_one_clip(fp4):
     E = avq.cache_page_bytes(BF16, ps, d, fp4)
     whole = T // ps
     cache = torch.zeros(whole + 3 * n, Hkv, E, dtype=torch.uint8, device="cuda")
-    table = torch.zeros(n, whole + 3, dtype=torch.int32)
+    table = torch.zeros(n, 40, dtype=torch.int32)  # room for 640 positions
     table[:, :whole] = torch.arange(whole)
     for i in range(n):
-        table[i, whole:] = whole + 3 * i + torch.arange(3)
+        table[i, whole:whole + 3] = whole + 3 * i + torch.arange(3)
     dev_table = table.cuda()
     Q, K, V = (torch.randn(T, h, d, generator=g).to(BF16).cuda() for h in (Hq, Hkv, Hkv))
     Q, K = avq.rotate_axes(Q, K, pos.cuda(), *c, axis)
