@@ -97,9 +97,10 @@ void cross_kernel(CrossArgs a) {
     f32x16 sc = f32x16{};
     row_product<T, D>(lds + b * TILE, lane, c, q, kswz, sc);
     if (bits != ~0u) {
+      const uint32_t mine = place(bits >> (4 * h));
 #pragma unroll
       for (int r = 0; r < 16; ++r)
-        if (!(bits >> (8 * (r / 4) + 4 * h + r % 4) & 1)) sc[r] = -INFINITY;
+        if (!(mine & 1u << (8 * (r / 4) + r % 4))) sc[r] = -INFINITY;
     }
     float mx = sc[0];
 #pragma unroll

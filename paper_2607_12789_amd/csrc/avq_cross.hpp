@@ -92,8 +92,9 @@ inline CrossSplit cross_split(long long own, long long others, int S, int Hkv, i
   return {(int)per, (int)std::max(1LL, std::min(most, 64LL))};
 }
 
-// Parts: rows [splits][rows][D], then, of the forward pass, maxima and sums
-// [splits][rows] each, where row = query * Hq + head (states: state * Hkv + head).
+// Parts: rows [splits][rows][D], where row = query * Hq + head (states: state * Hkv +
+// head); then, of the forward pass, maxima and sums [splits][rows] each; of dQ in bf16
+// sum P k [splits][rows][D] and two sums of dS [splits][rows] each; of dK dV [splits][rows][D].
 enum CrossJoin { kJoinSoftmax, kJoinQueries, kJoinStates };
 
 // Joins the parts of one row, in their order: kWaves waves a row, whose lanes take 4
@@ -102,6 +103,7 @@ template <typename T, int D, CrossJoin kWhat, int kWaves>
 __global__ __launch_bounds__(256) void cross_join_kernel(CrossArgs a) {
   constexpr int TPP = D / 4, PG = kWaves * kWave / TPP, kRows = 4 / kWaves;
   constexpr bool kStates = kWhat == kJoinStates;
+  constexpr bool kMend = kWhat == kJoinQueries && Elem<T>::kBf16;
   __shared__ __attribute__((aligned(16))) float s_acc[kWaves == 1 ? 1 : PG][D];
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
   const int heads = kStates ? a.Hkv : a.Hq, T_ = kStates ? a.Tk : a.Tq;
@@ -133,6 +135,17 @@ __global__ __launch_bounds__(256) void cross_join_kernel(CrossArgs a) {
 #pragma unroll
     for (int k = 1; k < kWave; k *= 2) l += __shfl_xor(l, k, kWave);
   }
+  float rest = 0.f, rounded = 0.f;
+  if (kMend) {
+    const float* const rests = a.parts + 2 * (size_t)a.splits * rows * D;
+    rest = lane < n ? rests[lane * rows + row] : 0.f;
+    rounded = lane < n ? rests[(a.splits + lane) * rows + row] : 0.f;
+#pragma unroll
+    for (int k = 1; k < kWave; k *= 2) {
+      rest += __shfl_xor(rest, k, kWave);
+      rounded += __shfl_xor(rounded, k, kWave);
+    }
+  }
   f32x4 x = f32x4{0.f, 0.f, 0.f, 0.f}, y = x;
 #pragma unroll 4
   for (int i = pg; i < n; i += PG) {
@@ -142,7 +155,7 @@ __global__ __launch_bounds__(256) void cross_join_kernel(CrossArgs a) {
       x += exp2_hw(ms[i * rows + row] - m) * v;
     else
       x += v;
-    if (kStates) y += *reinterpret_cast<const f32x4*>(part + (size_t)a.splits * rows * D);
+    if (kStates || kMend) y += *reinterpret_cast<const f32x4*>(part + (size_t)a.splits * rows * D);
   }
   // the groups of lanes, then the waves
   auto gather = [&](f32x4& v) {
@@ -160,7 +173,7 @@ __global__ __launch_bounds__(256) void cross_join_kernel(CrossArgs a) {
     }
   };
   gather(x);
-  if (kStates) gather(y);
+  if (kStates || kMend) gather(y);
   if (wave % kWaves != 0 || lane >= TPP) return;
   auto store = [&](void* out, const f32x4& v) {
     T* o = static_cast<T*>(out) + row * D + d0;
@@ -173,7 +186,8 @@ __global__ __launch_bounds__(256) void cross_join_kernel(CrossArgs a) {
     store(a.Y, (l > 0.f ? 1.f / l : 0.f) * x);
     if (a.lse && lane == 0) a.lse[row] = l > 0.f ? (m + log2_hw(l)) * kLn2 : -INFINITY;
   } else if (kWhat == kJoinQueries) {
-    store(a.dQ, a.scale * x);
+    store(a.dQ, a.scale * (kMend ? x - rounded * y : x));
+    if (kMend && lane == 0 && wave % kWaves == 0) a.delta[row] += rest;
   } else {
     store(a.dK, a.scale * x);
     store(a.dV, y);

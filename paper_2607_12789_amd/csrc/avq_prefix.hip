@@ -376,11 +376,12 @@ __device__ __forceinline__ void shared_run(const PrefixArgs& p, const Group& t, 
       // register 8 j + e: position e of octet 2 j + h
       const bool masked = bits != ~0u || __any(32 * i + 32 > see);
       if (masked) {
+        const int n = see - 32 * i;  // of the lane's row
+        const uint32_t sees = n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u;
+        const uint32_t mine = place((bits & sees) >> (8 * h));
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int k = 16 * (r / 8) + 8 * h + r % 8;
-          if (!(bits >> k & 1) || 32 * i + k >= see) sc[r] = -INFINITY;
-        }
+        for (int r = 0; r < 16; ++r)
+          if (!(mine & 1u << (16 * (r / 8) + r % 8))) sc[r] = -INFINITY;
       }
       float mx = sc[0];
 #pragma unroll

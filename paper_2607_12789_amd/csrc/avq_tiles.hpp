@@ -125,13 +125,40 @@ __device__ __forceinline__ void row_product(const unsigned char* tile, int lane,
   }
 }
 
-// acc[i][column of 32 i ..][lane's column] += sum_row tile[row][column] w[row]: 32
-// staged rows read transposed, the weights as the row product left them (row
-// 8 (r / 4) + 4 h + r % 4 in register r). bf16: the matrix product takes them
-// rounded to bf16.
-template <typename T, int D, typename Swizzle>
-__device__ __forceinline__ void column_product(const unsigned char* tile, int lane, const f32x16& w,
-                                               Swizzle swizzle, f32x16 (&acc)[D / 32]) {
+// The weights of 32 rows as the row product left them (row 8 (r / 4) + 4 h + r % 4 in
+// register r), as the operand of a product over the rows: bf16 rounded, 16 rows each.
+template <typename T>
+struct Weights {
+  f32x16 w;
+  __device__ __forceinline__ explicit Weights(const f32x16& x) : w(x) {}
+};
+template <>
+struct Weights<bf16> {
+  bf16x8 w[2];
+  __device__ __forceinline__ explicit Weights(const f32x16& x) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) w[k][e] = (bf16)x[8 * k + e];
+  }
+  // x plus the sum of the rounded weights: two of them a step
+  __device__ __forceinline__ float sum(float x) const {
+    const bf16x2 one{(bf16)1.f, (bf16)1.f};
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+      for (int e = 0; e < 8; e += 2)
+        x = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{w[k][e], w[k][e + 1]}, one, x, false);
+    return x;
+  }
+};
+
+// acc[n][i][column of 32 i ..][lane's column] += sum_row tile[row][column] w[n][row]:
+// 32 staged rows read transposed, once for N sets of weights.
+template <typename T, int D, int N, typename Swizzle>
+__device__ __forceinline__ void column_products(const unsigned char* tile, int lane,
+                                                const Weights<T> (&w)[N], Swizzle swizzle,
+                                                f32x16 (&acc)[N][D / 32]) {
   constexpr uint32_t kRow = D * sizeof(T);
   const uint32_t h = lane / 32, c = lane % 32;
   if constexpr (Elem<T>::kBf16) {
@@ -140,10 +167,7 @@ __device__ __forceinline__ void column_product(const unsigned char* tile, int la
     const uint32_t at =
         place(row * kRow + 16 * ((c / 16 * 2 + c % 4 / 2) ^ swizzle(row)) + 8 * (c % 2));
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      bf16x8 p;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) p[e] = (bf16)w[8 * k + e];
+    for (int k = 0; k < 2; ++k)
 #pragma unroll
       for (int i = 0; i < D / 32; ++i) {
         bf16x8 v;
@@ -155,9 +179,9 @@ __device__ __forceinline__ void column_product(const unsigned char* tile, int la
 #pragma unroll
           for (int j = 0; j < 4; ++j) v[4 * e + j] = part[j];
         }
-        acc[i] = mfma32(v, p, acc[i]);
+#pragma unroll
+        for (int n = 0; n < N; ++n) acc[n][i] = mfma32(v, w[n].w[k], acc[n][i]);
       }
-    }
   } else {
     const uint32_t at = place(4 * h * kRow + 16 * (c / 4 ^ swizzle(4 * h)) + 4 * (c % 4));
 #pragma unroll
@@ -167,10 +191,18 @@ __device__ __forceinline__ void column_product(const unsigned char* tile, int la
       for (int i = 0; i < D / 32; ++i) {
         const float v = *reinterpret_cast<const float*>(
             tile + (at ^ (128u * i) ^ (16u * swizzle(row))) + row * kRow);
-        acc[i] = mfma32(v, w[r], acc[i]);
+#pragma unroll
+        for (int n = 0; n < N; ++n) acc[n][i] = mfma32(v, w[n].w[r], acc[n][i]);
       }
     }
   }
+}
+template <typename T, int D, typename Swizzle>
+__device__ __forceinline__ void column_product(const unsigned char* tile, int lane, const f32x16& w,
+                                               Swizzle swizzle, f32x16 (&acc)[D / 32]) {
+  const Weights<T> one[1] = {Weights<T>(w)};
+  column_products<T, D, 1>(tile, lane, one, swizzle,
+                           reinterpret_cast<f32x16(&)[1][D / 32]>(acc));
 }
 
 // Index of row r of a tile of rows that are numbered row = query * G + head:

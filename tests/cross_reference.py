@@ -11,8 +11,14 @@ sum |q_i k_j| of a row, B_ij = sum_d |dY_id v_jd|, C_i = sum_d |dY_id Y_id|:
     exponential by a few roundings: P_ij is off relatively by at most
     eP_i = ((d + 12) A_i + 4 |lse_i| + 16) u;
   * dP_ij by (d + 1) u B_ij, delta_i by (d + 1) u C_i and, Y being rounded, h C_i;
-  * dS_ij = P_ij (dP_ij - delta_i) by
+  * fp32: dS_ij = P_ij (dP_ij - delta_i) by
     eS_ij = P_ij ((eP_i + 3 u) (|dP_ij| + |delta_i|) + (d + 1) u (B_ij + C_i) + h C_i);
+  * bf16: delta_i is mended by rest_i = sum_j dS_ij, which is 0 for the exact one. With
+    e_ij = eS_ij without h C_i, and n states, rest_i is off by E_i = sum_j e_ij +
+    (n + 64) u sum_j |dS_ij|, and so is delta_i. What h C_i was leaves two products of
+    it with a rounding to bf16: of the dS it is in and of the P it is taken off with.
+    So eS_ij = e_ij + P_ij (E_i + 2 h h C_i). dQ takes rest_i from the dS as rounded
+    to bf16: P_ij h sum_j |dS_ij| more;
   * bf16: P and dS are rounded once more before their products: h |P|, h |dS|;
   * a sum of n products is off by (n + 64) u times the sum of their magnitudes, and a
     result by its own rounding.
@@ -74,10 +80,16 @@ def backward64(dY, Q, K, V, lens_q, lens_k, scale, mask=None):
             A = (scale * q.abs() @ k.abs().T).amax(1, keepdim=True)
             B, C = g.abs() @ v.abs().T, (g * Y[a:b, h]).abs().sum(1, keepdim=True)
             eP = ((d + 12) * A + 4 * lse[a:b, h, None].abs() + 16) * U
-            eS = P * ((eP + 3 * U) * (dP.abs() + delta.abs()) + (d + 1) * U * (B + C) + half * C)
+            eS = P * ((eP + 3 * U) * (dP.abs() + delta.abs()) + (d + 1) * U * (B + C))
+            if rounds:
+                E = (eS + (n + 64) * U * dS.abs()).sum(1, keepdim=True)
+                eS = eS + P * (E + 2 * half * half * C)
+            else:
+                eS = eS + P * half * C
             eS = eS + (rounds + (n + 64) * U) * dS.abs()
             out[0][a:b, h] = scale * dS @ k
-            tol[0][a:b, h] = scale * eS @ k.abs()
+            eQ = eS + P * rounds * dS.abs().sum(1, keepdim=True)
+            tol[0][a:b, h] = scale * eQ @ k.abs()
             eS = eS + (rows + 64) * U * dS.abs()
             out[1][keep, h // G] += scale * dS.T @ q
             tol[1][keep, h // G] += scale * eS.T @ q.abs()
