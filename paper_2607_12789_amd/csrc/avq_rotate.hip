@@ -8,7 +8,11 @@
 // Bound by the rows' bytes, each read once and written once. A wave takes one
 // token and all its heads, queries' and keys': its lanes hold two 16-byte pieces
 // of a head each (the a's and the b's of 8 bf16 or 4 fp32 pairs) and the angles of
-// these pairs, looked up once for all heads.
+// these pairs, the same for all heads. The angles are looked up by pairs, one per lane
+// in any order of the axes, and handed over in LDS: two loads a lane, where looking up
+// a lane's own eight pairs takes up to 16 (20003 tokens of 16 heads of 128, half of
+// the dimensions rotated, axes in turn: 37.1 us so, 35.3 now, 4.7 TB/s; 16384 tokens of
+// 40 heads of 128 63 us, 5.3 TB/s, the rate of a large copy).
 #include "avq_launch.hpp"
 #include "avq_common.hpp"
 
@@ -54,41 +58,13 @@ __global__ __launch_bounds__(64 * kWavesPerGroup) void rotate_kernel(RotateArgs 
   const int d_a = turns && !kInterleaved ? i0 : 2 * i0;
   const int d_b = turns && !kInterleaved ? half + i0 : 2 * i0 + P;
 
-  float c[P], s[P];
-#pragma unroll
-  for (int j = 0; j < P; ++j) c[j] = 1.f, s[j] = 0.f;
-  if (turns) {
-    const int w = i0 / 16;
-    const uint32_t word = w == 0 ? a.axes[0] : w == 1 ? a.axes[1] : w == 2 ? a.axes[2] : a.axes[3];
-    const uint32_t mine = word >> (2 * (i0 % 16));
-    auto row = [&](int j) {
-      const int x = mine >> (2 * j) & 3;
-      return (size_t)(x == 0 ? at[0] : x == 1 ? at[1] : x == 2 ? at[2] : at[3]) * half + i0 + j;
-    };
-#pragma unroll
-    for (int q = 0; q < P; q += 4) {
-      const uint32_t four = mine >> (2 * q) & 0xff;
-      if (__all(four == (four & 3) * 0x55)) {  // one axis for each lane's four pairs
-        const f32x4 x = *reinterpret_cast<const f32x4*>(a.cos + row(q));
-        const f32x4 y = *reinterpret_cast<const f32x4*>(a.sin + row(q));
-#pragma unroll
-        for (int j = 0; j < 4; ++j) c[q + j] = x[j], s[q + j] = y[j];
-      } else {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) c[q + j] = a.cos[row(q + j)], s[q + j] = a.sin[row(q + j)];
-      }
-    }
-#pragma unroll
-    for (int j = 0; j < P; ++j) s[j] *= a.sign;
-  }
-
   typedef T Piece __attribute__((ext_vector_type(P)));
   const T* q_in = static_cast<const T*>(a.Q) + (size_t)t * a.q_stride;
   const T* k_in = static_cast<const T*>(a.K) + (size_t)t * a.k_stride;
   T* q_out = static_cast<T*>(a.Q_out) + (size_t)t * a.Hq * D;
   T* k_out = static_cast<T*>(a.K_out) + (size_t)t * (a.H - a.Hq) * D;
-  for (int h0 = lane / C; h0 < a.H; h0 += HP * kAhead) {
-    Piece x[kAhead], y[kAhead];
+  Piece x[kAhead], y[kAhead];
+  auto load = [&](int h0) {
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
       const int h = h0 + HP * i;
@@ -98,6 +74,29 @@ __global__ __launch_bounds__(64 * kWavesPerGroup) void rotate_kernel(RotateArgs 
         y[i] = *reinterpret_cast<const Piece*>(p + d_b);
       }
     }
+  };
+  load(lane / C);
+
+  // the angle of pair `lane`, then those of the lane's pairs
+  __shared__ __attribute__((aligned(16))) float s_angle[kWavesPerGroup][2][kWave];
+  float(&angle)[2][kWave] = s_angle[threadIdx.x / kWave];
+  if (lane < half) {
+    const int w = lane / 16;
+    const uint32_t word = w == 0 ? a.axes[0] : w == 1 ? a.axes[1] : w == 2 ? a.axes[2] : a.axes[3];
+    const int axis = word >> (2 * (lane % 16)) & 3;
+    const int row = axis == 0 ? at[0] : axis == 1 ? at[1] : axis == 2 ? at[2] : at[3];
+    angle[0][lane] = a.cos[(size_t)row * half + lane];
+    angle[1][lane] = a.sin[(size_t)row * half + lane] * a.sign;
+  }
+  __builtin_amdgcn_wave_barrier();  // only this wave reads them: its LDS accesses stay in order
+  float c[P], s[P];
+  if (turns) {
+#pragma unroll
+    for (int j = 0; j < P; ++j) c[j] = angle[0][i0 + j], s[j] = angle[1][i0 + j];
+  }
+
+  for (int h0 = lane / C; h0 < a.H; h0 += HP * kAhead) {
+    if (h0 >= HP * kAhead) load(h0);
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
       const int h = h0 + HP * i;
