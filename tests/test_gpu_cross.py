@@ -313,3 +313,83 @@ def test_two_streams():
     for a, b in zip(want, got):
         for x, y in zip(a, b):
             assert torch.equal(x, y)
+
+
+def test_rows_past_32_bits():
+    """Elements past 2^31: the last source of a long packed array."""
+    T, Hq, Hkv, d = 1_100_000, 16, 16, 128
+    lens_q, lens_k, n = [T - 70, 70], [T - 100, 100], 100
+    Q, K, V, dY = make([n], [n], Hq, Hkv, d, BF16, 15)
+    big = [torch.zeros(T, 16, d, dtype=BF16, device="cuda") for _ in range(4)]
+    for x, y in zip(big, (Q, K, V, dY)):
+        x[T - n:] = y.cuda()
+    mask = torch.ones(T, dtype=torch.bool, device="cuda")
+    mask[:T - 100] = False  # the first source sees nothing
+    c, k = cu(lens_q), cu(lens_k)
+    Y, lse = avq.cross_attention_fwd(*big[:3], c, k, 0.1, mask=mask, with_lse=True)
+    check_forward(Y[T - 70:].cpu(), lse[T - 70:].cpu(), Q[30:], K, V, [70], [100], 0.1)
+    assert (Y[:T - 70] == 0).all() and (lse[:T - 70] == -math.inf).all()
+    y64, l64 = forward64(Q[30:], K, V, [70], [100], 0.1)
+    Y[T - 70:], lse[T - 70:] = y64.to(BF16).cuda(), l64.float().cuda()
+    got = avq.cross_attention_bwd(big[3], *big[:3], Y, lse, c, k, 0.1, mask=mask)
+    check_backward([got[0][T - 70:].cpu(), got[1][T - 100:].cpu(), got[2][T - 100:].cpu()], dY[30:],
+                   Q[30:], K, V, [70], [100], 0.1)
+    for x, m in zip(got, (70, 100, 100)):
+        assert (x[:T - m] == 0).all()
+
+
+def test_many_sources_of_few_states():
+    """More sources than a wave has lanes, of all lengths, some without queries, states or
+    visible ones."""
+    g = torch.Generator().manual_seed(30)
+    lens_q = torch.randint(0, 5, (150,), generator=g).tolist()
+    lens_k = (torch.randint(0, 70, (150,), generator=g) * (torch.rand(150, generator=g) < 0.8)).tolist()
+    Q, K, V, dY = make(lens_q, lens_k, 2, 1, 64, BF16, 31)
+    mask = torch.rand(sum(lens_k), generator=g) < 0.3
+    both(Q, K, V, dY, lens_q, lens_k, 0.2, mask)
+
+
+def test_unaligned_rows_are_refused():
+    Q, K, V, dY = (x.cuda() for x in make([8], [8], 2, 1, 64, BF16))
+    odd = torch.empty(8 * 128 + 1, dtype=BF16, device="cuda")[1:].view(8, 2, 64)
+    with pytest.raises(avq.AvqError):
+        avq.cross_attention_fwd(odd, K, V, cu([8]), cu([8]), 0.3)
+    Y, lse = avq.cross_attention_fwd(Q, K, V, cu([8]), cu([8]), 0.3, with_lse=True)
+    with pytest.raises(avq.AvqError):
+        avq.cross_attention_bwd(odd, Q, K, V, Y, lse, cu([8]), cu([8]), 0.3)
+
+
+def test_two_graphs():
+    """Two captured graphs, replayed in turn and at once on two streams."""
+    lens_q, lens_k = [40, 3], [200, 700]
+    c, k = cu(lens_q), cu(lens_k)
+    graphs, inputs = [], []
+    for seed in (1, 2):
+        x = [t.cuda() for t in make(lens_q, lens_k, 4, 2, 64, BF16, seed)]
+
+        def step(x=x):
+            Y, lse = avq.cross_attention_fwd(*x[:3], c, k, 0.2, with_lse=True)
+            return (Y, lse) + avq.cross_attention_bwd(x[3], *x[:3], Y, lse, c, k, 0.2)
+
+        want = step()
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            out = step()
+        graphs.append((g, out, want, torch.cuda.Stream()))
+        inputs.append(x)  # a graph reads them where they are
+    for at_once in (False, True):
+        for _ in range(3):
+            for _, out, _, _ in graphs:
+                for t in out:
+                    t.zero_()
+            torch.cuda.synchronize()
+            for g, _, _, st in graphs:
+                with torch.cuda.stream(st):
+                    g.replay()
+                if not at_once:
+                    torch.cuda.synchronize()
+            torch.cuda.synchronize()
+            for _, out, want, _ in graphs:
+                for a, b in zip(out, want):
+                    assert torch.equal(a, b)

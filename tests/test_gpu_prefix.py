@@ -299,3 +299,39 @@ def test_two_streams():
     torch.cuda.synchronize()
     for a, b in zip(want, got):
         assert torch.equal(a[0], b[0].cpu()) and torch.equal(a[1], b[1].cpu())
+
+
+@pytest.mark.parametrize("fp4", [False, True])
+def test_pages_past_32_bits(fp4):
+    """Pages that lie past 2^32 bytes of the pool."""
+    s = Setup([(300, [310, 600, 305])], 4, 2, 128, BF16, fp4, 64, seed=14)
+    E, n = s.cache.shape[2], s.n_pages
+    far = (5 << 30) // (2 * E)
+    pool = torch.zeros(far + n, 2, E, dtype=torch.uint8, device="cuda")
+    pool[far:] = s.cache.cuda()
+    table = torch.where(s.table >= 0, s.table + far, s.table)
+    lens = torch.tensor(s.lens, dtype=torch.int32)
+    Y, lse = avq.cache_prefix_attention_fwd(
+        s.Q.cuda(), pool, *(x.cuda() for x in (table.int(), lens, s.cu, s.shared)), 64, 0.2, fp4=fp4,
+        with_lse=True)
+    s.check(Y.cpu(), lse.cpu())
+
+
+def test_bad_queries_stay_in_their_sequence():
+    """An infinity or NaN in one sequence's queries leaves the others of its group."""
+    s = Setup([(300, [340, 600, 350, 301])], 4, 2, 64, BF16, False, 16, seed=15)
+    s.Q[1] = math.inf
+    s.Q[2, 0, 1] = math.nan
+    Y, lse = s.run()
+    for i in (0, 3):
+        t = Setup.__new__(Setup)
+        t.__dict__.update(s.__dict__)
+        t.Q, t.table, t.lens = s.Q[i:i + 1], s.table[i:i + 1], s.lens[i:i + 1]
+        t.check(Y[i:i + 1], lse[i:i + 1])
+
+
+def test_long_shared_positions_in_many_runs():
+    """Every run of several tiles, rows of several tiles, lengths that end anywhere."""
+    s = Setup([(2500, [2501, 2530, 2600] * 4), (1900, [1901, 2000])], 8, 1, 64, BF16, False, 64,
+              n_q=4, seed=16)
+    s.check(*s.run())

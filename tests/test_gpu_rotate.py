@@ -167,3 +167,24 @@ def test_graph_and_stream():
         torch.cuda.synchronize()
         now = avq.rotate_axes(Q, K, pos, cos, sin, axis)
         assert torch.equal(out[0], now[0]) and torch.equal(out[1], now[1])
+
+
+def test_rows_past_32_bits():
+    axis, T = blocked(64, 2), 1_100_000
+    Q, K, pos, cos, sin = make(50, 16, 1, 128, 128, 2, 9, BF16, 6)
+    big = torch.zeros(T, 16, 128, dtype=BF16, device="cuda")
+    big[T - 50:] = Q.cuda()
+    at = torch.zeros(T, 2, dtype=torch.int32, device="cuda")
+    at[T - 50:] = pos.cuda()
+    q, _ = avq.rotate_axes(big, None, at, cos.cuda(), sin.cuda(), axis)
+    check(q[T - 50:], Q, pos, cos, sin, axis, False, False)
+    assert (q[:T - 50] == 0).all()
+
+
+def test_unaligned_rows_are_refused():
+    Q, K, pos, cos, sin = (x.cuda() for x in make(7, 2, 2, 64, 64, 2, 9, BF16, 3))
+    odd = torch.empty(7 * 128 + 1, dtype=BF16, device="cuda")[1:].view(7, 2, 64)
+    with pytest.raises(avq.AvqError):
+        avq.rotate_axes(odd, K, pos, cos, sin, blocked(32, 2))
+    with pytest.raises(avq.AvqError):
+        avq.rotate_axes(Q, K, pos, cos, sin, blocked(32, 2), K_out=odd)
