@@ -677,10 +677,11 @@ int64_t avq_cache_prefix_attention_workspace(int32_t S, int32_t n_groups, int32_
  * Positions below P_g = min(shared[g], lens[cu_groups[g]]) are read through the
  * table of the group's first sequence, for all of its sequences (where sharing does
  * not pay, through each one's own; a group whose sequences do not hold the same there
- * gets unspecified outputs). A group of one sequence, and sequences of no group, share
- * nothing. If the first sequence of a group is idle (lens 0), so is the sharing: P_g =
- * 0, and every sequence reads its own pages. Y and lse are those of
- * avq_cache_attention_fwd on the same arguments, but for the rounding of the sums.
+ * gets unspecified outputs). A group of one sequence, sequences of no group, and those
+ * that hold fewer than P_g positions share nothing. If the first sequence of a group
+ * is idle (lens 0), so is the sharing: P_g = 0, and every sequence reads its own pages.
+ * Y and lse are those of avq_cache_attention_fwd on the same arguments, but for the
+ * rounding of the sums.
  *
  *   cu_groups    [n_groups + 1] int32; it must not decrease (if it does, outputs are
  *                unspecified); values outside [0, S] are taken as the nearest

@@ -905,7 +905,7 @@ def cache_prefix_attention_fwd(Q, cache, block_table, lens, cu_groups, shared, p
 
     cu_groups int32 [groups + 1]: group g is the sequences cu_groups[g] ..
     cu_groups[g + 1] - 1; shared int32 [groups]: how many first positions they have in
-    common. The other arguments, and what is returned, are those of
+    common (a sequence that holds fewer reads its own). The other arguments, and what is returned, are those of
     ``cache_attention_fwd``; workspace: a uint8 tensor of
     ``cache_prefix_attention_workspace(...)`` bytes (allocated if needed and not given).
     """

@@ -61,7 +61,9 @@ __device__ __forceinline__ int units_of(int len, int unit) {
 }
 
 // Positions that the sequences of a group attend to together: the first shared ones
-// that its first sequence holds. One sequence alone shares nothing.
+// that its first sequence holds. One sequence alone shares nothing, and a sequence that
+// holds fewer reads its own: behind its end the first one's may hold anything, and a
+// value times weight 0 is not 0 if it is infinite or NaN.
 __device__ __forceinline__ int shared_length(const CacheAttnArgs& a, int g, int first, int end) {
   if (end - first < 2) return 0;
   return max(0, min(a.shared[g], length_of(a, first)));
@@ -158,7 +160,7 @@ __device__ __forceinline__ void cache_attention_run(const CacheAttnArgs& a, cons
       __syncthreads();
     }
   }
-  auto start_of = [&](int s) {
+  auto start_of = [&](int s, int len) {
     if constexpr (!kGroups) return 0;
     auto first = [&](int i) { return in_lds ? s_cu[i] : group_first(a, i); };
     int lo = -1, hi = a.n_groups;  // first(lo) <= s < first(hi)
@@ -167,7 +169,8 @@ __device__ __forceinline__ void cache_attention_run(const CacheAttnArgs& a, cons
       if (first(mid) <= s) lo = mid; else hi = mid;
     }
     if (lo < 0 || s >= first(lo + 1)) return 0;
-    return in_lds ? s_shared[lo] : shared_length(a, lo, first(lo), first(lo + 1));
+    const int P = in_lds ? s_shared[lo] : shared_length(a, lo, first(lo), first(lo + 1));
+    return len < P ? 0 : P;  // a sequence that holds fewer shares nothing
   };
   // keys of a segment, from the octet on in which the sequence starts
   auto keys_of = [&](int len, int start) { return max(0, len - (start & ~7)); };
@@ -180,7 +183,7 @@ __device__ __forceinline__ void cache_attention_run(const CacheAttnArgs& a, cons
     if (s >= a.S) break;
     const int n = length_of(a, s);
     if (i == 0) mine_len = n;
-    mine += units_of(kGroups ? keys_of(n, start_of(s)) : n, a.unit);
+    mine += units_of(kGroups ? keys_of(n, start_of(s, n)) : n, a.unit);
   }
   const int incl = wave_incl_scan(mine);
   if (lane == kWave - 1) s_wave[wave] = incl;
@@ -206,13 +209,13 @@ __device__ __forceinline__ void cache_attention_run(const CacheAttnArgs& a, cons
   if (x >= 0 && x < mine) s_first[0] = tid * per, s_first[1] = x, s_first[2] = mine_len;
   __syncthreads();
   int s = s_first[0], len = s_first[2];
-  int start = start_of(s), n_units = units_of(kGroups ? keys_of(len, start) : len, a.unit);
+  int start = start_of(s, len), n_units = units_of(kGroups ? keys_of(len, start) : len, a.unit);
   x = s_first[1];
   while (x >= n_units && s + 1 < a.S) {
     x -= n_units;
     ++s;
     len = length_of(a, s);
-    start = start_of(s);
+    start = start_of(s, len);
     n_units = units_of(kGroups ? keys_of(len, start) : len, a.unit);
   }
 
@@ -594,7 +597,7 @@ __device__ __forceinline__ void cache_attention_run(const CacheAttnArgs& a, cons
       ++hr;
     }
     len = length_of(a, s);
-    start = start_of(s);
+    start = start_of(s, len);
     n_units = units_of(kGroups ? keys_of(len, start) : len, a.unit);
   }
 }

@@ -188,10 +188,10 @@ __device__ __forceinline__ void shared_run(const PrefixArgs& p, const Group& t, 
   // ---- the lane's row -------------------------------------------------------------
   const int per = a.n_q * a.G;
   const int row0 = r0 + 32 * wave, row = row0 + c;
-  const bool has_row = row < t.rows, wave_has = row0 < t.rows;
-  const int at_row = min(row, t.rows - 1), s = t.first + at_row / per;
+  const int at_row = min(row, t.rows - 1), s = t.first + at_row / per, len = length_of(a, s);
+  const bool has_row = row < t.rows && len >= t.P, wave_has = row0 < t.rows;
   const int qi = at_row % per / a.G, hq = hkv * a.G + at_row % a.G;
-  const int see = min(t.P, length_of(a, s) - a.n_q + qi + 1);  // positions it sees
+  const int see = min(t.P, len - a.n_q + qi + 1);  // positions it sees
   RowFrag<T> q[kRowSteps<T, D>];
   load_row<T, D>(static_cast<const T*>(a.Q) + ((size_t)s * a.n_q + qi) * a.q_stride +
                      (size_t)hq * D,

@@ -330,6 +330,25 @@ def test_bad_queries_stay_in_their_sequence():
         t.check(Y[i:i + 1], lse[i:i + 1])
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("fp4", [False, True])
+def test_bad_values_behind_a_shorter_sequence(fp4, dtype):
+    """A value that is not finite, of shared positions behind the end of one sequence,
+    is nothing to that one."""
+    s = Setup([(300, [310, 100, 640, 150])], 4, 2, 64, dtype, fp4, 16, seed=14)
+    page, slot = int(s.table[0, 200 // 16]), torch.tensor([200 % 16])
+    assert page == int(s.table[2, 200 // 16])
+    x = s.views()["Vs" if fp4 else "V"]
+    s.put(x, page, slot, "V", 0xff if fp4 else math.nan)
+    Y, lse = s.run()
+    assert not Y[[0, 2]].isfinite().any() and lse.isfinite().all()
+    for i in (1, 3):
+        K, V, ok = read_cache(s.cache, s.table, i, s.lens[i], dtype, fp4, 16, 64)
+        for h in range(4):
+            check_attention(Y[i, :, h], lse[i, :, h], s.Q[i, :, h], K[h // 2, ok], V[h // 2, ok],
+                            0.2, torch.tensor([int(ok.sum())]), f"sequence {i} head {h}")
+
+
 def test_long_shared_positions_in_many_runs():
     """Every run of several tiles, rows of several tiles, lengths that end anywhere."""
     s = Setup([(2500, [2501, 2530, 2600] * 4), (1900, [1901, 2000])], 8, 1, 64, BF16, False, 64,
