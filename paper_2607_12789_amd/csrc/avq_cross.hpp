@@ -72,15 +72,19 @@ __device__ __forceinline__ int splits_of(const CrossArgs& a, int n) {
 
 // How the work of a kernel's tiles is shared out. The host knows the sources' mean
 // lengths only: with `own` rows (or states) and `others` it runs over per source, W
-// workgroups take equal parts of the whole, but 4 or 8 steps at least. A source of
+// workgroups take equal parts of the whole, but 2 to 8 steps at least. A source of
 // four times the mean length is still divided like that, a longer one in as many
 // parts.
 struct CrossSplit {
   int per, splits;
 };
 inline CrossSplit cross_split(long long own, long long others, int S, int Hkv, int W, bool wide) {
-  // parts of many rows cost as much as some more steps
-  const int least = !wide && own / S > kCrossTile ? 8 : 4;
+  // parts of many rows cost as much as some more steps. Of few rows only one wave has
+  // any, and a step of fp32 at d = 128 takes it 4 us (one query, 2000 states, 8 heads:
+  // 24.1 us with 4 steps, 15.8 with 2; 4 queries of 8 sources of 1000, 2 key-value
+  // heads, d = 64: 17.0 and 13.2), where one of bf16 is worth less than a part (8 sources
+  // of 784, 12 heads, d = 64: 11.1 us with 4, 13.2 with 2).
+  const int least = own / S > kCrossTile ? (wide ? 4 : 8) : wide && own / S <= 32 ? 2 : 4;
   const long long tiles = ((own + S - 1) / S + kCrossTile - 1) / kCrossTile * S * Hkv;
   // parts of few rows cost little: twice as many, shorter ones, which lengths of all
   // kinds leave less uneven
