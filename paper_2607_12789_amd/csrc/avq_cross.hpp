@@ -6,8 +6,8 @@
 // r % G of its group, and 128 rows at a time read each state once. A tile is 128
 // rows (or, for the states' gradients, 128 states) of one source; lengths are
 // known on the device only, so the grid has rows / 128 + S tiles per key-value
-// head, at least as many as the sources need: tile first / 128 + s + i is the
-// i-th of source s, and those that belong to none exit.
+// head, at least as many as the sources need, and workgroups that find none exit
+// (many sources: tile first / 128 + s + i is the i-th of source s).
 #pragma once
 
 #include "avq_cache.hpp"
@@ -40,17 +40,52 @@ struct CrossArgs {
 constexpr int kCrossTile = 128;  // rows or states of a workgroup
 constexpr int kCrossWaves = 4;
 
+// Workgroups that share a tile's n steps, each about a.per of them. The same on the
+// joining side.
+__device__ __forceinline__ int splits_of(const CrossArgs& a, int n) {
+  return max(1, min(a.splits, (n + a.per - 1) / a.per));
+}
+
 struct CrossTile {
-  int s, lt;           // source, tile of its rows (or states)
+  int s, lt, hkv;      // source, tile of its rows (or states), key-value head
   int qa, ka, Lq, Lk;  // its queries and states
+  int split, splits;   // which of the workgroups that share its steps
 };
 
-// Tile of the source's rows (kStates: of its states), false if there is none.
+// The tile of this workgroup's rows (kStates: states), false if it has none.
+//
+// Up to 64 sources, one per lane: tiles, heads and splits in one line, so that the
+// workgroups without work come last. Among the others they leave some CUs with three
+// workgroups and others with one (1024 queries and states of 8 heads, d = 64, fp32:
+// forward 43.5 us so, 36.8 in one line, backward 110.7 and 99.2; 8 sources of 10 to 3000,
+// fp32: 796 and 711; 4096 queries and states twice, bf16, loses 1%).
 template <bool kStates>
-__device__ __forceinline__ bool find_cross_tile(const CrossArgs& a, int tile, int lane,
-                                                CrossTile& t) {
+__device__ __forceinline__ bool find_cross_tile(const CrossArgs& a, int lane, CrossTile& t) {
+  if (a.S <= kWave) {
+    int qa = 0, qb = 0, ka = 0, kb = 0;
+    if (lane < a.S) {
+      packed_range(a.cu_q, lane, a.Tq, qa, qb);
+      packed_range(a.cu_k, lane, a.Tk, ka, kb);
+    }
+    const int rows = (qb - qa) * a.G, own = kStates ? kb - ka : rows, others = kStates ? rows : kb - ka;
+    const int tiles = (own + kCrossTile - 1) / kCrossTile, splits = splits_of(a, (others + 31) / 32);
+    // cu that decrease could ask for more than the grid has: no sum overflows
+    const int n = min((long long)tiles * a.Hkv * splits, (long long)gridDim.x * gridDim.y);
+    const int incl = wave_incl_scan(n), w = blockIdx.y * gridDim.x + blockIdx.x;
+    if (w >= last_lane(incl)) return false;
+    t.s = __popcll(__ballot(incl <= w));
+    auto at = [&](int x) { return __builtin_amdgcn_readlane(x, t.s); };
+    t.qa = at(qa), t.Lq = at(qb) - t.qa, t.ka = at(ka), t.Lk = at(kb) - t.ka, t.splits = at(splits);
+    const int i = w - at(incl - n), j = i / a.Hkv;
+    t.hkv = i - j * a.Hkv;
+    t.split = j / at(tiles);
+    t.lt = j - t.split * at(tiles);
+    return true;
+  }
   const int per = kStates ? 1 : a.G, T = kStates ? a.Tk : a.Tq;
   const int32_t* cu = kStates ? a.cu_k : a.cu_q;
+  const int tile = blockIdx.x / a.Hkv;
+  t.hkv = blockIdx.x - tile * a.Hkv;
   t.s = find_sequence(a.S, tile, lane, [&](int k) {
     return (long long)(min(max(cu[k], 0), T) * per / kCrossTile) + k;
   });
@@ -61,13 +96,9 @@ __device__ __forceinline__ bool find_cross_tile(const CrossArgs& a, int tile, in
   t.Lk = b - t.ka;
   const int first = kStates ? t.ka : t.qa * a.G, n = kStates ? t.Lk : t.Lq * a.G;
   t.lt = tile - (first / kCrossTile + t.s);
-  return t.lt >= 0 && (long long)t.lt * kCrossTile < n;
-}
-
-// Workgroups that share a tile's n steps, each about a.per of them. The same on the
-// joining side.
-__device__ __forceinline__ int splits_of(const CrossArgs& a, int n) {
-  return max(1, min(a.splits, (n + a.per - 1) / a.per));
+  t.split = blockIdx.y;
+  t.splits = splits_of(a, ((kStates ? t.Lq * a.G : t.Lk) + 31) / 32);
+  return t.lt >= 0 && (long long)t.lt * kCrossTile < n && t.split < t.splits;
 }
 
 // How the work of a kernel's tiles is shared out. The host knows the sources' mean

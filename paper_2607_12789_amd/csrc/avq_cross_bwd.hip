@@ -47,12 +47,9 @@ void cross_dq_kernel(CrossArgs a) {
   const int lane = threadIdx.x % kWave;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int h = lane / 32, c = lane % 32;
-  const int hkv = blockIdx.x % a.Hkv, tile = blockIdx.x / a.Hkv;
   CrossTile t;
-  if (!find_cross_tile<false>(a, tile, lane, t)) return;
-  const int n_tiles = (t.Lk + 31) / 32, splits = splits_of(a, n_tiles);
-  const int split = blockIdx.y;
-  if (split >= splits) return;
+  if (!find_cross_tile<false>(a, lane, t)) return;
+  const int n_tiles = (t.Lk + 31) / 32, hkv = t.hkv, split = t.split, splits = t.splits;
   const int t_begin = (int)((long long)n_tiles * split / splits);
   const int t_end = (int)((long long)n_tiles * (split + 1) / splits);
 
@@ -202,13 +199,10 @@ void cross_dkv_kernel(CrossArgs a) {
   const int tid = threadIdx.x, lane = tid % kWave;
   const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int h = lane / 32, c = lane % 32;
-  const int hkv = blockIdx.x % a.Hkv, tile = blockIdx.x / a.Hkv;
   CrossTile t;
-  if (!find_cross_tile<true>(a, tile, lane, t)) return;
-  const int rows = t.Lq * a.G;
-  const int n_tiles = (rows + 31) / 32, splits = splits_of(a, n_tiles);
-  const int split = blockIdx.y;
-  if (split >= splits) return;
+  if (!find_cross_tile<true>(a, lane, t)) return;
+  const int rows = t.Lq * a.G, n_tiles = (rows + 31) / 32;
+  const int hkv = t.hkv, split = t.split, splits = t.splits;
   const int t_begin = (int)((long long)n_tiles * split / splits);
   const int t_end = (int)((long long)n_tiles * (split + 1) / splits);
 

@@ -65,6 +65,18 @@ def test_lengths(lens_q, lens_k, d, dtype):
     both(Q, K, V, dY, lens_q, lens_k, 1 / math.sqrt(d))
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("S", [63, 64, 65])
+@pytest.mark.parametrize("long", ["states", "queries"])
+def test_sources_of_all_lengths(long, S, dtype):
+    """As many sources as a wave has lanes, one less and one more, whose states (or
+    queries) are shared out over several workgroups, some of no length."""
+    few, many = [i * 7 % 13 for i in range(S)], [i * 331 % 400 if i % 9 else 0 for i in range(S)]
+    lens_q, lens_k = (few, many) if long == "states" else (many, few)
+    Q, K, V, dY = make(lens_q, lens_k, 2, 1, 64, dtype, 6)
+    both(Q, K, V, dY, lens_q, lens_k, 0.2)
+
+
 @pytest.mark.parametrize("Hq,Hkv", [(1, 1), (7, 1), (6, 6), (8, 2), (24, 8), (5, 5), (33, 1)])
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_heads(Hq, Hkv, dtype):
