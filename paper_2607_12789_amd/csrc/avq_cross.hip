@@ -135,19 +135,32 @@ void cross_kernel(CrossArgs a) {
 
   l = add_xor<32>(l);
   if (!fused) ms = m * a.scale_log2;
-  if (!has_row) return;
   const size_t at = (size_t)qi * a.Hq + hq;
-  if (splits > 1) {
-    const size_t rows_all = (size_t)a.Tq * a.Hq, part = split * rows_all + at;
-    store_row<float, D>(a.parts + part * D, h, 1.f, o);
-    if (h == 0) {
+  const float inv = l > 0.f ? 1.f / l : 0.f;
+  if (has_row && h == 0) {
+    if (splits > 1) {
+      const size_t rows_all = (size_t)a.Tq * a.Hq, part = split * rows_all + at;
       a.parts[a.splits * rows_all * D + part] = ms;
       a.parts[a.splits * rows_all * (D + 1) + part] = l;
+    } else if (a.lse) {
+      a.lse[at] = l > 0.f ? (ms + log2_hw(l)) * kLn2 : -INFINITY;
     }
-    return;
   }
-  store_row<T, D>(static_cast<T*>(a.Y) + at * D, h, l > 0.f ? 1.f / l : 0.f, o);
-  if (a.lse && h == 0) a.lse[at] = l > 0.f ? (ms + log2_hw(l)) * kLn2 : -INFINITY;
+  if (splits > 1) {
+    if (has_row)
+      store_row<float, D>(a.parts + ((size_t)split * a.Tq * a.Hq + at) * D, h, 1.f, o);
+  } else if (kB && rows - t.lt * kCrossTile > 32) {
+    // whole rows: 4 sources of 4096 queries and 31 to 128 states, 12 heads, d = 64, 21.7
+    // us by store_row, 18.6 so; of 1024 and 2048, 16 heads, d = 128, 113 and 107. For one
+    // row the barrier is not worth it, nor in fp32 the registers.
+    __syncthreads();  // the last tile is read
+    if (!wave_has) return;
+    const RowsOf row_of(a, t, row0);
+    store_rows<T, D, T>(lds + wave * TILE, lane, inv, o, rows - row0,
+                        [&](int r) { return static_cast<T*>(a.Y) + row_of(a, t, r) * D; });
+  } else if (has_row) {
+    store_row<T, D>(static_cast<T*>(a.Y) + at * D, h, inv, o);
+  }
 }
 
 long long tiles_of(long long rows, int S) { return rows / kCrossTile + S; }
@@ -178,6 +191,7 @@ hipError_t launch_cross_attention(int S, int Tq, int Tk, int Hq, int Hkv, float 
   a.tiles = (int)tiles_of((long long)Tq * a.G, S);
   const CrossSplit split = split_for<T>(S, Tq, Tk, Hq, Hkv);
   a.per = split.per, a.splits = split.splits;
+  a.g_reciprocal = reciprocal_of(a.G);
   a.scale = scale, a.scale_log2 = scale * kLog2e, a.lazy = kLazy / a.scale_log2;
   a.parts = static_cast<float*>(workspace);
   const dim3 grid((unsigned)(a.tiles * Hkv), (unsigned)a.splits);

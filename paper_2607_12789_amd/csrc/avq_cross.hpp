@@ -283,4 +283,53 @@ __device__ __forceinline__ void stage_states(const T* base, int64_t stride, uint
   }
 }
 
+// Stores a wave's first n rows, times f (of the lane's row), to at(r): handed over in
+// LDS (32 D sizeof(T) bytes of the wave's own), so that an instruction writes whole rows,
+// or halves, instead of 16 bytes of each of 32.
+template <typename T, int D, typename Out, typename At>
+__device__ __forceinline__ void store_rows(unsigned char* lds, int lane, float f,
+                                           const f32x16 (&o)[D / 32], int n, At at) {
+  constexpr int P = sizeof(Out) / sizeof(T), C = D / P;  // passes, columns of each
+  constexpr int U = C * (int)sizeof(Out) / 16, RPI = kWave / U;
+  const int h = lane / 32, c = lane % 32;
+#pragma unroll
+  for (int p = 0; p < P; ++p) {
+#pragma unroll
+    for (int i = 0; i < C / 32; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; r += 4) {
+        const f32x16& x = o[p * (C / 32) + i];
+        const int d0 = 32 * i + 2 * r;  // + 4 h
+        if constexpr (sizeof(Out) == 2)
+          *reinterpret_cast<bf16x4*>(lds + c * 16 * U + 16 * ((d0 / 8) ^ (c % U)) + 8 * h) =
+              bf16x4{(bf16)(x[r] * f), (bf16)(x[r + 1] * f), (bf16)(x[r + 2] * f),
+                     (bf16)(x[r + 3] * f)};
+        else
+          *reinterpret_cast<f32x4*>(lds + c * 16 * U + 16 * ((d0 / 4 + h) ^ (c % U))) =
+              f32x4{x[r] * f, x[r + 1] * f, x[r + 2] * f, x[r + 3] * f};
+      }
+    __builtin_amdgcn_wave_barrier();  // only this wave reads them: its LDS accesses stay in order
+#pragma unroll
+    for (int k = 0; k < 32 / RPI; ++k) {
+      const int r = RPI * k + lane / U, u = lane % U;
+      if (r < n)
+        *reinterpret_cast<f32x4*>(reinterpret_cast<unsigned char*>(at(r) + p * C) + 16 * u) =
+            *reinterpret_cast<const f32x4*>(lds + r * 16 * U + 16 * (u ^ (r % U)));
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
+// Query and head of row r of a wave's 32, whose first is row0 of its source and
+// key-value head.
+struct RowsOf {
+  int q0, head0;  // of row0
+  __device__ __forceinline__ RowsOf(const CrossArgs& a, const CrossTile& t, int row0)
+      : q0(t.qa + row0 / a.G), head0(row0 % a.G) {}
+  __device__ __forceinline__ size_t operator()(const CrossArgs& a, const CrossTile& t, int r) const {
+    const int x = head0 + r, dq = quotient(x, a.g_reciprocal);
+    return (size_t)(q0 + dq) * a.Hq + t.hkv * a.G + (x - dq * a.G);
+  }
+};
+
 }  // namespace avq
