@@ -325,14 +325,16 @@ __device__ __forceinline__ void shared_run(const PrefixArgs& p, const Group& t, 
   constexpr int NB = kBuffers<T, D, FP4>, AHEAD = kTilesAhead<T, D, FP4>;
   Raw raw[2];
   uint32_t bits_in[NB];
+  Pages first[AHEAD];
+#pragma unroll
+  for (int x = 0; x < AHEAD; ++x) first[x] = lookup(t_begin + x);
+  Pages ahead = lookup(t_begin + AHEAD);
 #pragma unroll
   for (int x = 0; x < AHEAD; ++x)
     if (t_begin + x < t_end) {
-      const Pages g = lookup(t_begin + x);
-      bits_in[x] = bits_of(t_begin + x, g);
-      issue(t_begin + x, g, raw[x % 2], lds.k[x], lds.v[x]);
+      bits_in[x] = bits_of(t_begin + x, first[x]);
+      issue(t_begin + x, first[x], raw[x % 2], lds.k[x], lds.v[x]);
     }
-  Pages ahead = lookup(t_begin + AHEAD);
   // the queries arrive here, before the loop: a wait for them inside it would be one
   // for the copies too
 #pragma unroll
@@ -441,15 +443,14 @@ __device__ __forceinline__ void shared_run(const PrefixArgs& p, const Group& t, 
 // heads, n positions' tiles in all and W workgroups that is between n / W and
 // n / (W - t); for up to 16 groups the lanes try 64 lengths between (80 sequences of 5
 // groups in 4 bits 58 to 44 us).
-__device__ __forceinline__ int run_tiles(const PrefixArgs& p, int lane) {
+__device__ __forceinline__ int run_tiles(const PrefixArgs& p, int lane, const Group& mine) {
   const CacheAttnArgs& a = p.c;
   const float W = p.shared_blocks, heads = a.cache.Hkv;
   float n = 0.f, t = 0.f;
-  Group mine{0, 0, 0};
   for (int g = lane; g < a.n_groups; g += kWave) {
-    mine = group_of(a, g);
-    n += (float)mine.row_tiles() * (float)mine.tiles() * heads;
-    t += (float)mine.row_tiles() * heads;
+    const Group x = g < kWave ? mine : group_of(a, g);
+    n += (float)x.row_tiles() * (float)x.tiles() * heads;
+    t += (float)x.row_tiles() * heads;
   }
   n = wave_sum(n), t = wave_sum(t);
   const int lo = max(kLeastTiles, (int)fminf(ceilf(n / W), 1e9f));
@@ -473,13 +474,14 @@ template <typename T, int D, bool FP4>
 __device__ __forceinline__ void shared_runs(const PrefixArgs& p, int w, const Buffers& lds) {
   const CacheAttnArgs& a = p.c;
   const int lane = threadIdx.x % kWave;
-  const int per = run_tiles(p, lane);
+  Group mine{0, 0, 0};  // the lane's group of those looked at
+  if (lane < a.n_groups) mine = group_of(a, lane);
+  const int per = run_tiles(p, lane, mine);
   if (w == 0 && threadIdx.x == 0) *p.per = per;
   long long before = 0;  // runs of the groups before g0
   long long next = w;
   for (int g0 = 0; g0 < a.n_groups; g0 += kWave) {
-    Group mine{0, 0, 0};
-    if (g0 + lane < a.n_groups) mine = group_of(a, g0 + lane);
+    if (g0 > 0) mine = g0 + lane < a.n_groups ? group_of(a, g0 + lane) : Group{0, 0, 0};
     const int runs = runs_of(mine.tiles(), per, p.splits);
     const int n = mine.row_tiles() * runs * a.cache.Hkv;  // at most 2^24 tiles of 64 runs
     const int incl = wave_incl_scan(n), all = last_lane(incl);
