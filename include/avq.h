@@ -647,9 +647,10 @@ int64_t avq_cross_attention_bwd_workspace(avq_dtype_t dtype, int32_t S, int32_t 
  *   dQ           [Tq][Hq][d], dK, dV [Tk][Hkv][d], dtype, contiguous, out
  *   workspace    avq_cross_attention_bwd_workspace() bytes
  * Sizes as the forward call. Two to four launches. bf16: products with fp32
- * accumulation; P and dS, fp32, are rounded to bf16 for the products they enter.
- * fp32: fp32 throughout. P is taken from lse, whose rounding leaves a relative error
- * of |lse| 2^-23 in it.
+ * accumulation; P and dS, fp32, are rounded to bf16 for the products they enter, and
+ * dY_i . Y_i, off by Y's rounding, is mended by the sum of dS, which is 0. fp32: fp32
+ * throughout. P is taken from lse, whose rounding leaves a relative error of |lse| 2^-23
+ * in it: 10^-4 for logits of a thousand, a tenth for a million.
  */
 avq_status_t avq_cross_attention_bwd(avq_dtype_t dtype, int32_t S, int32_t Tq, int32_t Tk,
                                      int32_t Hq, int32_t Hkv, int32_t d, float scale,

@@ -18,7 +18,8 @@
 // hand. There rest_i is the sum of the dS as they are rounded for the product, whose
 // errors then have no part along that sum either. dQ and dK against 64 bits, of their
 // norms: 0.0032 to 0.0038 without, 0.0022 to 0.0025 with it, where rounding them alone
-// leaves 0.0017; 4096 queries and states, 16/4 heads, d = 128, twice: 885 to 959 us.
+// leaves 0.0017; 4096 queries and states, 16/4 heads, d = 128, twice: 885 us without, 959
+// with it (both kernels and the join, on one card; 995 to 1065 on others).
 //
 // Both as the forward kernel: 32 owned rows (or states) per wave, one per lane and
 // its partner, the others in tiles of 32 through LDS, double buffered. What a tile
