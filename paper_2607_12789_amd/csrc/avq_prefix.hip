@@ -514,10 +514,15 @@ void prefix_kernel(PrefixArgs a) {
   __shared__ __attribute__((aligned(16))) unsigned char k0[TILE], k1[TILE], k2[kThird];
   __shared__ __attribute__((aligned(16))) unsigned char v0[TILE], v1[TILE], v2[kThird];
   const int n = a.shared_blocks;
+  // (assigned: LDS addresses in an initializer do not compile without optimisation)
   if ((int)blockIdx.x < n) {
-    shared_runs<T, D, FP4>(a, blockIdx.x, Buffers{{k0, k1, k2}, {v0, v1, v2}});
+    Buffers lds;
+    lds.k[0] = k0, lds.k[1] = k1, lds.k[2] = k2;
+    lds.v[0] = v0, lds.v[1] = v1, lds.v[2] = v2;
+    shared_runs<T, D, FP4>(a, blockIdx.x, lds);
   } else {
-    SharedExchange<D> area{{k0, k1, v0, v1}};
+    SharedExchange<D> area;
+    area.o[0] = k0, area.o[1] = k1, area.o[2] = v0, area.o[3] = v1;
     cache_attention_run<T, D, FP4, NT, true>(a.c, blockIdx.x - n, gridDim.x - n, area);
   }
 }
