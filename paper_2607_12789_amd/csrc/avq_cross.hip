@@ -175,7 +175,7 @@ CrossSplit split_for(int S, int Tq, int Tk, int Hq, int Hkv) {
 template <typename T, int D>
 size_t cross_attention_workspace(int S, int Tq, int Tk, int Hq, int Hkv) {
   const int splits = split_for<T>(S, Tq, Tk, Hq, Hkv).splits;
-  return splits == 1 ? 0 : (size_t)Tq * Hq * splits * (D + 2) * sizeof(float);
+  return splits == 1 ? 0 : ((size_t)Tq * Hq * splits * (D + 2) + 4) * sizeof(float);
 }
 
 template <typename T, int D>
@@ -194,6 +194,8 @@ hipError_t launch_cross_attention(int S, int Tq, int Tk, int Hq, int Hkv, float 
   a.g_reciprocal = reciprocal_of(a.G);
   a.scale = scale, a.scale_log2 = scale * kLog2e, a.lazy = kLazy / a.scale_log2;
   a.parts = static_cast<float*>(workspace);
+  a.slots = cross_slots<T, D>(S, (long long)Tq * a.G, 768);
+  a.steps = reinterpret_cast<int32_t*>(a.parts + (size_t)Tq * Hq * a.splits * (D + 2));
   const dim3 grid((unsigned)(a.tiles * Hkv), (unsigned)a.splits);
   if (mask)
     hipLaunchKernelGGL((cross_kernel<T, D, true>), grid, dim3(256), 0, stream, a);

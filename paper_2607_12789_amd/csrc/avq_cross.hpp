@@ -32,6 +32,8 @@ struct CrossArgs {
   uint32_t g_reciprocal;
   int tiles;          // per key-value head, at most
   int per, splits;    // steps of 32 that a workgroup takes; workgroups of a tile, at most
+  int slots;          // workgroups that run at once (0: steps are not chosen anew)
+  int32_t* steps;     // steps that a workgroup takes, for the joining launch
   float scale, scale_log2;
   float lazy;  // kLazy / scale_log2
   float* parts;
@@ -40,10 +42,41 @@ struct CrossArgs {
 constexpr int kCrossTile = 128;  // rows or states of a workgroup
 constexpr int kCrossWaves = 4;
 
-// Workgroups that share a tile's n steps, each about a.per of them. The same on the
+// Workgroups that share a tile's n steps, each about per of them. The same on the
 // joining side.
-__device__ __forceinline__ int splits_of(const CrossArgs& a, int n) {
-  return max(1, min(a.splits, (n + a.per - 1) / a.per));
+__device__ __forceinline__ int splits_of(const CrossArgs& a, int per, int n) {
+  return max(1, min(a.splits, (n + per - 1) / per));
+}
+
+// Time of `total` workgroups of `per` steps each, in steps: bf16, whose waves fill one
+// another's latencies, in rounds of those that run at once; fp32, whose products add up,
+// by the most on one CU, and one alone takes an eighth longer. Start and end of a workgroup
+// cost about two steps.
+__host__ __device__ inline float cross_cost(int slots, float total, float per) {
+  return slots > 256 ? ceilf(total / slots) * (per + 2.f)
+                     : per * fmaxf(1.12f, ceilf(total / 256.f)) + 2.f * ceilf(total / 256.f);
+}
+
+// Steps that a workgroup takes: the 64 lanes try a.per and the numbers behind it on the
+// sources' lengths (lane s: workgroups of one part, steps). 2 to 16 sources: us, forward
+// and backward, by the mean length and so: 5 of up to 517 queries and 1025 states, fp32, d =
+// 64, 32.9 + 94.2 and 30.6 + 80.7; 8 of up to 1500 and 3000, 12 heads, d = 64, a quarter
+// hidden, 92.1 + 187.7 and 81.2 + 193.9; 2 of 2048 and 1024, 16/4 heads, d = 64, 57.6 + 109.3
+// and 44.3 + 110.2. fp32 at d = 128 lost by it (5 of up to 1500 and 3000, 6 heads, 82.7 +
+// 563 and 90.1 + 583), as do few rows (8 of 5 and 784, 11.5 and 14.0).
+__device__ __forceinline__ int steps_of(const CrossArgs& a, int lane, int tiles, int n) {
+  const int per = a.per + lane;
+  const float inv = 1.f / per;
+  float total = 0.f;
+  for (int s = 0; s < a.S; ++s) {
+    const float parts = floorf(((float)__builtin_amdgcn_readlane(n, s) + per - 0.5f) * inv);
+    total += (float)__builtin_amdgcn_readlane(tiles, s) * fmaxf(1.f, fminf(parts, (float)a.splits));
+  }
+  const float cost = cross_cost(a.slots, total, per);
+  float least = cost;
+#pragma unroll
+  for (int k = 1; k < kWave; k *= 2) least = fminf(least, __shfl_xor(least, k, kWave));
+  return a.per + (int)__builtin_ctzll(__ballot(cost == least));
 }
 
 struct CrossTile {
@@ -68,7 +101,10 @@ __device__ __forceinline__ bool find_cross_tile(const CrossArgs& a, int lane, Cr
       packed_range(a.cu_k, lane, a.Tk, ka, kb);
     }
     const int rows = (qb - qa) * a.G, own = kStates ? kb - ka : rows, others = kStates ? rows : kb - ka;
-    const int tiles = (own + kCrossTile - 1) / kCrossTile, splits = splits_of(a, (others + 31) / 32);
+    const int tiles = (own + kCrossTile - 1) / kCrossTile, steps = (others + 31) / 32;
+    const int per = a.splits > 1 && a.slots > 0 ? steps_of(a, lane, tiles * a.Hkv, steps) : a.per;
+    if (a.splits > 1 && blockIdx.x + blockIdx.y == 0 && threadIdx.x == 0) *a.steps = per;
+    const int splits = splits_of(a, per, steps);
     // cu that decrease could ask for more than the grid has: no sum overflows
     const int n = min((long long)tiles * a.Hkv * splits, (long long)gridDim.x * gridDim.y);
     const int incl = wave_incl_scan(n), w = blockIdx.y * gridDim.x + blockIdx.x;
@@ -82,6 +118,7 @@ __device__ __forceinline__ bool find_cross_tile(const CrossArgs& a, int lane, Cr
     t.lt = j - t.split * at(tiles);
     return true;
   }
+  if (a.splits > 1 && blockIdx.x + blockIdx.y == 0 && threadIdx.x == 0) *a.steps = a.per;
   const int per = kStates ? 1 : a.G, T = kStates ? a.Tk : a.Tq;
   const int32_t* cu = kStates ? a.cu_k : a.cu_q;
   const int tile = blockIdx.x / a.Hkv;
@@ -97,7 +134,7 @@ __device__ __forceinline__ bool find_cross_tile(const CrossArgs& a, int lane, Cr
   const int first = kStates ? t.ka : t.qa * a.G, n = kStates ? t.Lk : t.Lq * a.G;
   t.lt = tile - (first / kCrossTile + t.s);
   t.split = blockIdx.y;
-  t.splits = splits_of(a, ((kStates ? t.Lq * a.G : t.Lk) + 31) / 32);
+  t.splits = splits_of(a, a.per, ((kStates ? t.Lq * a.G : t.Lk) + 31) / 32);
   return t.lt >= 0 && (long long)t.lt * kCrossTile < n && t.split < t.splits;
 }
 
@@ -127,6 +164,13 @@ inline CrossSplit cross_split(long long own, long long others, int S, int Hkv, i
   return {(int)per, (int)std::max(1LL, std::min(most, 64LL))};
 }
 
+// CrossArgs::slots of a kernel that holds W workgroups at once (bf16).
+template <typename T, int D>
+int cross_slots(int S, long long own, int W) {
+  if (S < 2 || S > 16 || own / S <= 32 || (!Elem<T>::kBf16 && D == 128)) return 0;
+  return Elem<T>::kBf16 ? W : 256;
+}
+
 // Parts: rows [splits][rows][D], where row = query * Hq + head (states: state * Hkv +
 // head); then, of the forward pass, maxima and sums [splits][rows] each; of dQ in bf16
 // sum P k [splits][rows][D] and two sums of dS [splits][rows] each; of dK dV [splits][rows][D].
@@ -153,7 +197,7 @@ __global__ __launch_bounds__(256) void cross_join_kernel(CrossArgs a) {
   packed_range(a.cu_q, s, a.Tq, qa, qb);
   packed_range(a.cu_k, s, a.Tk, ka, kb);
   if (token < (kStates ? ka : qa) || token >= (kStates ? kb : qb)) return;
-  const int n = splits_of(a, (((kStates ? (qb - qa) * a.G : kb - ka)) + 31) / 32);
+  const int n = splits_of(a, *a.steps, (((kStates ? (qb - qa) * a.G : kb - ka)) + 31) / 32);
   if (n == 1) return;  // stored already
   const int pg = (wave % kWaves * kWave + lane) / TPP, d0 = lane % TPP * 4;
   const float* const ms = a.parts + (size_t)a.splits * rows * D;

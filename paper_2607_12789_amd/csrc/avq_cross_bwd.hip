@@ -379,7 +379,7 @@ Plan plan_of(int S, int Tq, int Tk, int Hq, int Hkv) {
 template <typename T, int D>
 size_t cross_attention_bwd_workspace(int S, int Tq, int Tk, int Hq, int Hkv) {
   const Plan p = plan_of<T, D>(S, Tq, Tk, Hq, Hkv);
-  return (p.delta + p.parts) * sizeof(float);
+  return (p.delta + p.parts + 4) * sizeof(float);
 }
 
 template <typename T, int D>
@@ -400,8 +400,10 @@ hipError_t launch_cross_attention_bwd(int S, int Tq, int Tk, int Hq, int Hkv, fl
   a.g_reciprocal = reciprocal_of(a.G);
   a.scale = scale, a.scale_log2 = scale * kLog2e;
   a.delta = static_cast<float*>(workspace), a.parts = a.delta + p.delta;
+  a.steps = reinterpret_cast<int32_t*>(a.parts + p.parts);
   hipError_t e = hipSuccess;
   if (Tq > 0) {
+    a.slots = cross_slots<T, D>(S, (long long)Tq * a.G, 512);
     a.tiles = (int)p.row_tiles, a.per = p.rows.per, a.splits = p.rows.splits;
     const dim3 grid((unsigned)(a.tiles * Hkv), (unsigned)a.splits);
     if (mask)
@@ -412,6 +414,7 @@ hipError_t launch_cross_attention_bwd(int S, int Tq, int Tk, int Hq, int Hkv, fl
     if (e == hipSuccess && a.splits > 1) e = launch_cross_join<T, D, kJoinQueries>(a, stream);
   }
   if (e != hipSuccess || Tk == 0) return e;
+  a.slots = cross_slots<T, D>(S, Tk, 512);
   a.tiles = (int)p.state_tiles, a.per = p.states.per, a.splits = p.states.splits;
   const dim3 grid((unsigned)(a.tiles * Hkv), (unsigned)a.splits);
   if (mask)

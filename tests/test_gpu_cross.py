@@ -77,6 +77,16 @@ def test_sources_of_all_lengths(long, S, dtype):
     both(Q, K, V, dY, lens_q, lens_k, 0.2)
 
 
+@pytest.mark.parametrize("dtype,d", [(BF16, 64), (BF16, 128), (F32, 64), (F32, 128)])
+@pytest.mark.parametrize("S", [2, 5, 16, 17])
+def test_uneven_sources(S, d, dtype):
+    """One source holds most of the work; both its rows and its states are shared out."""
+    lens_q, lens_k = [33 + i * 7 for i in range(S)], [40 + i * 11 for i in range(S)]
+    lens_q[S // 2], lens_k[S // 2] = 700, 1500
+    Q, K, V, dY = make(lens_q, lens_k, 2, 1, d, dtype, 7)
+    both(Q, K, V, dY, lens_q, lens_k, 1 / math.sqrt(d))
+
+
 @pytest.mark.parametrize("Hq,Hkv", [(1, 1), (7, 1), (6, 6), (8, 2), (24, 8), (5, 5), (33, 1)])
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_heads(Hq, Hkv, dtype):
