@@ -316,6 +316,10 @@ void cross_dkv_kernel(CrossArgs a) {
     step(i, 0, q_even, y_even, q_odd, y_odd);
     if (i + 1 < t_end) step(i + 1, 1, q_odd, y_odd, q_even, y_even);
   }
+  if (kMask && !seen) {  // 0 also where a gradient is not finite
+#pragma unroll
+    for (int i = 0; i < DT; ++i) dk[i] = f32x16{}, dv[i] = f32x16{};
+  }
   const size_t at0 = (size_t)(t.ka + key0) * a.Hkv + hkv, rows_all = (size_t)a.Tk * a.Hkv;
   float* const part = a.parts + (split * rows_all + at0) * D;
   if (kWholeRows<T, D> && t.Lk - t.lt * kCrossTile > 32) {

@@ -78,6 +78,26 @@ def test_sources_of_all_lengths(long, S, dtype):
 
 
 @pytest.mark.parametrize("dtype,d", [(BF16, 64), (BF16, 128), (F32, 64), (F32, 128)])
+@pytest.mark.parametrize("rows", [20, 900])
+@pytest.mark.parametrize("bad", [math.inf, math.nan])
+def test_bad_gradients_and_hidden_states(bad, rows, d, dtype):
+    """States that take no part get gradients of 0, whatever the others' are; queries that
+    see no state too."""
+    lens_q, lens_k = [rows, 9], [130, 40]
+    Q, K, V, dY = make(lens_q, lens_k, 2, 1, d, dtype, 8)
+    mask = torch.arange(170) % 3 > 0
+    mask[130:] = False
+    dY[7] = dY[rows + 3] = bad
+    Y, lse = fwd(Q, K, V, lens_q, lens_k, 0.2, mask)
+    dQ, dK, dV = avq.cross_attention_bwd(gpu(dY), gpu(Q), gpu(K), gpu(V), Y, lse, cu(lens_q),
+                                         cu(lens_k), 0.2, mask=gpu(mask))
+    hidden = ~gpu(mask)
+    assert not dK[hidden].any() and not dV[hidden].any() and not dQ[rows:].any()
+    assert not dV[~hidden].isfinite().any() and not dQ[7].isfinite().any()
+    assert dQ[:7].isfinite().all() and dQ[8:].isfinite().all()
+
+
+@pytest.mark.parametrize("dtype,d", [(BF16, 64), (BF16, 128), (F32, 64), (F32, 128)])
 @pytest.mark.parametrize("S", [2, 5, 16, 17])
 def test_uneven_sources(S, d, dtype):
     """One source holds most of the work; both its rows and its states are shared out."""
