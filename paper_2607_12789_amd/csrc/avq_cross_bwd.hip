@@ -383,7 +383,7 @@ Plan plan_of(int S, int Tq, int Tk, int Hq, int Hkv) {
 template <typename T, int D>
 size_t cross_attention_bwd_workspace(int S, int Tq, int Tk, int Hq, int Hkv) {
   const Plan p = plan_of<T, D>(S, Tq, Tk, Hq, Hkv);
-  return (p.delta + p.parts + 4) * sizeof(float);
+  return (p.delta + p.parts + (p.parts > 0 ? 4 : 0)) * sizeof(float);  // and CrossArgs::steps
 }
 
 template <typename T, int D>
