@@ -157,7 +157,7 @@ inline CrossSplit cross_split(long long own, long long others, int S, int Hkv, i
   // parts of few rows cost little: twice as many, shorter ones, which lengths of all
   // kinds leave less uneven
   if (own / S <= 32) W *= 2;
-  if (tiles >= W) return {least, 1};
+  if (tiles >= W || own == 0) return {least, 1};  // nothing to divide
   const long long mean = (others / S + 31) / 32, all = (others + 31) / 32;
   const long long per = std::max<long long>(least, (tiles * mean + W - 1) / W);
   const long long most = std::min((all + per - 1) / per, 4 * ((mean + per - 1) / per));

@@ -130,6 +130,17 @@ def test_workspaces(L):
             avq.cache_prefix_attention_workspace(*bad)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("d", [64, 128])
+def test_no_queries_need_no_workspace(L, dtype, d):
+    """Without queries nothing is launched, however many states there are to divide."""
+    for S, Tk, Hq, Hkv in ((1, 1 << 16, 4, 2), (3, 40, 4, 1), (1, 1 << 24, 1, 1)):
+        assert L.avq_cross_attention_workspace(dtype, S, 0, Tk, Hq, Hkv, d) == 0
+        kw = dict(dtype=dtype, S=S, Tq=0, Tk=Tk, Hq=Hq, Hkv=Hkv, d=d, qs=Hq * d, ks=Hkv * d,
+                  vs=Hkv * d)
+        assert cross(L, Q=None, Y=None, ws=None, ws_bytes=0, **kw) == OK, L.avq_last_error()
+
+
 def test_binding_refuses_host_tensors():
     x, c = torch.zeros(4, 2, 64), torch.zeros(2, dtype=torch.int32)
     for call in (lambda: avq.rotate_axes(x, x, c[:, None], x[0], x[0], (0,) * 32),
