@@ -103,3 +103,13 @@ def test_host_abi_under_asan_ubsan(tmp_path):
                    check=True)
     _run_pytest_under(str(rt), {"AVQ_LIB": str(lib)},
                       ["test_abi_host.py", "test_order.py"], tmp_path)
+
+
+def test_serving_and_cross_calls_under_asan_ubsan(tmp_path, monkeypatch):
+    """The same build under the refusals and workspace sizes of the serving, rotation,
+    cross attention and shared-prefix calls."""
+    run = _run_pytest_under
+    monkeypatch.setattr(sys.modules[__name__], "_run_pytest_under",
+                        lambda preload, env, tests, tmp: run(
+                            preload, env, ["test_serving_host.py", "test_cross_host.py"], tmp))
+    test_host_abi_under_asan_ubsan(tmp_path)
