@@ -118,3 +118,77 @@ def check_backward(got, dY, Q, K, V, lens_q, lens_k, scale, mask=None):
         t = t * (1 + 2.0 ** -6) + HALF_STEP[x.dtype] * (y.abs() + t) + 1e-30
         err = (x.double() - y).abs()
         assert (err <= t).all(), f"{name}: off by {(err / t).max():.3g} times the bound"
+
+
+def backward_of(dY, Q, K, V, Y, lse, lens_q, lens_k, scale, mask=None):
+    """(dQ, dK, dV) and the bounds on them without the results' own rounding, where the
+    backward pass is handed any Y and lse, those that the forward kernel stored say.
+
+    As above, but for what these two are off by, which is known: lse by l_i, delta_i by
+    eta_i = dY_i . (Y_i - the exact one).
+      * P_ij is off relatively by l_i more: eP_i = ((d + 12) A_i + 4 |lse_i| + 16) u + l_i;
+      * C_i is taken of the Y handed over, and e_ij = P_ij ((eP_i + 3 u) (|dP_ij| +
+        |delta_i|) + (d + 1) u (B_ij + C_i));
+      * fp32: eS_ij = e_ij + P_ij |eta_i|;
+      * bf16: the sum of dS is -eta_i, as far as the P sum to 1 (off by eP_i): E_i = sum_j
+        (e_ij + (n + 64) u |dS_ij|) + |eta_i| (eP_i + (n + 64) u), and eS_ij = e_ij + P_ij
+        E_i;
+      * bf16, dQ: the dS rounded there hold P_ij eta_i, and so do the P that it is taken
+        off with, and rest_i as the sum of the former: P_ij h (sum_j |dS_ij| + 3 |eta_i|)
+        more.
+    """
+    Hq, G, d = Q.shape[1], Q.shape[1] // K.shape[1], Q.shape[2]
+    h16 = HALF_STEP[Q.dtype] if Q.dtype == torch.bfloat16 else 0.0
+    Y64, lse64 = forward64(Q, K, V, lens_q, lens_k, scale, mask)
+    out = [torch.zeros(x.shape, dtype=torch.float64) for x in (Q, K, V)]
+    tol = [torch.zeros(x.shape, dtype=torch.float64) for x in (Q, K, V)]
+    for (a, b), (c, e) in zip(split(lens_q), split(lens_k)):
+        keep = torch.arange(c, e)
+        if mask is not None:
+            keep = keep[mask[c:e].bool()]
+        if not len(keep) or a == b:
+            continue
+        rows, n = (b - a) * G, len(keep)
+        for h in range(Hq):
+            q, k, v, g = (Q[a:b, h].double(), K[keep, h // G].double(), V[keep, h // G].double(),
+                          dY[a:b, h].double())
+            y, y64, l64 = Y[a:b, h].double(), Y64[a:b, h], lse64[a:b, h, None]
+            P = torch.exp(scale * q @ k.T - l64)
+            dP, delta = g @ v.T, (g * y64).sum(1, keepdim=True)
+            dS = P * (dP - delta)
+            eta = (g * (y - y64)).sum(1, keepdim=True).abs()
+            A = (scale * q.abs() @ k.abs().T).amax(1, keepdim=True)
+            B, C = g.abs() @ v.abs().T, (g * y).abs().sum(1, keepdim=True)
+            eP = ((d + 12) * A + 4 * l64.abs() + 16) * U + (lse[a:b, h, None].double() - l64).abs()
+            eS = P * ((eP + 3 * U) * (dP.abs() + delta.abs()) + (d + 1) * U * (B + C))
+            if h16:
+                E = (eS + (n + 64) * U * dS.abs()).sum(1, keepdim=True) + eta * (eP + (n + 64) * U)
+                eS = eS + P * E
+            else:
+                eS = eS + P * eta
+            eS = eS + (h16 + (n + 64) * U) * dS.abs()
+            out[0][a:b, h] = scale * dS @ k
+            eQ = eS + P * h16 * (dS.abs().sum(1, keepdim=True) + 3 * eta)
+            tol[0][a:b, h] = scale * eQ @ k.abs()
+            eS = eS + (rows + 64) * U * dS.abs()
+            out[1][keep, h // G] += scale * dS.T @ q
+            tol[1][keep, h // G] += scale * eS.T @ q.abs()
+            out[2][keep, h // G] += P.T @ g
+            tol[2][keep, h // G] += (P * (eP + h16 + (rows + 64) * U)).T @ g.abs()
+    return out, tol
+
+
+def check_backward_of(got, dY, Q, K, V, Y, lse, lens_q, lens_k, scale, mask=None):
+    """got: (dQ, dK, dV) of the kernels, given this Y and lse."""
+    want, tol = backward_of(dY, Q, K, V, Y, lse, lens_q, lens_k, scale, mask)
+    for name, x, y, t in zip(("dQ", "dK", "dV"), got, want, tol):
+        assert torch.isfinite(x).all(), f"{name}: not finite"
+        t = t * (1 + 2.0 ** -6) + HALF_STEP[x.dtype] * (y.abs() + t) + 1e-30
+        err = (x.double() - y).abs()
+        assert (err <= t).all(), f"{name}: off by {(err / t).max():.3g} times the bound"
+
+
+def about(x, mean, spread):
+    """x scaled to `spread` around `mean`: values that lie close together, where what
+    delta is off by counts most (dS is small, the sums of P k are not)."""
+    return (mean + spread * x.float()).to(x.dtype)

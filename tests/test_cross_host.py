@@ -7,7 +7,7 @@ import pytest
 import torch
 
 from paper_2607_12789_amd import avq
-from tests.cross_reference import backward64, forward64
+from tests.cross_reference import about, backward64, check_backward_of, forward64
 
 OK, INVALID, UNSUPPORTED = avq.AVQ_OK, avq.AVQ_ERR_INVALID_ARG, avq.AVQ_ERR_UNSUPPORTED
 F32, BF16 = avq.AVQ_F32, avq.AVQ_BF16
@@ -179,3 +179,37 @@ def test_reference_gradients():
         assert abs((want[i] * u).sum().item() - near) <= abs(near - far) + 1e-10
     assert (want[1][~mask] == 0).all() and (want[2][~mask] == 0).all()
     assert not math.isnan(sum(t.sum().item() for t in want))
+
+
+def test_bounds_tell_a_mended_delta():
+    """The bounds on gradients from a Y that is off by its own rounding, against the
+    kernels' steps with their roundings to bf16: kept with the mended delta, not without."""
+    g = torch.Generator().manual_seed(4)
+    lens_q, lens_k, scale, h16 = [9], [70], 0.2, torch.bfloat16
+    Q, K, V, dY = (torch.randn(n, 1, 64, generator=g).to(h16) for n in (9, 70, 70, 9))
+    K, V = about(K, 1.0, 0.3), about(V, 4.0, 0.1)
+
+    def rounded(x):
+        return x.to(h16).double()
+
+    q, k, v, dy = (x[:, 0].double() for x in (Q, K, V, dY))
+    S = scale * q @ k.T
+    p = torch.exp(S - S.amax(1, keepdim=True))
+    y = rounded(rounded(p) @ v / p.sum(1, keepdim=True))
+    lse = torch.logsumexp(S, 1).float().double()
+    P = torch.exp(S - lse[:, None])
+    dP, delta = dy @ v.T, (dy * y).sum(1, keepdim=True)
+    dS = P * (dP - delta)
+    taken = rounded(dS)
+    mended = rounded(P * (dP - delta - dS.sum(1, keepdim=True)))
+    dV = rounded(P).T @ dy
+    one = [scale * taken @ k, scale * taken.T @ q, dV]
+    other = [scale * (taken @ k - taken.sum(1, keepdim=True) * (rounded(P) @ k)), scale * mended.T @ q,
+             dV]
+    args = (dY, Q, K, V, y.to(h16)[:, None], lse.float()[:, None], lens_q, lens_k, scale)
+    check_backward_of([x.to(h16)[:, None] for x in other], *args)
+    for i, name in enumerate(("dQ", "dK")):
+        mixed = list(other)
+        mixed[i] = one[i]
+        with pytest.raises(AssertionError, match=name):
+            check_backward_of([x.to(h16)[:, None] for x in mixed], *args)

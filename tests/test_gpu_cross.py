@@ -5,7 +5,8 @@ import pytest
 import torch
 
 from paper_2607_12789_amd import avq
-from tests.cross_reference import check_backward, check_forward, forward64
+from tests.cross_reference import (about, check_backward, check_backward_of, check_forward,
+                                   forward64)
 
 pytestmark = pytest.mark.gpu
 BF16, F32 = torch.bfloat16, torch.float32
@@ -435,3 +436,26 @@ def test_two_graphs():
             for _, out, want, _ in graphs:
                 for a, b in zip(out, want):
                     assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("close", [False, True])
+@pytest.mark.parametrize("lens_q,lens_k", [([37], [33]), ([300, 1], [90, 700]), ([3], [2000]),
+                                           ([513, 2, 0, 70], [40, 1100, 9, 0]),
+                                           ([5] * 20, [100] * 20), ([1] * 70, [3] * 70)])
+def test_gradients_of_what_the_forward_call_stored(lens_q, lens_k, close, d, dtype):
+    """The pair as a training step calls it: the backward pass is handed the forward
+    kernel's own Y and lse. close: keys and values that lie close together, where what
+    delta is off by through Y's rounding counts most. Some states are hidden."""
+    Q, K, V, dY = make(lens_q, lens_k, 4, 2, d, dtype, 40)
+    if close:
+        K, V = about(K, 1.0, 0.3), about(V, 4.0, 0.1)
+    mask = torch.rand(sum(lens_k), generator=torch.Generator().manual_seed(41)) < 0.8
+    scale = 1 / math.sqrt(d)
+    Y, lse = fwd(Q, K, V, lens_q, lens_k, scale, mask)
+    check_forward(Y.cpu(), lse.cpu(), Q, K, V, lens_q, lens_k, scale, mask)
+    got = avq.cross_attention_bwd(gpu(dY), gpu(Q), gpu(K), gpu(V), Y, lse, cu(lens_q), cu(lens_k),
+                                  scale, mask=gpu(mask))
+    check_backward_of([x.cpu() for x in got], dY, Q, K, V, Y.cpu(), lse.cpu(), lens_q, lens_k, scale,
+                      mask)

@@ -354,3 +354,82 @@ def test_long_shared_positions_in_many_runs():
     s = Setup([(2500, [2501, 2530, 2600] * 4), (1900, [1901, 2000])], 8, 1, 64, BF16, False, 64,
               n_q=4, seed=16)
     s.check(*s.run())
+
+
+def huge(s, page, slot):
+    """The key at a place becomes 2^40 in all dimensions."""
+    w, slots = s.views(), torch.tensor([slot])
+    if s.fp4:
+        s.put(w["Kc"], page, slots, "Kc", 0x22)  # 1 and 1
+        s.put(w["Ks"], page, slots, "Ks", 127 + 40)
+    else:
+        s.put(w["K"], page, slots, "K", 2.0 ** 40)
+
+
+@pytest.mark.parametrize("dtype,d", [(BF16, 64), (BF16, 128), (F32, 64), (F32, 128)])
+@pytest.mark.parametrize("fp4", [False, True])
+@pytest.mark.parametrize("where", ["shared", "own", "both", "last"])
+@pytest.mark.parametrize("groups", [[(600, [640, 700, 612, 330])], [(2, [2, 600, 700, 4])]])
+@pytest.mark.parametrize("scale", [0.125, 8.0])
+def test_one_huge_key_among_ordinary_ones(scale, groups, where, fp4, d, dtype):
+    """Logits of 2^43 and more take the softmax's second form, maximum first, in the
+    shared positions, in a sequence's own, or in both, where they weigh the same. Head 0
+    sees equal logits, head 1 sees the huge ones, the others with the other sign. Early
+    drafts do not see the last position ("last"), and those of a sequence of two positions
+    see none."""
+    Hq, n_q, ps = 4, 4, 16
+    s = Setup(groups, Hq, 1, d, dtype, fp4, ps, n_q, seed=20)
+    s.Q = -s.Q.abs()
+    s.Q[:, :, 0], s.Q[:, :, 1] = 0, 1
+    P = groups[0][0]
+    places = {"shared": [1], "own": [595 if P < 500 else 605], "last": [s.lens[1] - 1]}
+    places["both"] = places["shared"] + places["own"]
+    for at in places[where]:  # as sequence 1 reads it
+        huge(s, int(s.table[1, at // ps]), at % ps)
+        if at < P and P % ps > at % ps and int(s.table[1, at // ps]) != int(s.table[0, at // ps]):
+            for i in range(s.S):  # a copy of the page for each sequence
+                if s.lens[i] > at:
+                    huge(s, int(s.table[i, at // ps]), at % ps)
+    Y, lse = s.run(scale)
+    for i, n in enumerate(s.lens):
+        K, V, ok = read_cache(s.cache, s.table, i, n, dtype, fp4, ps, d)
+        assert ok.all()
+        big = K[0, :, 0] == 2.0 ** 40
+        for t in range(n_q):
+            seen = torch.arange(n) <= n - n_q + t
+            here = seen & big
+            for h in range(Hq):
+                what = f"sequence {i} token {t} head {h}"
+                y, l = Y[i, t, h], lse[i, t, h]
+                if h != 1 or not here.any():
+                    keep = seen if h < 2 else seen & ~big
+                    check_attention(y[None], l[None], s.Q[i, t, h][None], K[0, keep], V[0, keep],
+                                    scale, torch.tensor([int(keep.sum())]), what)
+                    continue
+                # the mean of their values, as summed and divided in fp32 and rounded; the
+                # maximum is exact, log2(e), its product, ln 2 and theirs are rounded
+                v = V[0, here]
+                tol = 2.0 ** -8 if dtype == BF16 else 2.0 ** -24
+                tol = tol * v.mean(0).abs() + 3 * 2.0 ** -24 * v.abs().sum(0)
+                assert ((y.double() - v.mean(0)).abs() <= tol).all(), what
+                assert abs(l.item() / (scale * d * 2.0 ** 40) - 1) <= 5 * 2.0 ** -24, what
+
+
+@pytest.mark.parametrize("fp4", [False, True])
+@pytest.mark.parametrize("n", [16, 17, 20, 64, 65, 80])
+def test_many_groups_in_many_runs(n, fp4):
+    """16 groups and more, which are looked at 64 at a time: shared positions of all lengths
+    from none to 63 tiles, whose runs are several for some and one for others, also behind
+    the 64th group."""
+    shared = [(i * 613) % 400 if i % 6 else (i * 977) % 2000 for i in range(n)]
+    shared[1], shared[n - 1] = 2000, 1990
+    groups = [(m, [m + 1 + i % 9, m + 4]) for i, m in enumerate(shared)]
+    s = Setup(groups, 2, 1, 64, BF16, fp4, 64, seed=21)
+    Y, lse = s.run()
+    few = sorted({0, 1, 2, 5, 6, 12, 15, n // 2, n - 2, n - 1} | set(range(63, n)))
+    for g in few:
+        t = Setup.__new__(Setup)
+        t.__dict__.update(s.__dict__)
+        own = slice(2 * g, 2 * g + 2)
+        t.Q, t.table, t.lens = s.Q[own], s.table[own], s.lens[own]
+        t.check(Y[own], lse[own])
