@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from paper_2607_12789_amd import avq
-from tests.cross_reference import (about, check_backward, check_backward_of, check_forward,
+from tests.cross_reference import (HALF_STEP, about, check_backward, check_backward_of, check_forward,
                                    forward64)
 
 pytestmark = pytest.mark.gpu
@@ -459,3 +459,50 @@ def test_gradients_of_what_the_forward_call_stored(lens_q, lens_k, close, d, dty
                                   scale, mask=gpu(mask))
     check_backward_of([x.cpu() for x in got], dY, Q, K, V, Y.cpu(), lse.cpu(), lens_q, lens_k, scale,
                       mask)
+
+
+def huge(lens_k, at, Hq, Hkv, d, dtype):
+    """Two sources of 34 queries; states `at` of the first are 2^40. Query 0 of each sees
+    equal logits, query 1 sees the huge ones, the others see them with the other sign."""
+    Q, K, V, _ = make([34, 34], lens_k, Hq, Hkv, d, dtype, 42)
+    Q = -Q.abs()
+    Q[0] = Q[34] = 0
+    Q[1] = Q[35] = 1
+    K[at] = 2.0 ** 40
+    return Q, K, V
+
+
+@pytest.mark.parametrize("dtype,d", [(BF16, 64), (BF16, 128), (F32, 64), (F32, 128)])
+@pytest.mark.parametrize("n,at,divided", [(60, [40], False), (88, [0], False), (60, [59], False),
+                                          (88, [10, 87], False), (300, [200], True),
+                                          (3000, [0], True), (3000, [1500, 2999], True)])
+@pytest.mark.parametrize("masked", [False, True])
+def test_one_huge_state_among_ordinary_ones(masked, n, at, divided, d, dtype):
+    """Logits of 2^43 and more take the softmax's second form, maximum first, in some
+    parts of the states and not in others."""
+    Hq, Hkv, lens_q, lens_k = 2, 1, [34, 34], [n, 40]
+    Q, K, V = huge(lens_k, at, Hq, Hkv, d, dtype)
+    mask = None
+    if masked:  # a huge one more, which is hidden, and ordinary ones
+        mask = torch.arange(n + 40) % 7 != 3
+        mask[at] = True
+        K[3] = 2.0 ** 41
+        assert not mask[3]
+    assert (avq.cross_attention_workspace(dtype, 2, 68, n + 40, Hq, Hkv, d) > 0) == divided
+    Y, lse = (x.cpu() for x in fwd(Q, K, V, lens_q, lens_k, 0.125, mask))
+    seen = torch.ones(n, dtype=torch.bool) if mask is None else mask[:n]
+    check_forward(Y[:1], lse[:1], Q[:1], K[:n], V[:n], [1], [n], 0.125, seen)
+    # the mean of the huge ones' values: their sum and its quotient rounded in fp32, then
+    # to the type
+    v = V[at, 0].double()
+    tol = HALF_STEP[dtype] * v.mean(0).abs() + 3 * 2.0 ** -24 * v.abs().sum(0)
+    if len(at) == 1:
+        tol = torch.zeros_like(tol)
+    assert ((Y[1].double() - v.mean(0)).abs() <= tol).all()
+    # the maximum is exact; log2(e), its product, ln 2 and theirs are rounded
+    assert ((lse[1].double() / (0.125 * d * 2.0 ** 40) - 1).abs() <= 5 * 2.0 ** -24).all()
+    rest = seen.clone()
+    rest[at] = False
+    check_forward(Y[2:34], lse[2:34], Q[2:34], K[:n], V[:n], [32], [n], 0.125, rest)
+    check_forward(Y[34:], lse[34:], Q[34:], K[n:], V[n:], [34], [40], 0.125,
+                  None if mask is None else mask[n:])
