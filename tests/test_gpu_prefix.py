@@ -413,3 +413,23 @@ def test_one_huge_key_among_ordinary_ones(scale, groups, where, fp4, d, dtype):
                 tol = tol * v.mean(0).abs() + 3 * 2.0 ** -24 * v.abs().sum(0)
                 assert ((y.double() - v.mean(0)).abs() <= tol).all(), what
                 assert abs(l.item() / (scale * d * 2.0 ** 40) - 1) <= 5 * 2.0 ** -24, what
+
+
+@pytest.mark.parametrize("fp4", [False, True])
+@pytest.mark.parametrize("n", [16, 17, 20, 64, 65, 80])
+def test_many_groups_in_many_runs(n, fp4):
+    """16 groups and more, which are looked at 64 at a time: shared positions of all lengths
+    from none to 63 tiles, whose runs are several for some and one for others, also behind
+    the 64th group."""
+    shared = [(i * 613) % 400 if i % 6 else (i * 977) % 2000 for i in range(n)]
+    shared[1], shared[n - 1] = 2000, 1990
+    groups = [(m, [m + 1 + i % 9, m + 4]) for i, m in enumerate(shared)]
+    s = Setup(groups, 2, 1, 64, BF16, fp4, 64, seed=21)
+    Y, lse = s.run()
+    few = sorted({0, 1, 2, 5, 6, 12, 15, n // 2, n - 2, n - 1} | set(range(63, n)))
+    for g in few:
+        t = Setup.__new__(Setup)
+        t.__dict__.update(s.__dict__)
+        own = slice(2 * g, 2 * g + 2)
+        t.Q, t.table, t.lens = s.Q[own], s.table[own], s.lens[own]
+        t.check(Y[own], lse[own])
