@@ -680,7 +680,8 @@ int64_t avq_cache_prefix_attention_workspace(int32_t S, int32_t n_groups, int32_
  * not pay, through each one's own; a group whose sequences do not hold the same there
  * gets unspecified outputs). A group of one sequence, sequences of no group, and those
  * that hold fewer than P_g positions share nothing. If the first sequence of a group
- * is idle (lens 0), so is the sharing: P_g = 0, and every sequence reads its own pages.
+ * is idle (lens 0), so is the sharing: P_g = 0, and every sequence reads its own pages;
+ * put one that is not idle first.
  * Y and lse are those of avq_cache_attention_fwd on the same arguments, but for the
  * rounding of the sums.
  *
@@ -691,7 +692,10 @@ int64_t avq_cache_prefix_attention_workspace(int32_t S, int32_t n_groups, int32_
  *   workspace    avq_cache_prefix_attention_workspace() bytes; NULL allowed if
  *                max_pages * page_size <= AVQ_CACHE_UNDIVIDED (nothing is then shared)
  * n_groups >= 1; (S n_q Hq / Hkv / 128 + n_groups) Hkv < 2^24. Two launches, one without a
- * workspace. It pays from a few tens of megabytes on that are read less.
+ * workspace. It pays in batches of dozens of sequences, four or more a group (in 4 bits
+ * eight), that share thousands of positions. In smaller batches and groups, with shorter
+ * shared parts, or where most positions are the sequences' own, avq_cache_attention_fwd is
+ * as fast or faster (32 pairs in 4 bits: up to four times): the choice is the caller's.
  */
 avq_status_t avq_cache_prefix_attention_fwd(avq_dtype_t dtype, avq_cache_t format, int32_t S,
                                             int32_t n_groups, int32_t n_q, int32_t Hq, int32_t Hkv,

@@ -905,9 +905,11 @@ def cache_prefix_attention_fwd(Q, cache, block_table, lens, cu_groups, shared, p
 
     cu_groups int32 [groups + 1]: group g is the sequences cu_groups[g] ..
     cu_groups[g + 1] - 1; shared int32 [groups]: how many first positions they have in
-    common (a sequence that holds fewer reads its own). The other arguments, and what is returned, are those of
-    ``cache_attention_fwd``; workspace: a uint8 tensor of
-    ``cache_prefix_attention_workspace(...)`` bytes (allocated if needed and not given).
+    common (a sequence that holds fewer reads its own). Where groups are small or most
+    positions are the sequences' own, ``cache_attention_fwd`` is faster. The other
+    arguments, and what is returned, are those of ``cache_attention_fwd``; workspace: a
+    uint8 tensor of ``cache_prefix_attention_workspace(...)`` bytes (allocated if needed
+    and not given).
     """
     S, n_q, Hq, d, q_stride = _newest(Q)
     n_pages, Hkv, _, max_pages = _cache(cache, block_table, Q.dtype, page_size, d, fp4, S)

@@ -400,10 +400,11 @@ bool cross_tiles_fit(int32_t S, int32_t Tq, int32_t Tk, int32_t Hq, int32_t Hkv)
   const int64_t rows = (int64_t)Tq * (Hq / Hkv);
   return (rows / 128 + S) * Hkv < kMaxBlocks && ((int64_t)Tk / 128 + S) * Hkv < kMaxBlocks;
 }
-bool cross_sizes(avq_dtype_t dtype, int32_t S, int32_t Tq, int32_t Tk, int32_t Hq, int32_t Hkv, int32_t d) {
-  return (dtype == AVQ_F32 || dtype == AVQ_BF16) && S >= 1 && S <= (1 << 20) && Hq >= 1 && Hkv >= 1 && Hq <= kMaxHeads && Hq % Hkv == 0 &&
-         (d == 64 || d == 128) && Tq >= 0 && Tk >= 0 && Tq <= (1 << 24) && Tk <= (1 << 24) &&
-         cross_tiles_fit(S, Tq, Tk, Hq, Hkv);
+bool cross_sizes(avq_dtype_t dtype, int32_t S, int32_t Tq, int32_t Tk, int32_t Hq, int32_t Hkv,
+                 int32_t d) {
+  return (dtype == AVQ_F32 || dtype == AVQ_BF16) && S >= 1 && S <= (1 << 20) && Hq >= 1 &&
+         Hkv >= 1 && Hq <= kMaxHeads && Hq % Hkv == 0 && (d == 64 || d == 128) && Tq >= 0 &&
+         Tk >= 0 && Tq <= (1 << 24) && Tk <= (1 << 24) && cross_tiles_fit(S, Tq, Tk, Hq, Hkv);
 }
 
 avq_status_t check_cross(const char* name, avq_dtype_t dtype, int32_t S, int32_t Tq, int32_t Tk,

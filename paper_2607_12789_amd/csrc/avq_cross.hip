@@ -151,7 +151,7 @@ void cross_kernel(CrossArgs a) {
       store_row<float, D>(a.parts + ((size_t)split * a.Tq * a.Hq + at) * D, h, 1.f, o);
   } else if (kB && rows - t.lt * kCrossTile > 32) {
     // whole rows: 4 sources of 4096 queries and 31 to 128 states, 12 heads, d = 64, 21.7
-    // us by store_row, 18.6 so; of 1024 and 2048, 16 heads, d = 128, 113 and 107. For one
+    // us by store_row, 18.6 so; of 1024 and 2048, 16 heads, d = 128, 113 and 109. For one
     // row the barrier is not worth it, nor in fp32 the registers.
     __syncthreads();  // the last tile is read
     if (!wave_has) return;

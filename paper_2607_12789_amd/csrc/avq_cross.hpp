@@ -64,6 +64,11 @@ __host__ __device__ inline float cross_cost(int slots, float total, float per) {
 // hidden, 92.1 + 187.7 and 81.2 + 193.9; 2 of 2048 and 1024, 16/4 heads, d = 64, 57.6 + 109.3
 // and 44.3 + 110.2. fp32 at d = 128 lost by it (5 of up to 1500 and 3000, 6 heads, 82.7 +
 // 563 and 90.1 + 583), as do few rows (8 of 5 and 784, 11.5 and 14.0).
+// Backward in bf16, by the mean length and so: 3 sources of up to 1500 and 3000, 16/4 heads,
+// d = 128, 251 and 212; 16 of up to 600 and 900, 8/2 heads, d = 128, 120 and 106; 4 of 4096
+// and 31 to 128, 12 heads, d = 64, 59.6 and 58.2. Sources of one length are as they were or
+// lose up to 2% (4 of 256 and 2048, 16/4 heads, d = 64, 86.0 and 87.4); most lost 8 of up to
+// 1500 and 3000, 12 heads, d = 64, of other lengths than above: 155 and 170, all of it in dQ.
 __device__ __forceinline__ int steps_of(const CrossArgs& a, int lane, int tiles, int n) {
   const int per = a.per + lane;
   const float inv = 1.f / per;
@@ -142,7 +147,10 @@ __device__ __forceinline__ bool find_cross_tile(const CrossArgs& a, int lane, Cr
 // lengths only: with `own` rows (or states) and `others` it runs over per source, W
 // workgroups take equal parts of the whole, but 2 to 8 steps at least. A source of
 // four times the mean length is still divided like that, a longer one in as many
-// parts.
+// parts. A tile has 64 parts at most, one for each lane of the joining wave: few tiles over
+// very many states leave CUs without work (one query of 8 heads that share a key-value
+// head, bf16, d = 128: 65536 states 30 us, 2^20 states 500, 5 times as long as their bytes
+// take; of 16 heads, 4 key-value heads, 33 and 570).
 struct CrossSplit {
   int per, splits;
 };
@@ -164,7 +172,12 @@ inline CrossSplit cross_split(long long own, long long others, int S, int Hkv, i
   return {(int)per, (int)std::max(1LL, std::min(most, 64LL))};
 }
 
-// CrossArgs::slots of a kernel that holds W workgroups at once (bf16).
+// CrossArgs::slots of a kernel that holds W workgroups at once (bf16). The steps of more
+// than 16 sources are not chosen anew, which the forward call would pay for: us, forward and
+// backward, so and chosen, of up to 500 and 1500, 4 heads, d = 64, bf16: 17 sources 27 + 74 and
+// 29 + 68, 32 31 + 67 and 38 + 66, 64 51 + 99 and 71 + 100; fp32 of up to 400 and 900, 4/2
+// heads: 17 47 + 145 and 47 + 129, 48 76 + 261 and 80 + 262. 8/2 heads, d = 128, bf16, would
+// gain: 17 45 + 134 and 48 + 116, 32 79 + 203 and 72 + 189, 64 79 + 270 and 79 + 270.
 template <typename T, int D>
 int cross_slots(int S, long long own, int W) {
   if (S < 2 || S > 16 || own / S <= 32 || (!Elem<T>::kBf16 && D == 128)) return 0;

@@ -37,7 +37,8 @@ namespace {
 // Whole rows are stored at once (store_rows) where that leaves the kernels their
 // registers: 4 sources of 4096 queries and 31 to 128 states, 12 heads, bf16, d = 64, 64.2
 // us by store_row, 59.6 so; 4096 queries and states twice, d = 128, 1001 and 1065 (8 to 10
-// registers spilled), 8 sources of 10 to 3000, fp32, d = 64, 709 and 765.
+// registers spilled; as they are, dQ's kernel spills 3 with a mask, dK's and dV's 1 without
+// one), 8 sources of 10 to 3000, fp32, d = 64, 709 and 765.
 template <typename T, int D>
 constexpr bool kWholeRows = Elem<T>::kBf16 && D == 64;
 

@@ -442,7 +442,11 @@ __device__ __forceinline__ void shared_run(const PrefixArgs& p, const Group& t, 
 // there are that many workgroups. Runs are whole tiles, so with t tiles of rows and
 // heads, n positions' tiles in all and W workgroups that is between n / W and
 // n / (W - t); for up to 16 groups the lanes try 64 lengths between (80 sequences of 5
-// groups in 4 bits 58 to 44 us).
+// groups in 4 bits 58 to 44 us). For more, every workgroup would go through all groups
+// first. us, by the longest and so, groups of 2 to 6, d = 128, bf16 and 4 bits: 32 that share
+// up to 6000, one key-value head, 27 / 29 and 31 / 32; 48 of up to 8000 38 / 39 and 42 / 44; 64
+// of up to 6000 41 / 43 and 44 / 46. With 4 key-value heads it would gain: 17 of up to 12000
+// 64 / 70 and 58 / 62, 32 of up to 6000 71 / 78 and 58 / 62.
 __device__ __forceinline__ int run_tiles(const PrefixArgs& p, int lane, const Group& mine) {
   const CacheAttnArgs& a = p.c;
   const float W = p.shared_blocks, heads = a.cache.Hkv;
@@ -632,7 +636,11 @@ hipError_t launch_tiles(PrefixArgs& a, hipStream_t stream) {
   // As many workgroups as run at once, one per CU of them (the first) for the shared
   // positions: two of these on a CU take nearly twice as long. us (d = 128, bf16) with
   // 256 of 512 workgroups and with as many as the work's proportion asks for, up to 448:
-  // 256 sequences that share 32000 positions 139 / 163, 64 that share 16000 41 / 42.
+  // 256 sequences that share 32000 positions 139 / 163, 64 that share 16000 41 / 42. Those
+  // that find nothing shared exit, and the sequences' own positions have the others alone:
+  // with nothing to share this takes longer than the attention without groups (64 groups of
+  // one sequence of 4000, 16/4 heads: bf16 100 and 100, 4 bits 49 and 32; 16 of these: 32
+  // and 27, 22 and 16).
   const int W = std::min(kMaxWorkgroups / NT, dev.cus * kPrefixPerCu<T, D, FP4, NT>);
   a.shared_blocks = std::min(dev.cus, W / 2);
   hipLaunchKernelGGL((prefix_kernel<T, D, FP4, NT>), dim3((unsigned)W), dim3(kThreads), 0, stream, a);
