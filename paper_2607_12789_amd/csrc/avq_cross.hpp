@@ -149,7 +149,7 @@ __device__ __forceinline__ bool find_cross_tile(const CrossArgs& a, int lane, Cr
 // four times the mean length is still divided like that, a longer one in as many
 // parts. A tile has 64 parts at most, one for each lane of the joining wave: few tiles over
 // very many states leave CUs without work (one query of 8 heads that share a key-value
-// head, bf16, d = 128: 65536 states 30 us, 2^20 states 500, 5 times as long as their bytes
+// head, bf16, d = 128: 65536 states 30 us, 2^20 states 500, almost 5 times what their bytes
 // take; of 16 heads, 4 key-value heads, 33 and 570).
 struct CrossSplit {
   int per, splits;
